@@ -271,6 +271,46 @@ int kvb_direct(const kvb_shape *shape, const kvb_store *store, const int32_t *sl
                const float *g, const float *beta, void *out, void *stream);
 
 /*
+ * Whole sequences: ragged, packed along one token axis.  Sequence b's tokens are rows start[b] .. start[b+1]-1 of
+ * every token array (an empty sequence is fine).  shape: B sequences; cap and rec_dtype are not looked at.
+ */
+typedef struct kvb_seqs {
+    const int32_t *start;    /* device [B+1], ascending, within 0..n_tokens (cut off to that)          */
+    const int32_t *slot;     /* device [B]: sequence b's states are row slot[b] of the state arrays; a
+                                sequence whose slot is outside 0..n_slots-1 is skipped, no slot may
+                                appear twice.  NULL: row b                                             */
+    int64_t  q_stride;       /* elements from one token's row of q to the next, so that q, k and v may   */
+    int64_t  k_stride;       /* be parts of the rows of one projection: at least the row, in bytes a     */
+    int64_t  v_stride;       /* multiple of 16; 0: packed.  Heads of a token are contiguous              */
+    int32_t  n_tokens;       /* rows of the token arrays                                               */
+    int32_t  n_slots;        /* rows of the state arrays                                               */
+} kvb_seqs;
+
+/*
+ * kvb_scan -- the recurrence over whole sequences of any length, the way a prompt that no record
+ * buffer holds enters a state (and the forward pass of training).  From state0, for each token in order,
+ *      e_t = v_t - alpha_t k_t S,  S <- alpha_t S + beta_t k_t^T e_t,  o_t = scale q_t S       (Eq. 11-12)
+ * in chunks of 64 tokens with all arithmetic to fp32 (16-bit inputs are exact).
+ *   q, k    device [n_tokens, Hk, dk] in_dtype     v  device [n_tokens, Hv, dv] in_dtype
+ *   g, beta device [n_tokens, Hv] fp32
+ *   state0  device [n_slots, Hv, dk, dv] fp32, or NULL: zero
+ *   state1  the same, written: the state behind the last token (an empty sequence's is its state0); NULL:
+ *           not wanted.  May be state0.  With a store's state array and the requests' slots, kvb_decode
+ *           and the other calls go on from there (the record buffers must be empty, fill 0).
+ *   out     device [n_tokens, Hv, dv] out_dtype, packed
+ *   work    device, kvb_scan_work(shape, seqs) bytes, 16-byte aligned; what it holds means nothing
+ *           before and after the call.  kvb_scan_work depends on B, Hv and n_tokens alone, grows with
+ *           them, and returns one of the error codes for what the call would refuse.
+ * Head sizes and types as elsewhere: dk == dv in {32, 64, 128}, fp32, bf16 or fp16.
+ * A value that is not finite may make NaN of any output of its head in the 64-token chunk that holds it (counted from the
+ * sequence's start) and behind it; log decays down to -infinity are fine.
+ */
+int64_t kvb_scan_work(const kvb_shape *shape, const kvb_seqs *seqs);
+int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs,
+             const void *q, const void *k, const void *v, const float *g, const float *beta,
+             const float *state0, float *state1, void *out, void *work, void *stream);
+
+/*
  * Kernel timer (measurement aid, no part of the method).  A timer owns two HIP events.
  * kvb_timer_arm makes the NEXT kernel that the calling thread launches through this
  * library record its own begin and end timestamps into them; kvb_timer_read waits for that

@@ -1,6 +1,6 @@
 // Host side of the library: argument checks (all before the first HIP call), the extern "C" entry
 // points of include/kvb.h, the kernel timer.
-#include "kvb_device.h"
+#include "kvb_scan_device.h"
 
 namespace kvb_impl {
 
@@ -147,9 +147,87 @@ int step_common(const kvb_shape *sh, const kvb_store *st, const int32_t *slot, i
     return finish_launch();
 }
 
+// The element types and head sizes of a scan (cap and rec_dtype of the shape mean nothing there), and its sequences.
+int check_seqs(const kvb_shape *sh, const kvb_seqs *sq)
+{
+    if (!sh || !sq)
+        return KVB_EINVAL;
+    if (sh->B < 0 || sh->Hk <= 0 || sh->Hv <= 0 || sh->Hv % sh->Hk != 0 || sh->dk <= 0 || sh->dv <= 0)
+        return KVB_EINVAL;
+    if (sq->n_tokens < 0 || sq->n_slots < 0)
+        return KVB_EINVAL;
+    if (sh->in_dtype != KVB_F32 && sh->in_dtype != KVB_BF16 && sh->in_dtype != KVB_F16)
+        return KVB_EUNSUPPORTED;
+    if (sh->out_dtype != KVB_F32 && (sh->in_dtype == KVB_F32 || sh->out_dtype != sh->in_dtype))
+        return KVB_EUNSUPPORTED;
+    if (sh->dk != sh->dv || (sh->dk != 32 && sh->dk != 64 && sh->dk != 128))
+        return KVB_EUNSUPPORTED;
+    const int64_t size = sh->in_dtype == KVB_F32 ? 4 : 2, width[3] = {(int64_t)sh->Hk * sh->dk, (int64_t)sh->Hk * sh->dk, (int64_t)sh->Hv * sh->dv};
+    const int64_t stride[3] = {sq->q_stride, sq->k_stride, sq->v_stride};
+    for (int i = 0; i < 3; ++i)
+        if (stride[i] != 0 && (stride[i] < width[i] || stride[i] > INT64_MAX / 4 / ((int64_t)sq->n_tokens + 1) || stride[i] * size % 16 != 0))
+            return KVB_EINVAL;
+    // one workgroup for each chunk and qk-head, and up to eight for each sequence and v-head
+    if (scan_chunks(sq->n_tokens, sh->B) > INT32_MAX / sh->Hk || (int64_t)sh->B * sh->Hv > INT32_MAX / 8)
+        return KVB_EINVAL;
+    return KVB_OK;
+}
+int check_seq_pointers(const kvb_shape *sh, const kvb_seqs *sq, const void *q, const void *k, const void *v, const float *g,
+                       const float *beta, const float *state0, const void *work)
+{
+    if (!sq->start || !aligned(sq->start, 4) || !aligned(sq->slot, 4) || !aligned(state0, 16) || !aligned(work, 16))
+        return KVB_EINVAL;
+    if (sq->n_tokens > 0 && !work)
+        return KVB_EINVAL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(g, 4) || !aligned(beta, 4))
+        return KVB_EINVAL;
+    if (sq->n_tokens > 0 && (!q || !k || !v || !g || !beta))
+        return KVB_EINVAL;
+    return KVB_OK;
+}
+
+int64_t scan_work_bytes(const kvb_shape *sh, const kvb_seqs *sq)
+{
+    return 4 * scan_chunks(sq->n_tokens, sh->B) * sh->Hv * SCAN_PREP;
+}
+
 }  // namespace
 
 extern "C" {
+
+int64_t kvb_scan_work(const kvb_shape *shape, const kvb_seqs *seqs)
+{
+    const int rc = check_seqs(shape, seqs);
+    return rc != KVB_OK ? rc : scan_work_bytes(shape, seqs);
+}
+
+int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs, const void *q, const void *k, const void *v, const float *g, const float *beta,
+             const float *state0, float *state1, void *out, void *work, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_seqs(shape, seqs);
+    if (rc == KVB_OK)
+        rc = check_seq_pointers(shape, seqs, q, k, v, g, beta, state0, work);
+    if (rc != KVB_OK)
+        return rc;
+    if (!aligned(state1, 16) || !aligned(out, 16) || (seqs->n_tokens > 0 && !out))
+        return KVB_EINVAL;
+    if (shape->B == 0)
+        return KVB_OK;
+    const int64_t qk = (int64_t)shape->Hk * shape->dk, vv = (int64_t)shape->Hv * shape->dv;
+    ScanArgs a{q, k, v, g, beta, state0, state1, out, seqs->start, seqs->slot, static_cast<float *>(work),
+               seqs->q_stride ? seqs->q_stride : qk, seqs->k_stride ? seqs->k_stride : qk, seqs->v_stride ? seqs->v_stride : vv,
+               shape->B, seqs->n_slots, seqs->n_tokens, shape->Hk, shape->Hv, shape->Hv / shape->Hk, shape->out_dtype == KVB_F32, shape->scale};
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    g_launch_status = hipSuccess;
+    if (shape->in_dtype == KVB_F32)
+        launch_scan_typed<float>(shape->dk, a, hs);
+    else if (shape->in_dtype == KVB_BF16)
+        launch_scan_typed<bf16_t>(shape->dk, a, hs);
+    else
+        launch_scan_typed<f16_t>(shape->dk, a, hs);
+    return finish_launch();
+}
 
 int kvb_decode(const kvb_shape *shape, const kvb_store *store, const int32_t *slot, const void *q, const void *k,
                const void *v, const float *g, const float *beta, void *out, void *stream)

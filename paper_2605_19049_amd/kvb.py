@@ -20,6 +20,7 @@ STORE_STREAM, STORE_RESIDENT, STORE_FILL_APART = 1, 2, 4
 FILL_APART = 32   # words from one slot's fill to the next with STORE_FILL_APART
 
 EXPORTS = ("kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact", "kvb_direct",
+           "kvb_scan_work", "kvb_scan",
            "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read", "kvb_timer_destroy",
            "kvb_strerror", "kvb_version")
 
@@ -37,6 +38,12 @@ class KvbStore(ctypes.Structure):
                 ("n_slots", ctypes.c_int32), ("flags", ctypes.c_int32),
                 ("block_table", ctypes.c_void_p), ("block_size", ctypes.c_int32),
                 ("max_blocks", ctypes.c_int32), ("n_blocks", ctypes.c_int32)]
+
+
+class KvbSeqs(ctypes.Structure):
+    _fields_ = [("start", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("n_tokens", ctypes.c_int32),
+                ("n_slots", ctypes.c_int32)]
 
 
 class KvbError(RuntimeError):
@@ -71,7 +78,11 @@ def lib():
         L.kvb_verify_tree.argtypes = [sp, tp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp]
         L.kvb_compact.argtypes = [sp, tp, vp, i32, vp, vp, vp]
         L.kvb_direct.argtypes = [sp, tp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp]
-        for name in ("kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
+        qp = ctypes.POINTER(KvbSeqs)
+        L.kvb_scan_work.argtypes = [sp, qp]
+        L.kvb_scan.argtypes = [sp, qp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.kvb_scan_work.restype = ctypes.c_int64
+        for name in ("kvb_scan", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
                      "kvb_direct", "kvb_version",
                      "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read"):
             getattr(L, name).restype = ctypes.c_int
@@ -215,6 +226,35 @@ def kvb_direct(sh, st, slot, lens, Lmax, q, k, v, g, beta, out, stream=None, che
     rc = lib().kvb_direct(ctypes.byref(sh), ctypes.byref(st), _ptr(slot), _ptr(lens), Lmax, _ptr(q),
                           _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(out), _stream(stream))
     return _check(rc, "kvb_direct", check)
+
+
+def _token_stride(x, what):
+    """Elements from one token's row to the next of a [n_tokens, heads, d] tensor whose tokens are contiguous, 0 for up to one token."""
+    if x is None or x.shape[0] < 2:
+        return 0
+    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or x.stride(0) < x.shape[1] * x.shape[2]:
+        raise ValueError("%s of shape %s and stride %s: [n_tokens, heads, d] with contiguous tokens is wanted" % (what, tuple(x.shape), tuple(x.stride())))
+    return x.stride(0)
+
+
+def seqs(start, n_tokens, n_slots, slot=None, q=None, k=None, v=None):
+    """A kvb_seqs; q, k, v: the tensors whose token strides it takes (None: packed)."""
+    return KvbSeqs(_ptr(start), _ptr(slot), _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v"), n_tokens, n_slots)
+
+
+def _work(nbytes, where):
+    return _check(nbytes, where, True) if nbytes < 0 else nbytes
+
+
+def scan_work(sh, sq):
+    """Bytes of workspace that kvb_scan needs."""
+    return _work(lib().kvb_scan_work(ctypes.byref(sh), ctypes.byref(sq)), "kvb_scan_work")
+
+
+def kvb_scan(sh, sq, q, k, v, g, beta, state0, state1, out, work, stream=None, check=True):
+    rc = lib().kvb_scan(ctypes.byref(sh), ctypes.byref(sq), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state0),
+                        _ptr(state1), _ptr(out), _ptr(work), _stream(stream))
+    return _check(rc, "kvb_scan", check)
 
 
 def bind(fn_name, *args):
