@@ -279,9 +279,9 @@ typedef struct kvb_seqs {
     const int32_t *slot;     /* device [B]: sequence b's states are row slot[b] of the state arrays; a
                                 sequence whose slot is outside 0..n_slots-1 is skipped, no slot may
                                 appear twice.  NULL: row b                                             */
-    int64_t  q_stride;       /* elements from one token's row of q to the next, so that q, k and v may   */
-    int64_t  k_stride;       /* be parts of the rows of one projection: at least the row, in bytes a     */
-    int64_t  v_stride;       /* multiple of 16; 0: packed.  Heads of a token are contiguous              */
+    int64_t  q_stride;       /* elements from one token's row of q to the next, so that q, k and v may */
+    int64_t  k_stride;       /* be parts of the rows of one projection: at least the row, in bytes a   */
+    int64_t  v_stride;       /* multiple of 16, at most 2^26; 0: packed.  Heads of a token are contiguous */
     int32_t  n_tokens;       /* rows of the token arrays                                               */
     int32_t  n_slots;        /* rows of the state arrays                                               */
 } kvb_seqs;

@@ -164,11 +164,11 @@ int check_seqs(const kvb_shape *sh, const kvb_seqs *sq)
         return KVB_EUNSUPPORTED;
     const int64_t size = sh->in_dtype == KVB_F32 ? 4 : 2, width[3] = {(int64_t)sh->Hk * sh->dk, (int64_t)sh->Hk * sh->dk, (int64_t)sh->Hv * sh->dv};
     const int64_t stride[3] = {sq->q_stride, sq->k_stride, sq->v_stride};
-    for (int i = 0; i < 3; ++i)
-        if (stride[i] != 0 && (stride[i] < width[i] || stride[i] > INT64_MAX / 4 / ((int64_t)sq->n_tokens + 1) || stride[i] * size % 16 != 0))
+    for (int i = 0; i < 3; ++i)   // (64 rows of 2^26 bytes in 32 bits)
+        if (width[i] * 4 > 1 << 26 || (stride[i] != 0 && (stride[i] < width[i] || stride[i] > 1 << 26 || stride[i] * size > 1 << 26 || stride[i] * size % 16 != 0)))
             return KVB_EINVAL;
-    // one workgroup for each chunk and qk-head, and up to eight for each sequence and v-head
-    if (scan_chunks(sq->n_tokens, sh->B) > INT32_MAX / sh->Hk || (int64_t)sh->B * sh->Hv > INT32_MAX / 8)
+    // one workgroup for each chunk and v-head, and up to eight for each sequence and v-head
+    if (scan_chunks(sq->n_tokens, sh->B) > INT32_MAX / sh->Hv || (int64_t)sh->B * sh->Hv > INT32_MAX / 8)
         return KVB_EINVAL;
     return KVB_OK;
 }
@@ -217,15 +217,12 @@ int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs, const void *q, const 
     const int64_t qk = (int64_t)shape->Hk * shape->dk, vv = (int64_t)shape->Hv * shape->dv;
     ScanArgs a{q, k, v, g, beta, state0, state1, out, seqs->start, seqs->slot, static_cast<float *>(work),
                seqs->q_stride ? seqs->q_stride : qk, seqs->k_stride ? seqs->k_stride : qk, seqs->v_stride ? seqs->v_stride : vv,
-               shape->B, seqs->n_slots, seqs->n_tokens, shape->Hk, shape->Hv, shape->Hv / shape->Hk, shape->out_dtype == KVB_F32, shape->scale};
+               shape->B, seqs->n_slots, seqs->n_tokens, shape->Hk, shape->Hv, shape->Hv / shape->Hk, shape->scale};
     hipStream_t hs = static_cast<hipStream_t>(stream);
     g_launch_status = hipSuccess;
-    if (shape->in_dtype == KVB_F32)
-        launch_scan_typed<float>(shape->dk, a, hs);
-    else if (shape->in_dtype == KVB_BF16)
-        launch_scan_typed<bf16_t>(shape->dk, a, hs);
-    else
-        launch_scan_typed<f16_t>(shape->dk, a, hs);
+    rc = dispatch_types(shape->in_dtype, shape->out_dtype, [&]<typename TIn, typename TOut>() { launch_scan_typed<TIn, TOut>(shape->dk, a, hs); });
+    if (rc != KVB_OK)
+        return rc;
     return finish_launch();
 }
 

@@ -21,13 +21,15 @@
 
 #include "kvb_device.h"
 
+#include <utility>
+
 namespace kvb_impl {
 
 constexpr int SC = 64;                      // tokens of a chunk
 constexpr int SCAN_TILES = 6;               // 16 x 32 tiles with something in them of a triangular 64 x 64 matrix
 constexpr int SCAN_UNITS = SCAN_TILES * 64; // of 8 floats each: what a lane holds of a tile as the matrix instruction's first operand
 constexpr int SCAN_MAT = SCAN_UNITS * 8;    // floats of a matrix's image
-constexpr int SCAN_GATES = 4 * SC;          // gamma = exp(c), rest = exp(c_last - c), beta, c; behind a chunk's end beta and rest are 0
+constexpr int SCAN_GATES = 4 * SC;          // gamma = exp(c), rest = exp(c_last - c), beta, 0; behind a chunk's end beta and rest are 0
 
 // floats of workspace for each (chunk, v-head)
 constexpr int SCAN_PREP = 2 * SCAN_MAT + SCAN_GATES;
@@ -43,7 +45,6 @@ struct ScanArgs {
     float *prep;           // [chunks][Hv][SCAN_PREP]
     int64_t q_stride, k_stride, v_stride;   // elements from a token's row to the next
     int32_t B, n_slots, n_tokens, Hk, Hv, r;
-    int32_t out_wide;      // fp32 outputs (otherwise the 16-bit input type)
     float scale;
 };
 
@@ -57,7 +58,9 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const int32_t *start, int n_tokens, int b)
 {
-    const int s = min(max(start[b], 0), n_tokens), e = min(max(start[b + 1], s), n_tokens);
+    // (scalars: addresses that are built on them are scalars too)
+    const int first = __builtin_amdgcn_readfirstlane(start[b]), behind = __builtin_amdgcn_readfirstlane(start[b + 1]);
+    const int s = min(max(first, 0), n_tokens), e = min(max(behind, s), n_tokens);
     return Span{s, e - s};
 }
 __device__ __forceinline__ int first_chunk(const Span &s, int b) { return s.first / SC + b; }
@@ -65,7 +68,7 @@ __device__ __forceinline__ int first_chunk(const Span &s, int b) { return s.firs
 // The state row of sequence b, or -1 if there is none.
 __device__ __forceinline__ int state_row(const int32_t *slot, int n_slots, int b)
 {
-    const int s = slot ? slot[b] : b;
+    const int s = __builtin_amdgcn_readfirstlane(slot ? slot[b] : b);
     return s >= 0 && s < n_slots ? s : -1;
 }
 
@@ -90,10 +93,47 @@ __device__ __forceinline__ ChunkAt chunk_at(const int32_t *start, int n_tokens, 
     return ChunkAt{b, s.first + at, min(SC, s.len - at)};
 }
 
+// f(0), .. f(N - 1), each number a compile-time one
+template <int N, typename F>
+__device__ __forceinline__ void static_for(F &&f)
+{
+    [&]<int... I>(std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }(std::make_integer_sequence<int, N>{});
+}
+
+// Sums over the lanes up to one's own, in fp64 (steps of 1, 2, 4 and 8 within rows of 16 lanes, then the rows' last lanes).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double x)
+{
+    const uint2 w = __builtin_bit_cast(uint2, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0u, w.x, CTRL, ROWS, 0xF, false), hi = __builtin_amdgcn_update_dpp(0u, w.y, CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, make_uint2(lo, hi));
+}
+__device__ __forceinline__ double sum_below(double x)
+{
+    x += shifted<0x111, 0xF>(x);
+    x += shifted<0x112, 0xF>(x);
+    x += shifted<0x114, 0xF>(x);
+    x += shifted<0x118, 0xF>(x);
+    x += shifted<0x142, 0xA>(x);
+    x += shifted<0x143, 0xC>(x);
+    return x;
+}
+// The log decays of a chunk's token in units of log 2 (the matrix of decays needs powers of two), cut off where they are zero anyhow
+__device__ __forceinline__ double log2_gate(float g) { return (double)(g < -1e5f ? -1e5f : g) * 1.4426950408889634; }
+__device__ __forceinline__ float decay(double c) { return __builtin_amdgcn_exp2f((float)c); }
+
 // bf16 pieces of an input value, and the most that any fp32 value is cut into
 template <typename T>
 constexpr int PIECES = __is_same(T, bf16_t) ? 1 : __is_same(T, f16_t) ? 2 : 3;
 constexpr int FULL = 3;
+
+// (both at once: the conversion of a pair is one instruction)
+__device__ __forceinline__ uint32_t pair_bf16(float lo, float hi)
+{
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    typedef __bf16 v2b __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2b));
+}
 
 // Eight values in N pieces, to nearest: each piece has 8 bits of what the ones before left.
 template <int N>
@@ -108,7 +148,7 @@ __device__ __forceinline__ void cut8(const float (&x)[8], uint4 (&p)[N])
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            w[j] = pack_pair<bf16_t>(rest[2 * j], rest[2 * j + 1]);
+            w[j] = pair_bf16(rest[2 * j], rest[2 * j + 1]);
             rest[2 * j] -= __uint_as_float(w[j] << 16);
             rest[2 * j + 1] -= __uint_as_float(w[j] & 0xFFFF0000u);
         }
@@ -138,12 +178,30 @@ __device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const uint
             if (i + j < FULL)
                 c = mfma16x32<bf16_t>(a[i], b[j], c);
 }
+// The same for M x N sums, each product of pieces for all of them in turn: a sum is not added to again before the others were.
+template <int M, int N, int NA, int NB>
+__device__ __forceinline__ void mma(f32x4_t (&c)[M][N], const uint4 (&a)[M][NA], const uint4 (&b)[N][NB])
+{
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (i + j < FULL)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        c[m][n] = mfma16x32<bf16_t>(a[m][i], b[n][j], c[m][n]);
+}
 
 // Operand layouts of v_mfma_f32_16x16x32: lane l holds row (first operand) or column (second) l % 16 and of the 32 that are summed
 // over the 8 that belong to l / 16; a sum has column l % 16 in lane l and rows 4 (l / 16) + 0..3 in its four registers.  The order of
-// what is summed over is free as long as both operands share it.  So 32 rows of a sum, two tiles of it, become a second
-// operand without a move between lanes: lane group g then holds rows 4g .. 4g+3 of the first tile and of the second, and the first
-// operand has its columns in that order: 4g .. 4g+3 and 16 + 4g .. 16 + 4g + 3 for group g.  "Paired order" below.
+// what is summed over is free as long as both operands share it, so the registers of two tiles of a sum become a second
+// operand without a move between lanes: lane group g has rows 4g .. 4g+3 of the first tile and of the second.
+//   Tokens: the tiles are tokens 16 rt .., and the images of M and P have their columns in that order (4g .. 4g+3, 16+4g .. 16+4g+3).
+//   Rows of the state: tile 2 ks + h has in its row 4g + r the state's row 32 ks + 8g + 4h + r (state_row_of), so that a
+//   lane group's eight are neighbours and the keys stand in LDS as they come.
+__device__ __forceinline__ int state_row_of(int tile, int g, int r) { return 32 * (tile / 2) + 8 * g + 4 * (tile % 2) + r; }
 __device__ __forceinline__ void pair8(const f32x4_t &a, const f32x4_t &b, float (&x)[8])
 {
 #pragma unroll
@@ -153,36 +211,122 @@ __device__ __forceinline__ void pair8(const f32x4_t &a, const f32x4_t &b, float 
     }
 }
 
-// A chunk's 64 x D keys (or queries) in LDS: piece, 16-token tile, 32-column step, lane, 16 bytes, in paired order.
+// A stretch of memory: loads behind its end give zeros and stores there do nothing, so that a chunk's missing tokens need no
+// test and no branch.  Offsets in bytes, 32 bits, from a scalar address.
+struct Buffer {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ Buffer(const void *p, uint32_t bytes) : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000)) {}
+    __device__ __forceinline__ uint4 load16(uint32_t at) const { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0)); }
+    __device__ __forceinline__ uint2 load8(uint32_t at) const { return __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0)); }
+    __device__ __forceinline__ uint32_t load4(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0); }
+    __device__ __forceinline__ uint16_t load2(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0); }
+    __device__ __forceinline__ void store8(uint32_t at, uint2 x) const
+    {
+        typedef uint32_t v2 __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2, x), r, at, 0, 0);
+    }
+    __device__ __forceinline__ void store4(uint32_t at, uint32_t x) const { __builtin_amdgcn_raw_buffer_store_b32(x, r, at, 0, 0); }
+    __device__ __forceinline__ void store2(uint32_t at, uint16_t x) const { __builtin_amdgcn_raw_buffer_store_b16(x, r, at, 0, 0); }
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw8(const Buffer &b, uint32_t at)
+{
+    if constexpr (sizeof(T) == 4)
+        return Raw8<T>{__builtin_bit_cast(float4, b.load16(at)), __builtin_bit_cast(float4, b.load16(at + 16))};
+    else
+        return Raw8<T>{b.load16(at)};
+}
+// the rows of one head in n tokens (the stride in elements, at most 2^26 bytes: 64 rows in 32 bits)
+template <typename T, int D>
+__device__ __forceinline__ Buffer head_rows(const T *p, int64_t stride, int n)
+{
+    return Buffer(p, (uint32_t)(n - 1) * (uint32_t)(stride * sizeof(T)) + D * (uint32_t)sizeof(T));
+}
+
+// A barrier of the workgroup that orders what it has in LDS and leaves loads and stores of memory in flight.
+__device__ __forceinline__ void lds_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// NC adjacent columns of the wave's 64 rows 16 rt + 4 g + r of a token array (g = lane / 16), untouched bits
+template <typename T, int NC>
+struct Rows64 {
+    using Raw = std::conditional_t<sizeof(T) * NC == 8, uint2, std::conditional_t<sizeof(T) * NC == 4, uint32_t, uint16_t>>;
+    Raw x[4][4];
+    // own: the lane's offset, that of its column in row 4 g
+    __device__ __forceinline__ void load(const Buffer &b, uint32_t own, uint32_t stride_bytes)
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t at = own + (16 * (i / 4) + i % 4) * stride_bytes;
+            if constexpr (sizeof(Raw) == 8)
+                x[i / 4][i % 4] = b.load8(at);
+            else if constexpr (sizeof(Raw) == 4)
+                x[i / 4][i % 4] = b.load4(at);
+            else
+                x[i / 4][i % 4] = b.load2(at);
+        }
+    }
+    __device__ __forceinline__ float value(int rt, int r, int ct) const
+    {
+        if constexpr (NC == 1) {
+            return to_f32(__builtin_bit_cast(T, x[rt][r]));
+        } else if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(ct ? x[rt][r].y : x[rt][r].x);
+        } else {
+            const float2 v = unpack_pair<T>(x[rt][r]);
+            return ct ? v.y : v.x;
+        }
+    }
+};
+// The same rows of a result
+template <typename T, int NC>
+__device__ __forceinline__ void put_rows(const Buffer &b, uint32_t own, uint32_t stride_bytes, float scale, const f32x4_t (&x)[4][NC])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int rt = i / 4, r = i % 4;
+        const uint32_t at = own + (16 * rt + r) * stride_bytes;
+        if constexpr (NC == 1 && sizeof(T) == 4)
+            b.store4(at, __float_as_uint(scale * x[rt][0][r]));
+        else if constexpr (NC == 1)
+            b.store2(at, from_f32<T>(scale * x[rt][0][r]).bits);
+        else if constexpr (sizeof(T) == 4)
+            b.store8(at, make_uint2(__float_as_uint(scale * x[rt][0][r]), __float_as_uint(scale * x[rt][NC - 1][r])));
+        else
+            b.store4(at, pack_pair<T>(scale * x[rt][0][r], scale * x[rt][NC - 1][r]));
+    }
+}
+
+// A chunk's 64 x D keys (or queries) in LDS: piece, 16-token tile, 32-column step, lane, 16 bytes.
 // loaded: by the workgroup's waves in turns of a (tile, step), 16 bytes (of a 16-bit type) a lane.
 template <typename T, int D, int NWV>
 struct TokenTile {
     static constexpr int STEPS = D / 32, N = 4 * STEPS / NWV, NP = PIECES<T>, WORDS = NP * 4 * STEPS * 64;
     static_assert(4 * STEPS % NWV == 0);
     Raw8<T> x[N];
-    __device__ __forceinline__ void load(const T *rows, int64_t stride, int n, int wave, int lane)
+    __device__ __forceinline__ void load(const Buffer &b, uint32_t stride_bytes, int wave, int lane)
     {
+        const uint32_t own = (lane % 16) * stride_bytes + 8 * (lane / 16) * (uint32_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int u = wave + NWV * i, row = min(16 * (u / STEPS) + lane % 16, n - 1);
-            x[i] = load_raw8(rows + row * stride + 32 * (u % STEPS) + 8 * (lane / 16));
+            const int u = wave + NWV * i;
+            x[i] = load_raw8<T>(b, own + 16 * (u / STEPS) * stride_bytes + 32 * (u % STEPS) * (uint32_t)sizeof(T));
         }
     }
     __device__ __forceinline__ void store(uint4 *img, int wave, int lane) const
     {
-        // a lane's eight columns are two runs of four, which belong to neighbouring lane groups
-        const int g = lane / 16, at = (2 * g % 4) * 16 + lane % 16, half = g / 2;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int u = wave + NWV * i;
             uint4 p[NP];
             cut_raw(x[i], p);
 #pragma unroll
-            for (int j = 0; j < NP; ++j) {
-                uint2 *to = reinterpret_cast<uint2 *>(img + (j * 4 * STEPS + u) * 64 + at) + half;
-                to[0] = make_uint2(p[j].x, p[j].y);
-                to[32] = make_uint2(p[j].z, p[j].w);
-            }
+            for (int j = 0; j < NP; ++j)
+                img[(j * 4 * STEPS + u) * 64 + lane] = p[j];
         }
     }
     // rows of tokens as the first operand: tile rt, columns 32 ks ..
@@ -192,8 +336,8 @@ struct TokenTile {
         for (int j = 0; j < NP; ++j)
             a[j] = img[((j * 4 + rt) * STEPS + ks) * 64 + lane];
     }
-    // the transpose: rows are columns 16 mt .. of the tile, summed over tokens 32 s .. in paired order (ds_read_b64_tr_b16: each 16
-    // lanes read four rows of 16 and get a column of four each)
+    // the transpose: rows are the state's rows of tile mt, summed over tokens 32 s .. (ds_read_b64_tr_b16: 16 lanes read four
+    // rows of 16, four columns a lane, and get a column of four each)
     static __device__ __forceinline__ void columns(const uint4 *img, int mt, int s, int lane, uint4 (&a)[NP])
     {
         typedef short v4s __attribute__((ext_vector_type(4)));
@@ -216,20 +360,17 @@ __host__ __device__ constexpr int tile_of(int rt, int s)
 {
     return UPPER ? (rt < 2 ? 2 * rt + s : 2 + rt) : (rt < 2 ? rt : 2 * rt - 2 + s);
 }
-template <bool UPPER>
-__host__ __device__ constexpr bool has_tile(int rt, int s) { return UPPER ? rt < 2 || s == 1 : rt >= 2 || s == 0; }
 
 // N units of 8 floats from a workspace into pieces in LDS, by all NTH threads of the workgroup
 template <int N, int NTH>
 struct MatTile {
     static constexpr int EACH = (N + NTH - 1) / NTH;
     Raw8<float> x[EACH];
-    __device__ __forceinline__ void load(const float *img, int tid)
+    __device__ __forceinline__ void load(const Buffer &b, int tid)   // (of N units)
     {
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (N % NTH == 0 || tid + NTH * i < N)
-                x[i] = load_raw8(img + (tid + NTH * i) * 8);
+            x[i] = load_raw8<float>(b, (tid + NTH * i) * 32);
     }
     __device__ __forceinline__ void store(uint4 *to, int tid) const
     {
@@ -245,13 +386,28 @@ struct MatTile {
                     to[j * N + tid + NTH * i] = p[j];
             }
     }
-    static __device__ __forceinline__ void tile(const uint4 *img, int t, int lane, uint4 (&a)[FULL])
-    {
+};
+// c += (matrix) (b), of which b holds rows 32 s .. of the second operand: img is the image in LDS, its pieces `apart` units from each other
+template <bool UPPER, int S, int NC>
+__device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *img, int apart, int lane, const uint4 (&b)[NC][FULL])
+{
+    constexpr int FROM = !UPPER && S == 1 ? 2 : 0, TO = UPPER && S == 0 ? 2 : 4;
+    uint4 a[TO - FROM][FULL];
+#pragma unroll
+    for (int rt = FROM; rt < TO; ++rt)
 #pragma unroll
         for (int j = 0; j < FULL; ++j)
-            a[j] = img[j * N + t * 64 + lane];
-    }
-};
+            a[rt - FROM][j] = img[j * apart + tile_of<UPPER>(rt, S) * 64 + lane];
+#pragma unroll
+    for (int i = 0; i < FULL; ++i)
+#pragma unroll
+        for (int j = 0; i + j < FULL; ++j)
+#pragma unroll
+            for (int rt = FROM; rt < TO; ++rt)
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+                    c[rt][n] = mfma16x32<bf16_t>(a[rt - FROM][i], b[n][j], c[rt][n]);
+}
 
 // One kernel of a call that makes several; an armed timer spans them from the first one's start to the last one's end.
 template <typename... Params, typename... Args>
@@ -274,7 +430,7 @@ void launch_part(void (*kernel)(Params...), bool first, bool last, int64_t block
 }
 
 // one unit per input type (kvb_scan_*.hip)
-template <typename TIn>
+template <typename TIn, typename TOut>
 void launch_scan_typed(int d, const ScanArgs &a, hipStream_t stream);
 
 }  // namespace kvb_impl

@@ -3,6 +3,6 @@
 
 namespace kvb_impl {
 
-template void launch_scan_typed<float>(int d, const ScanArgs &a, hipStream_t stream);
+template void launch_scan_typed<float, float>(int d, const ScanArgs &a, hipStream_t stream);
 
 }  // namespace kvb_impl
