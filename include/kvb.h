@@ -310,11 +310,50 @@ int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs,
              const void *q, const void *k, const void *v, const float *g, const float *beta,
              const float *state0, float *state1, void *out, void *work, void *stream);
 
+#define KVB_MAX_VOCAB (1 << 24) /* largest V of kvb_accept */
+
+typedef struct kvb_vocab {
+    int32_t B;       /* requests                                              */
+    int32_t T;       /* drafts a request has room for, 1..KVB_MAX_DRAFTS         */
+    int32_t V;       /* tokens of the vocabulary, 1..KVB_MAX_VOCAB               */
+    int32_t dtype;   /* of the probabilities: KVB_F32, KVB_BF16 or KVB_F16       */
+    int64_t stride;  /* elements from one row of probabilities to the next; 0: V */
+} kvb_vocab;
+
+/*
+ * kvb_accept -- which of the drafted tokens the target model accepts, from given random numbers, and the token that
+ * follows them: what comes between kvb_verify (whose outputs lead to the target's probabilities) and the commit.  Together
+ * the accepted drafts and the token are distributed as the target's own samples.
+ *   n_drafts device int32 [B]: drafts that request b has, 0..T (cut off to that); NULL: T each
+ *   parent   device int32 [B, T], as kvb_verify_tree's; NULL: a chain.  An entry outside -1 .. i-1 is taken as -1
+ *   tokens   device int32 [B, T]: the drafted tokens.  One outside 0..V-1 is never accepted
+ *   target   device [B, T+1, V] dtype: row 0 the target's probabilities behind the last committed token, row i + 1 those
+ *            behind draft i
+ *   draft    device [B, T, V] dtype: row i the probabilities that draft i was drawn from (siblings: independently); NULL: drafts
+ *            that were not drawn but chosen (the best tokens of a draft head, say), as if each was certain
+ *   u        device fp32 [B, T], s  device fp32 [B]: random numbers, uniform in [0, 1)
+ *   path     device int32 [B, T]: the accepted drafts, oldest first, then -1: kvb_compact's path
+ *   accepted device int32 [B]: how many: kvb_compact's path_len, kvb_flush's accepted
+ *   token    device int32 [B]: the token that follows the last accepted draft
+ *   work     device, kvb_accept_work(vocab) bytes, 8-byte aligned; what it holds means nothing before and after the call
+ * The walk starts at row 0 with r = the row and Z = 1 and looks at the drafts in order; draft i is tested if its parent is where
+ * the walk stands.  It is accepted if u_i q_i(x_i) Z < r(x_i); then the walk stands at it, r is its row and Z = 1.
+ * Otherwise r becomes max(r - Z q_i, 0) and Z its sum; for chosen drafts r(x_i) becomes 0 and Z loses what it was.  The token is
+ * drawn from r (from the row itself if nothing is left of r, -1 if that has nothing either): weights are r cut off to 0..1
+ * in whole multiples of 2^-48, rounded down, and the token is the first whose running sum exceeds floor(s W), W their sum.
+ * Each operation is one rounding in fp32, sums are exact: the results do not depend on the launch.  A probability that is not a
+ * number counts as 0.
+ */
+int64_t kvb_accept_work(const kvb_vocab *vocab);
+int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *parent, const int32_t *tokens,
+               const void *target, const void *draft, const float *u, const float *s,
+               int32_t *path, int32_t *accepted, int32_t *token, void *work, void *stream);
+
 /*
  * Kernel timer (measurement aid, no part of the method).  A timer owns two HIP events.
  * kvb_timer_arm makes the NEXT kernel that the calling thread launches through this
  * library record its own begin and end timestamps into them; kvb_timer_read waits for that
- * kernel and returns its duration.  Timers are host objects: create / destroy allocate and
+ * kernel and returns its duration (a call of several kernels: from the first one's begin to the last one's end).  Timers are host objects: create / destroy allocate and
  * free them, the only allocation this library ever performs.  Do not arm during stream capture.
  */
 typedef struct kvb_timer kvb_timer;

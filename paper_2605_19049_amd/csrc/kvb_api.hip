@@ -1,6 +1,6 @@
 // Host side of the library: argument checks (all before the first HIP call), the extern "C" entry
 // points of include/kvb.h, the kernel timer.
-#include "kvb_scan_device.h"
+#include "kvb_accept_device.h"
 
 namespace kvb_impl {
 
@@ -191,9 +191,51 @@ int64_t scan_work_bytes(const kvb_shape *sh, const kvb_seqs *sq)
     return 4 * scan_chunks(sq->n_tokens, sh->B) * sh->Hv * SCAN_PREP;
 }
 
+int check_vocab(const kvb_vocab *vo)
+{
+    if (!vo || vo->B < 0 || vo->T < 1 || vo->T > KVB_MAX_DRAFTS || vo->V < 1 || vo->V > KVB_MAX_VOCAB)
+        return KVB_EINVAL;
+    if (vo->stride != 0 && (vo->stride < vo->V || vo->stride > INT32_MAX))
+        return KVB_EINVAL;
+    if (vo->dtype != KVB_F32 && vo->dtype != KVB_BF16 && vo->dtype != KVB_F16)
+        return KVB_EUNSUPPORTED;
+    if (vo->B > (1 << 20))
+        return KVB_EINVAL;
+    return KVB_OK;
+}
+
 }  // namespace
 
 extern "C" {
+
+int64_t kvb_accept_work(const kvb_vocab *vocab)
+{
+    const int rc = check_vocab(vocab);
+    return rc != KVB_OK ? rc : 8 * (int64_t)vocab->B * accept_segments(vocab->B, vocab->V);
+}
+
+int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *parent, const int32_t *tokens, const void *target,
+               const void *draft, const float *u, const float *s, int32_t *path, int32_t *accepted, int32_t *token, void *work, void *stream)
+{
+    DisarmOnExit disarm;
+    const int rc = check_vocab(vocab);
+    if (rc != KVB_OK)
+        return rc;
+    if (vocab->B == 0)
+        return KVB_OK;
+    const size_t size = vocab->dtype == KVB_F32 ? 4 : 2;
+    if (!tokens || !target || !u || !s || !path || !accepted || !token || !work)
+        return KVB_EINVAL;
+    if (!aligned(n_drafts, 4) || !aligned(parent, 4) || !aligned(tokens, 4) || !aligned(target, size) || !aligned(draft, size) ||
+        !aligned(u, 4) || !aligned(s, 4) || !aligned(path, 4) || !aligned(accepted, 4) || !aligned(token, 4) || !aligned(work, 8))
+        return KVB_EINVAL;
+    const int segments = accept_segments(vocab->B, vocab->V);
+    const AcceptArgs a{n_drafts, parent, tokens, target, draft, u, s, path, accepted, token, static_cast<double *>(work),
+                       vocab->stride ? vocab->stride : vocab->V, vocab->B, vocab->T, vocab->V, segments, accept_segment(vocab->V, segments)};
+    g_launch_status = hipSuccess;
+    launch_accept(vocab->dtype, a, static_cast<hipStream_t>(stream));
+    return finish_launch();
+}
 
 int64_t kvb_scan_work(const kvb_shape *shape, const kvb_seqs *seqs)
 {

@@ -20,7 +20,7 @@ STORE_STREAM, STORE_RESIDENT, STORE_FILL_APART = 1, 2, 4
 FILL_APART = 32   # words from one slot's fill to the next with STORE_FILL_APART
 
 EXPORTS = ("kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact", "kvb_direct",
-           "kvb_scan_work", "kvb_scan",
+           "kvb_scan_work", "kvb_scan", "kvb_accept_work", "kvb_accept",
            "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read", "kvb_timer_destroy",
            "kvb_strerror", "kvb_version")
 
@@ -44,6 +44,11 @@ class KvbSeqs(ctypes.Structure):
     _fields_ = [("start", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("n_tokens", ctypes.c_int32),
                 ("n_slots", ctypes.c_int32)]
+
+
+class KvbVocab(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("stride", ctypes.c_int64)]
 
 
 class KvbError(RuntimeError):
@@ -82,7 +87,11 @@ def lib():
         L.kvb_scan_work.argtypes = [sp, qp]
         L.kvb_scan.argtypes = [sp, qp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.kvb_scan_work.restype = ctypes.c_int64
-        for name in ("kvb_scan", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
+        op = ctypes.POINTER(KvbVocab)
+        L.kvb_accept_work.argtypes = [op]
+        L.kvb_accept.argtypes = [op] + [vp] * 12
+        L.kvb_accept_work.restype = ctypes.c_int64
+        for name in ("kvb_scan", "kvb_accept", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
                      "kvb_direct", "kvb_version",
                      "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read"):
             getattr(L, name).restype = ctypes.c_int
@@ -255,6 +264,22 @@ def kvb_scan(sh, sq, q, k, v, g, beta, state0, state1, out, work, stream=None, c
     rc = lib().kvb_scan(ctypes.byref(sh), ctypes.byref(sq), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state0),
                         _ptr(state1), _ptr(out), _ptr(work), _stream(stream))
     return _check(rc, "kvb_scan", check)
+
+
+def vocab(B, T, V, dtype, stride=0):
+    """A kvb_vocab: B requests of up to T drafts over V tokens; stride: elements from row to row of the probabilities (0: V)."""
+    return KvbVocab(B, T, V, dtype, stride)
+
+
+def accept_work(vo):
+    """Bytes of workspace that kvb_accept needs."""
+    return _work(lib().kvb_accept_work(ctypes.byref(vo)), "kvb_accept_work")
+
+
+def kvb_accept(vo, n_drafts, parent, tokens, target, draft, u, s, path, accepted, token, work, stream=None, check=True):
+    rc = lib().kvb_accept(ctypes.byref(vo), _ptr(n_drafts), _ptr(parent), _ptr(tokens), _ptr(target), _ptr(draft), _ptr(u),
+                          _ptr(s), _ptr(path), _ptr(accepted), _ptr(token), _ptr(work), _stream(stream))
+    return _check(rc, "kvb_accept", check)
 
 
 def bind(fn_name, *args):
