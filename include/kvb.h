@@ -310,6 +310,26 @@ int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs,
              const void *q, const void *k, const void *v, const float *g, const float *beta,
              const float *state0, float *state1, void *out, void *work, void *stream);
 
+/*
+ * kvb_scan_backward -- the gradients of kvb_scan, from those of its outputs and last states.  The forward pass leaves
+ * nothing for it: states and triangular systems are worked out once more from the inputs.
+ *   q .. state0  as kvb_scan was given them (n_slots, slots and strides too)
+ *   dout     device [n_tokens, Hv, dv] out_dtype, packed
+ *   dstate1  device [n_slots, Hv, dk, dv] fp32, or NULL: zero
+ *   dq, dk, dv  device, written: in_dtype, strides of q, k and v.  q and k of a qk-head get the sum over its v-heads
+ *   dg, dbeta   device [n_tokens, Hv] fp32, written; dg is the gradient of the log decay
+ *   dstate0  device [n_slots, Hv, dk, dv] fp32, written, or NULL: not wanted.  May be dstate1
+ *   work     device, kvb_scan_backward_work(shape, seqs) bytes, 16-byte aligned: at d = 128 some 230 KB for each 64 tokens
+ *            of a v-head, the two states at each chunk's start above all
+ * Rows of skipped sequences are not written.  The same inputs give the same bits.  16-bit gradients are rounded once from sums to
+ * within 2^-16 of their terms (dq: 2^-24), all else is held to fp32.
+ */
+int64_t kvb_scan_backward_work(const kvb_shape *shape, const kvb_seqs *seqs);
+int kvb_scan_backward(const kvb_shape *shape, const kvb_seqs *seqs,
+                      const void *q, const void *k, const void *v, const float *g, const float *beta, const float *state0,
+                      const void *dout, const float *dstate1, void *dq, void *dk, void *dv,
+                      float *dg, float *dbeta, float *dstate0, void *work, void *stream);
+
 #define KVB_MAX_VOCAB (1 << 24) /* largest V of kvb_accept */
 
 typedef struct kvb_vocab {

@@ -14,7 +14,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["kvb_api.hip", "kvb_step_bf16.hip", "kvb_step_bf16_r16.hip", "kvb_step_f16.hip", "kvb_step_f16_r16.hip",
            "kvb_step_f32.hip", "kvb_verify_bf16.hip", "kvb_verify_f16.hip", "kvb_verify_f32.hip",
-           "kvb_flush.hip", "kvb_direct.hip", "kvb_scan_bf16.hip", "kvb_scan_f16.hip", "kvb_scan_f32.hip", "kvb_accept.hip"]
+           "kvb_flush.hip", "kvb_direct.hip", "kvb_scan_bf16.hip", "kvb_scan_f16.hip", "kvb_scan_f32.hip", "kvb_scan_grad_bf16.hip",
+           "kvb_scan_grad_f16.hip", "kvb_scan_grad_f32.hip", "kvb_accept.hip"]
 LIB = os.path.join(HERE, "libkvb.so")
 
 HIPCC_FLAGS = [

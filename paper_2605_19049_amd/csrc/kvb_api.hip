@@ -186,9 +186,23 @@ int check_seq_pointers(const kvb_shape *sh, const kvb_seqs *sq, const void *q, c
     return KVB_OK;
 }
 
+ScanArgs scan_args(const kvb_shape *sh, const kvb_seqs *sq, const void *q, const void *k, const void *v, const float *g, const float *beta,
+                   const float *state0, float *state1, void *out, float *prep, float *s0, float *z)
+{
+    const int64_t qk = (int64_t)sh->Hk * sh->dk, vv = (int64_t)sh->Hv * sh->dv;
+    return ScanArgs{q, k, v, g, beta, state0, state1, out, sq->start, sq->slot, prep, s0, z, sq->q_stride ? sq->q_stride : qk,
+                    sq->k_stride ? sq->k_stride : qk, sq->v_stride ? sq->v_stride : vv, sh->B, sq->n_slots, sq->n_tokens, sh->Hk, sh->Hv,
+                    sh->Hv / sh->Hk, sh->scale};
+}
+
 int64_t scan_work_bytes(const kvb_shape *sh, const kvb_seqs *sq)
 {
     return 4 * scan_chunks(sq->n_tokens, sh->B) * sh->Hv * SCAN_PREP;
+}
+
+int64_t grad_work_bytes(const kvb_shape *sh, const kvb_seqs *sq)
+{
+    return 4 * scan_chunks(sq->n_tokens, sh->B) * sh->Hv * grad_floats(sh->dk);
 }
 
 int check_vocab(const kvb_vocab *vo)
@@ -256,13 +270,45 @@ int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs, const void *q, const 
         return KVB_EINVAL;
     if (shape->B == 0)
         return KVB_OK;
-    const int64_t qk = (int64_t)shape->Hk * shape->dk, vv = (int64_t)shape->Hv * shape->dv;
-    ScanArgs a{q, k, v, g, beta, state0, state1, out, seqs->start, seqs->slot, static_cast<float *>(work),
-               seqs->q_stride ? seqs->q_stride : qk, seqs->k_stride ? seqs->k_stride : qk, seqs->v_stride ? seqs->v_stride : vv,
-               shape->B, seqs->n_slots, seqs->n_tokens, shape->Hk, shape->Hv, shape->Hv / shape->Hk, shape->scale};
+    const ScanArgs a = scan_args(shape, seqs, q, k, v, g, beta, state0, state1, out, static_cast<float *>(work), nullptr, nullptr);
     hipStream_t hs = static_cast<hipStream_t>(stream);
     g_launch_status = hipSuccess;
     rc = dispatch_types(shape->in_dtype, shape->out_dtype, [&]<typename TIn, typename TOut>() { launch_scan_typed<TIn, TOut>(shape->dk, a, hs); });
+    if (rc != KVB_OK)
+        return rc;
+    return finish_launch();
+}
+
+int64_t kvb_scan_backward_work(const kvb_shape *shape, const kvb_seqs *seqs)
+{
+    const int rc = check_seqs(shape, seqs);
+    return rc != KVB_OK ? rc : grad_work_bytes(shape, seqs);
+}
+
+int kvb_scan_backward(const kvb_shape *shape, const kvb_seqs *seqs, const void *q, const void *k, const void *v, const float *g,
+                      const float *beta, const float *state0, const void *dout, const float *dstate1, void *dq, void *dk, void *dv,
+                      float *dg, float *dbeta, float *dstate0, void *work, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_seqs(shape, seqs);
+    if (rc == KVB_OK)
+        rc = check_seq_pointers(shape, seqs, q, k, v, g, beta, state0, work);
+    if (rc != KVB_OK)
+        return rc;
+    if (!aligned(dout, 16) || !aligned(dstate1, 16) || !aligned(dq, 16) || !aligned(dk, 16) || !aligned(dv, 16) || !aligned(dg, 4) ||
+        !aligned(dbeta, 4) || !aligned(dstate0, 16))
+        return KVB_EINVAL;
+    if (seqs->n_tokens > 0 && (!dout || !dq || !dk || !dv || !dg || !dbeta))
+        return KVB_EINVAL;
+    if (shape->B == 0)
+        return KVB_OK;
+    const int64_t chunks = scan_chunks(seqs->n_tokens, shape->B) * shape->Hv, d = shape->dk;
+    float *prep = static_cast<float *>(work);   // (every part a multiple of 16 bytes)
+    float *s0 = prep + chunks * GRAD_PREP, *ds = s0 + chunks * d * d, *z = ds + chunks * d * d, *dd = z + chunks * SC * d, *part = dd + chunks * SC * d;
+    const GradArgs a{scan_args(shape, seqs, q, k, v, g, beta, state0, nullptr, nullptr, prep, s0, z), dout, dstate1, dq, dk, dv, dg, dbeta, dstate0, ds, dd, part};
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    g_launch_status = hipSuccess;
+    rc = dispatch_types(shape->in_dtype, shape->out_dtype, [&]<typename TIn, typename TOut>() { launch_scan_grad_typed<TIn, TOut>(shape->dk, a, hs); });
     if (rc != KVB_OK)
         return rc;
     return finish_launch();

@@ -29,10 +29,12 @@ constexpr int SC = 64;                      // tokens of a chunk
 constexpr int SCAN_TILES = 6;               // 16 x 32 tiles with something in them of a triangular 64 x 64 matrix
 constexpr int SCAN_UNITS = SCAN_TILES * 64; // of 8 floats each: what a lane holds of a tile as the matrix instruction's first operand
 constexpr int SCAN_MAT = SCAN_UNITS * 8;    // floats of a matrix's image
-constexpr int SCAN_GATES = 4 * SC;          // gamma = exp(c), rest = exp(c_last - c), beta, 0; behind a chunk's end beta and rest are 0
+constexpr int SCAN_GATES = 4 * SC;          // gamma = exp(c), rest = exp(c_last - c), beta, for the gradients q.k; behind a chunk's end
+                                            // beta, rest and q.k are 0
 
-// floats of workspace for each (chunk, v-head)
+// floats of workspace for each (chunk, v-head): M, P and the gates; for the gradients M, M', P' and the gates
 constexpr int SCAN_PREP = 2 * SCAN_MAT + SCAN_GATES;
+constexpr int GRAD_PREP = 3 * SCAN_MAT + SCAN_GATES;
 
 struct ScanArgs {
     const void *q, *k, *v;
@@ -42,7 +44,8 @@ struct ScanArgs {
     void *out;
     const int32_t *start;  // [B + 1]
     const int32_t *slot;   // or nullptr: sequence b's state is row b
-    float *prep;           // [chunks][Hv][SCAN_PREP]
+    float *prep;           // [chunks][Hv][SCAN_PREP or GRAD_PREP]
+    float *s0, *z;         // for the gradients: the state ahead of each chunk [chunks][Hv][d][d], and E - V [chunks][Hv][64][d]
     int64_t q_stride, k_stride, v_stride;   // elements from a token's row to the next
     int32_t B, n_slots, n_tokens, Hk, Hv, r;
     float scale;
@@ -122,6 +125,26 @@ __device__ __forceinline__ double sum_below(double x)
 __device__ __forceinline__ double log2_gate(float g) { return (double)(g < -1e5f ? -1e5f : g) * 1.4426950408889634; }
 __device__ __forceinline__ float decay(double c) { return __builtin_amdgcn_exp2f((float)c); }
 
+// Sums over the 16 lanes of a row, of 16 values at once: lane l % 16 = m gets that of x[m].  A lane keeps half of the values in each
+// step and hands the others to its mirror image in the row, the half row, the pair of its quad.
+template <int CTRL, int N>
+__device__ __forceinline__ void halve(float (&x)[16], bool upper)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float keep = upper ? x[N + i] : x[i], give = upper ? x[i] : x[N + i];
+        x[i] = keep + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(give), CTRL, 0xF, 0xF, false));
+    }
+}
+__device__ __forceinline__ float sum_rows16(float (&x)[16], int m)
+{
+    halve<0x140, 8>(x, m & 8);
+    halve<0x141, 4>(x, m & 4);
+    halve<0x4E, 2>(x, m & 2);
+    halve<0xB1, 1>(x, m & 1);
+    return x[0];
+}
+
 // bf16 pieces of an input value, and the most that any fp32 value is cut into
 template <typename T>
 constexpr int PIECES = __is_same(T, bf16_t) ? 1 : __is_same(T, f16_t) ? 2 : 3;
@@ -179,14 +202,16 @@ __device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const uint
                 c = mfma16x32<bf16_t>(a[i], b[j], c);
 }
 // The same for M x N sums, each product of pieces for all of them in turn: a sum is not added to again before the others were.
-template <int M, int N, int NA, int NB>
+// LIM: the pieces i and j with i + j < LIM; what is left out is below 2^-16 of a term with 2, which is for what nothing but a
+// result of 16 bits depends on.
+template <int LIM = FULL, int M, int N, int NA, int NB>
 __device__ __forceinline__ void mma(f32x4_t (&c)[M][N], const uint4 (&a)[M][NA], const uint4 (&b)[N][NB])
 {
 #pragma unroll
     for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j)
-            if (i + j < FULL)
+            if (i + j < LIM)
 #pragma unroll
                 for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -301,6 +326,24 @@ __device__ __forceinline__ void put_rows(const Buffer &b, uint32_t own, uint32_t
     }
 }
 
+// Four values down a column from each of two blocks; the lane's 8 bytes are the first or second half of the words at p and q
+__device__ __forceinline__ uint4 transposed_pair(const uint4 *p, const uint4 *q, int half)
+{
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s *Lds;
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(reinterpret_cast<const uint2 *>(p) + half));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(reinterpret_cast<const uint2 *>(q) + half));
+    const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+    return make_uint4(l.x, l.y, h.x, h.y);
+}
+// A 64 x 64 matrix's piece in LDS, tile row it, 32-column step s, lane (row m; group g: columns 4g .. and 16+4g .. of the step): its
+// columns 16 jt .. as a second operand, summed over rows 32 s ..
+__device__ __forceinline__ uint4 transposed(const uint4 *img, int jt, int s, int lane)
+{
+    const uint4 *p = img + (4 * s + jt / 2) * 64 + (lane % 4) * 16 + 4 * (lane / 16) + lane % 16 / 4;
+    return transposed_pair(p, p + 128, jt % 2);
+}
+
 // A chunk's 64 x D keys (or queries) in LDS: piece, 16-token tile, 32-column step, lane, 16 bytes.
 // loaded: by the workgroup's waves in turns of a (tile, step), 16 bytes (of a 16-bit type) a lane.
 template <typename T, int D, int NWV>
@@ -340,16 +383,11 @@ struct TokenTile {
     // rows of 16, four columns a lane, and get a column of four each)
     static __device__ __forceinline__ void columns(const uint4 *img, int mt, int s, int lane, uint4 (&a)[NP])
     {
-        typedef short v4s __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) v4s *Lds;
         const int at = (lane % 4) * 16 + 4 * (lane / 16) + lane % 16 / 4;
 #pragma unroll
         for (int j = 0; j < NP; ++j) {
             const uint4 *p = img + ((j * 4 + 2 * s) * STEPS + mt / 2) * 64 + at;
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(reinterpret_cast<const uint2 *>(p) + mt % 2));
-            const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(reinterpret_cast<const uint2 *>(p + STEPS * 64) + mt % 2));
-            const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
-            a[j] = make_uint4(l.x, l.y, h.x, h.y);
+            a[j] = transposed_pair(p, p + STEPS * 64, mt % 2);
         }
     }
 };
@@ -388,8 +426,8 @@ struct MatTile {
     }
 };
 // c += (matrix) (b), of which b holds rows 32 s .. of the second operand: img is the image in LDS, its pieces `apart` units from each other
-template <bool UPPER, int S, int NC>
-__device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *img, int apart, int lane, const uint4 (&b)[NC][FULL])
+template <bool UPPER, int S, int NC, int NB>
+__device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *img, int apart, int lane, const uint4 (&b)[NC][NB])
 {
     constexpr int FROM = !UPPER && S == 1 ? 2 : 0, TO = UPPER && S == 0 ? 2 : 4;
     uint4 a[TO - FROM][FULL];
@@ -401,7 +439,7 @@ __device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *i
 #pragma unroll
     for (int i = 0; i < FULL; ++i)
 #pragma unroll
-        for (int j = 0; i + j < FULL; ++j)
+        for (int j = 0; j < NB && i + j < FULL; ++j)
 #pragma unroll
             for (int rt = FROM; rt < TO; ++rt)
 #pragma unroll
@@ -429,9 +467,26 @@ void launch_part(void (*kernel)(Params...), bool first, bool last, int64_t block
         g_armed = nullptr;
 }
 
-// one unit per input type (kvb_scan_*.hip)
+// What the gradients need beside the forward pass's arguments (whose out and state1 are not used)
+struct GradArgs {
+    ScanArgs f;
+    const void *dout;
+    const float *dstate1;          // or nullptr: zero
+    void *dq, *dk, *dv;            // strides of q, k, v
+    float *dg, *dbeta, *dstate0;   // dstate0 or nullptr: not wanted
+    float *ds;                     // the state's gradient behind each chunk [chunks][Hv][d][d]
+    float *dd;                     // D [chunks][Hv][64][d]
+    float *part;                   // [chunks][Hv][GRAD_PARTS]
+};
+constexpr int GRAD_PARTS = 8 * 2 * SC;   // two sums a token of each of the (at most eight) waves that share a head's columns
+// floats of workspace for each (chunk, v-head)
+__host__ __device__ constexpr int64_t grad_floats(int d) { return GRAD_PREP + 2 * d * d + 2 * SC * d + GRAD_PARTS; }
+
+// one unit per input type (kvb_scan_*.hip, kvb_scan_grad_*.hip)
 template <typename TIn, typename TOut>
 void launch_scan_typed(int d, const ScanArgs &a, hipStream_t stream);
+template <typename TIn, typename TOut>
+void launch_scan_grad_typed(int d, const GradArgs &a, hipStream_t stream);
 
 }  // namespace kvb_impl
 #endif  // KVB_SCAN_DEVICE_H

@@ -1,0 +1,641 @@
+// kvb_scan_backward: the gradients of kvb_scan (images, layouts and precision: kvb_scan_device.h).
+//
+// With dO' = scale dO, the chunk's first state S0, the gradient dS1 of the state behind it, and E, G, M, P of the forward pass:
+//     X   = P' dO' + rest K dS1                      D   = X + M' beta X              dV = beta D
+//     dS0 = exp(c_last) dS1 + Q' (gamma dO') - K' (gamma dV)
+//     dQ  = gamma dO' S0' + W1 K                     W1_ij = exp(c_i - c_j) beta_j dO'_i.E_j   i >= j
+//     dK  = rest beta E dS1' - gamma dV S0' + W1' Q - W2 K - W2' K      W2_ij = exp(c_i - c_j) beta_j dV_i.E_j   i > j
+//     dbeta_i = D_i.E_i
+// (gamma = exp(c), rest = exp(c_last - c).)  A token's log decay scales what was there before it for all tokens from it on:
+//     dg_t = sum_{i >= t} (Q_i.dQ'_i + Z_i.dV_i - beta_i E_i.D'_i) + sum_{i < t} beta_i E_i.(rest K dS1)_i + exp(c_last) <dS1, S0>
+// over the chunk, with Z = E - V, and dQ' and D' without what has no decay in it (W1's diagonal; rest K dS1 and P's diagonal).
+// So every term is as small as its decays are, and nothing large cancels; W1's and P's diagonals are kept apart throughout.
+//   kvb_scan_prep_kernel<GRAD>, kvb_scan_kernel<STATES>   M, M', P' of all chunks; S0 and Z, from chunk to chunk
+//   kvb_scan_reverse_kernel                               dS, D and dV from the last chunk to the first, split like the forward pass
+//   kvb_scan_grad_kernel                                  dQ, dK, dbeta, dg of all chunks side by side; a workgroup has a qk-head and
+//                                                         adds up its v-heads in their order: the same bits every time
+#ifndef KVB_SCAN_GRAD_KERNEL_H
+#define KVB_SCAN_GRAD_KERNEL_H
+
+#include "kvb_scan_kernel.h"
+
+namespace kvb_impl {
+
+template <typename TIn, typename TOut, int D, int NC, int NWV>
+__global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const GradArgs ga)
+{
+    constexpr int NTH = 64 * NWV, KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
+    using Tok = TokenTile<TIn, D, NWV>;
+    using Mat = MatTile<2 * SCAN_UNITS, NTH>;
+    __shared__ uint4 kimg[Tok::WORDS], qimg[Tok::WORDS], mats[FULL * 2 * SCAN_UNITS];
+    __shared__ float4 gate[SCAN_GATES / 4];
+    const ScanArgs &a = ga.f;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
+    const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
+    const int b = unit / a.Hv, hv = unit - b * a.Hv, hk = hv / a.r;
+    const int row = state_row(a.slot, a.n_slots, b);
+    if (row < 0)
+        return;
+    const Span span = span_of(a.start, a.n_tokens, b);
+    const int chunks = (span.len + SC - 1) / SC, col = (part * NWV + wave) * 16 * NC + NC * m;
+    const size_t own = ((size_t)row * a.Hv + hv) * D * D;
+    const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
+
+    f32x4_t S[KT][NC] = {};   // the gradient of the state
+    auto state_at = [&](int t, int r) { return (uint32_t)(state_row_of(t, g, r) * D + col) * 4; };
+    auto store_state = [&](float *p) {
+        const Buffer to(p, 4 * D * D);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (NC == 2)
+                    to.store8(state_at(t, r), make_uint2(__float_as_uint(S[t][0][r]), __float_as_uint(S[t][NC - 1][r])));
+                else
+                    to.store4(state_at(t, r), __float_as_uint(S[t][0][r]));
+            }
+    };
+    if (ga.dstate1) {
+        const Buffer from(ga.dstate1 + own, 4 * D * D);
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if constexpr (NC == 2) {
+                    const uint2 x = from.load8(state_at(t, r));
+                    S[t][0][r] = __uint_as_float(x.x);
+                    S[t][NC - 1][r] = __uint_as_float(x.y);
+                } else {
+                    S[t][0][r] = __uint_as_float(from.load4(state_at(t, r)));
+                }
+            }
+    }
+
+    const TIn *kp = static_cast<const TIn *>(a.k) + span.first * a.k_stride + hk * D;
+    const TIn *qp = static_cast<const TIn *>(a.q) + span.first * a.q_stride + hk * D;
+    const TOut *op = static_cast<const TOut *>(ga.dout) + ((size_t)span.first * a.Hv + hv) * D;
+    const TIn *vp = static_cast<const TIn *>(a.v) + span.first * a.v_stride + hv * D;
+    TIn *dvp = static_cast<TIn *>(ga.dv) + span.first * a.v_stride + hv * D;
+    const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
+    const uint32_t vown = 4 * g * vst + col * sizeof(TIn), oown = 4 * g * ost + col * sizeof(TOut), eown = (4 * g * D + col) * 4;
+
+    Tok knext, qnext;
+    Mat mnext;
+    float gnext[SCAN_GATES / NTH];
+    Rows64<TOut, NC> onext;
+    Rows64<float, NC> znext;
+    Rows64<TIn, NC> vnext;
+    auto request = [&](int c) {
+        const int n = min(SC, span.len - c * SC);
+        knext.load(head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n), kst, wave, lane);
+        qnext.load(head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n), qst, wave, lane);
+        const Buffer image(a.prep + (own_chunk + (size_t)c * a.Hv) * GRAD_PREP + SCAN_MAT, 4 * (GRAD_PREP - SCAN_MAT));
+        mnext.load(image, tid);
+#pragma unroll
+        for (int i = 0; i < SCAN_GATES / NTH; ++i)
+            gnext[i] = __uint_as_float(image.load4(8 * SCAN_MAT + 4 * (tid + NTH * i)));
+        onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), oown, ost);
+        znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), eown, 4 * D);
+        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst);
+    };
+    f32x4_t y[4][NC];   // D of the chunk
+    auto put = [&](int c) {
+        put_rows<float, NC>(head_rows<float, D>(ga.dd + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), eown, 4 * D, 1.0f, y);
+    };
+    if (chunks > 0)
+        request(chunks - 1);
+    for (int c = chunks - 1; c >= 0; --c) {
+        const int n = min(SC, span.len - c * SC);
+        knext.store(kimg, wave, lane);
+        qnext.store(qimg, wave, lane);
+        mnext.store(mats, tid);
+#pragma unroll
+        for (int i = 0; i < SCAN_GATES / NTH; ++i)
+            reinterpret_cast<float *>(gate)[tid + NTH * i] = gnext[i];
+        f32x4_t dO[4][NC], E[4][NC], kd[4][NC], X[4][NC];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    dO[rt][ct][r] = onext.value(rt, r, ct);
+                    E[rt][ct][r] = vnext.value(rt, r, ct) + znext.value(rt, r, ct);
+                    kd[rt][ct][r] = 0.0f;
+                    X[rt][ct][r] = 0.0f;
+                }
+        lds_barrier();
+        store_state(ga.ds + (own_chunk + (size_t)c * a.Hv) * D * D);
+        if (c > 0)
+            request(c - 1);
+        // kd = K dS
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            uint4 s[NC][FULL], f[4][PIECES<TIn>];
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct) {
+                float x[8];
+                pair8(S[2 * ks][ct], S[2 * ks + 1][ct], x);
+                cut8(x, s[ct]);
+            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt)
+                Tok::rows(kimg, rt, ks, lane, f[rt]);
+            mma(kd, f, s);
+        }
+        // X = scale P' dO + rest kd
+        static_for<2>([&](auto step) {
+            constexpr int s = step();
+            uint4 p[NC][PIECES<TOut>];
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct) {
+                float x[8];
+                pair8(dO[2 * s][ct], dO[2 * s + 1][ct], x);
+                cut8(x, p[ct]);
+            }
+            mma_triangle<true, s>(X, mats + SCAN_UNITS, 2 * SCAN_UNITS, lane, p);
+        });
+        // D' = scale P' dO + M' beta X, kd = rest kd, X = scale P' dO + rest kd + scale q.k dO
+        float bt[4][4], own_share[4][4];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+            const float4 re = gate[16 + 4 * rt + g], be = gate[32 + 4 * rt + g], di = gate[48 + 4 * rt + g];
+            const float rs[4] = {re.x, re.y, re.z, re.w}, dg[4] = {di.x, di.y, di.z, di.w}, bs[4] = {be.x, be.y, be.z, be.w};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                bt[rt][r] = bs[r];
+                own_share[rt][r] = a.scale * dg[r];
+#pragma unroll
+                for (int ct = 0; ct < NC; ++ct) {
+                    kd[rt][ct][r] *= rs[r];
+                    y[rt][ct][r] = a.scale * X[rt][ct][r];
+                    X[rt][ct][r] = y[rt][ct][r] + kd[rt][ct][r] + own_share[rt][r] * dO[rt][ct][r];
+                }
+            }
+        }
+        static_for<2>([&](auto step) {
+            constexpr int s = step();
+            uint4 p[NC][FULL];
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct) {
+                float x[8];
+                pair8(X[2 * s][ct], X[2 * s + 1][ct], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    x[j] *= bt[2 * s + j / 4][j % 4];
+                cut8(x, p[ct]);
+            }
+            mma_triangle<true, s>(y, mats, 2 * SCAN_UNITS, lane, p);
+        });
+        // the tokens' sums of E D' and E rest kd over the wave's columns, and D
+        float inner[16], outer[16];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float in = 0.0f, on = 0.0f;
+#pragma unroll
+                for (int ct = 0; ct < NC; ++ct) {
+                    in = fmaf(E[rt][ct][r], y[rt][ct][r], in);
+                    on = fmaf(E[rt][ct][r], kd[rt][ct][r], on);
+                    y[rt][ct][r] += kd[rt][ct][r] + own_share[rt][r] * dO[rt][ct][r];
+                }
+                inner[4 * rt + r] = in;
+                outer[4 * rt + r] = on;
+            }
+        float *sums = ga.part + (own_chunk + (size_t)c * a.Hv) * GRAD_PARTS + (part * NWV + wave) * 2 * SC + 16 * (m / 4) + 4 * g + m % 4;
+        sums[0] = sum_rows16(inner, m);
+        sums[SC] = sum_rows16(outer, m);
+        // dS = exp(c_last) dS + Q' scale gamma dO - K' gamma beta D
+        const float last = reinterpret_cast<const float *>(gate)[SC - 1];
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct)
+                S[t][ct] *= last;
+        f32x4_t dv[4][NC];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            uint4 o[NC][FULL], d[NC][FULL], f[KT][PIECES<TIn>];
+#pragma unroll
+            for (int ct = 0; ct < NC; ++ct) {
+                float x[8], z[8];
+                pair8(dO[2 * s][ct], dO[2 * s + 1][ct], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int rt = 2 * s + j / 4;
+                    const float gm = reinterpret_cast<const float *>(gate)[16 * rt + 4 * g + j % 4];
+                    dv[rt][ct][j % 4] = bt[rt][j % 4] * y[rt][ct][j % 4];
+                    x[j] *= a.scale * gm;
+                    z[j] = -gm * dv[rt][ct][j % 4];
+                }
+                cut8(x, o[ct]);
+                cut8(z, d[ct]);
+            }
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+                Tok::columns(qimg, t, s, lane, f[t]);
+            mma(S, f, o);
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+                Tok::columns(kimg, t, s, lane, f[t]);
+            mma(S, f, d);
+        }
+        put_rows<TIn, NC>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst, 1.0f, dv);
+        put(c);
+        lds_barrier();
+    }
+    if (ga.dstate0)
+        store_state(ga.dstate0 + own);
+}
+
+// dQ, dK, dbeta and dg of one chunk and qk-head.  D / 32 waves; wave w has columns 32 w .. of dQ and dK for all 64 tokens, as their
+// transposes: dQ' = S0 dO' and so on have the state's rows as first operand, which each wave reads from memory once, and
+// the tokens' rows (dO, E, dV) as second, from LDS.  The two 64 x 64 matrices are worked out a tile column a
+// wave, transposed; their sums' registers, two tiles together, are a second operand for W K, and read back transposed one for W' Q.
+// Products that only dK depends on keep 2^-16 of a term for 16-bit dK; dQ is needed to fp32 for dg.
+template <typename TIn, typename TOut, int D, int NC>   // (NC: of kvb_scan_reverse_kernel)
+__global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs ga)
+{
+    constexpr int NWV = D / 32, KS = D / 32, NP = PIECES<TIn>, NO = PIECES<TOut>, LK = sizeof(TIn) == 2 ? 2 : FULL, ITS = 4 / NWV;
+    constexpr int ROWS = 4 * KS * 64;   // 16-byte words of a piece of 64 rows of D
+    constexpr int ONE = (NO + FULL + LK) * ROWS, W = 512, TWO = (FULL + LK) * W + 2 * NP * ROWS;
+    using Tok = TokenTile<TIn, D, NWV>;
+    // (d = 32: the matrices beside the rows, for its one wave has four tile columns to get rid of)
+    constexpr bool APART = D == 32;
+    constexpr int UNROLL = NP == FULL ? 1 : KS;   // (registers)
+    __shared__ uint4 lds[APART ? ONE + TWO : ONE > TWO ? ONE : TWO];
+    __shared__ float sums[3][4][SC], square[4];   // the tokens' dO'.E, Z.dV and Q.dQ', and <dS1, S0>, by waves
+    __shared__ double cs[SC];
+    uint4 *oimg = lds, *eimg = oimg + NO * ROWS, *vimg = eimg + FULL * ROWS;
+    uint4 *w1 = lds + (APART ? ONE : 0), *w2 = w1 + FULL * W, *kimg = w2 + LK * W, *qimg = kimg + NP * ROWS;
+    const ScanArgs &a = ga.f;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
+    const int w = blockIdx.x / a.Hk, hk = blockIdx.x - w * a.Hk;
+    const ChunkAt at = chunk_at(a.start, a.n_tokens, a.B, w);
+    if (at.n == 0 || state_row(a.slot, a.n_slots, at.b) < 0)
+        return;
+    const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
+    const Buffer kb = head_rows<TIn, D>(static_cast<const TIn *>(a.k) + at.first * a.k_stride + hk * D, a.k_stride, at.n);
+    const Buffer qb = head_rows<TIn, D>(static_cast<const TIn *>(a.q) + at.first * a.q_stride + hk * D, a.q_stride, at.n);
+    Tok kt, qt;
+    if constexpr (NP == 1) {   // (several pieces: no registers to hold them in)
+        kt.load(kb, kst, wave, lane);
+        qt.load(qb, qst, wave, lane);
+    }
+    f32x4_t dq[2][4] = {}, dk[2][4] = {};
+    const int mine = 32 * wave + 8 * g;   // the lane's first column: of the rows it stages and of what it stores
+    for (int h = 0; h < a.r; ++h) {
+        const int hv = hk * a.r + h;
+        const size_t unit = (size_t)w * a.Hv + hv;
+        const float *gates = a.prep + unit * GRAD_PREP + 3 * SCAN_MAT;
+        float gamma[4], rest[4], beta[4];   // of token 16 nt + m
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+            gamma[nt] = gates[16 * nt + m];
+            rest[nt] = gates[SC + 16 * nt + m];
+            beta[nt] = gates[2 * SC + 16 * nt + m];
+        }
+        const float last = gates[SC - 1];
+        if (wave == 0) {
+            const float g1 = a.g[(size_t)(at.first + min(lane, at.n - 1)) * a.Hv + hv];
+            cs[lane] = sum_below(lane < at.n ? log2_gate(g1) : 0.0);
+        }
+        {   // the tokens' rows: 16 columns of 32 a lane group, tile by tile
+            const Buffer vb = head_rows<TIn, D>(static_cast<const TIn *>(a.v) + at.first * a.v_stride + hv * D, a.v_stride, at.n);
+            const Buffer ob = head_rows<TOut, D>(static_cast<const TOut *>(ga.dout) + ((size_t)at.first * a.Hv + hv) * D, (int64_t)a.Hv * D, at.n);
+            const Buffer zb(a.z + unit * SC * D, 4 * SC * D), db(ga.dd + unit * SC * D, 4 * SC * D);
+            Raw8<TIn> v[4];
+            Raw8<TOut> o[4];
+            Raw8<float> z[4], d[4];
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
+                const int i = 16 * rt + m;
+                z[rt] = load_raw8<float>(zb, (i * D + mine) * 4);
+                d[rt] = load_raw8<float>(db, (i * D + mine) * 4);
+                v[rt] = load_raw8<TIn>(vb, i * vst + mine * (uint32_t)sizeof(TIn));
+                o[rt] = load_raw8<TOut>(ob, i * ost + mine * (uint32_t)sizeof(TOut));
+            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
+                float ex[8], dx[8], zx[8], ox[8], oe = 0.0f, zd = 0.0f;
+                unpack8(z[rt], zx);
+                unpack8(d[rt], dx);
+                unpack8(v[rt], ex);
+                unpack8(o[rt], ox);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    ex[j] += zx[j];
+                    dx[j] *= beta[rt];
+                    oe = fmaf(ox[j], ex[j], oe);
+                    zd = fmaf(zx[j], dx[j], zd);
+                }
+                uint4 po[NO], pe[FULL], pv[LK];
+                cut_raw(o[rt], po);
+                cut8(ex, pe);
+                cut8(dx, pv);
+                const int to = (rt * KS + wave) * 64 + lane;
+#pragma unroll
+                for (int j = 0; j < NO; ++j)
+                    oimg[j * ROWS + to] = po[j];
+#pragma unroll
+                for (int j = 0; j < FULL; ++j)
+                    eimg[j * ROWS + to] = pe[j];
+#pragma unroll
+                for (int j = 0; j < LK; ++j)
+                    vimg[j * ROWS + to] = pv[j];
+                oe += __shfl_xor(oe, 16);
+                zd += __shfl_xor(zd, 16);
+                oe += __shfl_xor(oe, 32);
+                zd += __shfl_xor(zd, 32);
+                if (g == 0) {
+                    sums[0][wave][16 * rt + m] = a.scale * oe;
+                    sums[1][wave][16 * rt + m] = zd;
+                }
+            }
+        }
+        __syncthreads();
+        // against the states: S0 dO', S0 dV', dS1 E'
+        f32x4_t q0[2][4] = {}, k0[2][4] = {}, k1[2][4] = {};
+        float sq = 0.0f;
+        const Buffer sb(a.s0 + unit * D * D, 4 * D * D), dsb(ga.ds + unit * D * D, 4 * D * D);
+#pragma unroll UNROLL
+        for (int ks = 0; ks < KS; ++ks) {
+            uint4 ps[2][FULL], pd[2][LK];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint32_t from = (state_row_of(2 * wave + t, m / 4, m % 4) * D + 32 * ks + 8 * g) * 4;
+                float x[8], y[8];
+                unpack8(load_raw8<float>(sb, from), x);
+                unpack8(load_raw8<float>(dsb, from), y);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    sq = fmaf(x[j], y[j], sq);
+                cut8(x, ps[t]);
+                cut8(y, pd[t]);
+            }
+            uint4 po[4][NO], pe[4][LK], pv[4][LK];
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt) {
+                const int from = (nt * KS + ks) * 64 + lane;
+#pragma unroll
+                for (int j = 0; j < NO; ++j)
+                    po[nt][j] = oimg[j * ROWS + from];
+#pragma unroll
+                for (int j = 0; j < LK; ++j) {
+                    pe[nt][j] = eimg[j * ROWS + from];
+                    pv[nt][j] = vimg[j * ROWS + from];
+                }
+            }
+            mma(q0, ps, po);
+            mma<LK>(k0, ps, pv);
+            mma<LK>(k1, pd, pe);
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int nt = 0; nt < 4; ++nt) {
+                q0[t][nt] *= a.scale * gamma[nt];
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    dk[t][nt][r] += rest[nt] * beta[nt] * k1[t][nt][r] - gamma[nt] * k0[t][nt][r];
+            }
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2)
+            sq += __shfl_xor(sq, s);
+        if (lane == 0)
+            square[wave] = sq;
+        auto put_matrices = [&](int it, const f32x4_t (&y1)[4], const f32x4_t (&y2)[4]) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int to = ((wave + NWV * it) * 2 + s) * 64 + lane;
+                float x[8];
+                uint4 p1[FULL], p2[LK];
+                pair8(y1[2 * s], y1[2 * s + 1], x);
+                cut8(x, p1);
+                pair8(y2[2 * s], y2[2 * s + 1], x);
+                cut8(x, p2);
+#pragma unroll
+                for (int j = 0; j < FULL; ++j)
+                    w1[j * W + to] = p1[j];
+#pragma unroll
+                for (int j = 0; j < LK; ++j)
+                    w2[j * W + to] = p2[j];
+            }
+        };
+        // W1' (without its diagonal) and -W2', tile columns `wave`, wave + NWV ..: rows j, columns i
+        f32x4_t x1[ITS][4] = {}, x2[ITS][4] = {};
+#pragma unroll (APART ? 1 : ITS)
+        for (int it = 0; it < ITS; ++it) {
+            const int tile = wave + NWV * it;
+#pragma unroll UNROLL
+            for (int ks = 0; ks < KS; ++ks) {
+                const int from = (tile * KS + ks) * 64 + lane;
+                uint4 po[1][NO], pv[1][LK], pe[4][FULL];
+#pragma unroll
+                for (int j = 0; j < NO; ++j)
+                    po[0][j] = oimg[j * ROWS + from];
+#pragma unroll
+                for (int j = 0; j < LK; ++j)
+                    pv[0][j] = vimg[j * ROWS + from];
+#pragma unroll
+                for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+                    for (int j = 0; j < FULL; ++j)
+                        pe[jt][j] = eimg[j * ROWS + (jt * KS + ks) * 64 + lane];
+                f32x4_t c1[4][1], c2[4][1];
+#pragma unroll
+                for (int jt = 0; jt < 4; ++jt) {
+                    c1[jt][0] = x1[it][jt];
+                    c2[jt][0] = x2[it][jt];
+                }
+                mma(c1, pe, po);
+                mma<LK>(c2, pe, pv);
+#pragma unroll
+                for (int jt = 0; jt < 4; ++jt) {
+                    x1[it][jt] = c1[jt][0];
+                    x2[it][jt] = c2[jt][0];
+                }
+            }
+            const int i = 16 * tile + m;
+            const double ci = cs[i];
+#pragma unroll
+            for (int jt = 0; jt < 4; ++jt) {
+                const float4 b4 = *reinterpret_cast<const float4 *>(gates + 2 * SC + 16 * jt + 4 * g);
+                const float bj[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 16 * jt + 4 * g + r;
+                    const float d = decay(ci - cs[j]) * bj[r];
+                    x1[it][jt][r] = i > j ? a.scale * d * x1[it][jt][r] : 0.0f;
+                    x2[it][jt][r] = i > j ? -d * x2[it][jt][r] : 0.0f;
+                }
+            }
+            if constexpr (APART)
+                put_matrices(it, x1[it], x2[it]);
+        }
+        if constexpr (!APART) {
+            __syncthreads();
+#pragma unroll
+            for (int it = 0; it < ITS; ++it)
+                put_matrices(it, x1[it], x2[it]);
+        }
+        if constexpr (NP > 1) {
+            kt.load(kb, kst, wave, lane);
+            qt.load(qb, qst, wave, lane);
+        }
+        kt.store(kimg, wave, lane);
+        qt.store(qimg, wave, lane);
+        __syncthreads();
+        // dQ' += K' W1', dK' -= K' W2' (summed over j); dK' += Q' W1 - K' W2 (summed over i)
+        static_for<2>([&](auto step) {
+            constexpr int s = step(), FROM = 2 * s;   // columns from 32 s on have something in rows 32 s ..
+            uint4 fk[2][NP], fq[2][NP];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                Tok::columns(kimg, 2 * wave + t, s, lane, fk[t]);
+                Tok::columns(qimg, 2 * wave + t, s, lane, fq[t]);
+            }
+            {
+                uint4 b1[4 - FROM][FULL], b2[4 - FROM][LK];
+                f32x4_t cq[2][4 - FROM], ck[2][4 - FROM];
+#pragma unroll
+                for (int it = FROM; it < 4; ++it) {
+                    const int from = (it * 2 + s) * 64 + lane;
+#pragma unroll
+                    for (int j = 0; j < FULL; ++j)
+                        b1[it - FROM][j] = w1[j * W + from];
+#pragma unroll
+                    for (int j = 0; j < LK; ++j)
+                        b2[it - FROM][j] = w2[j * W + from];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        cq[t][it - FROM] = q0[t][it];
+                        ck[t][it - FROM] = dk[t][it];
+                    }
+                }
+                mma(cq, fk, b1);
+                mma<LK>(ck, fk, b2);
+#pragma unroll
+                for (int it = FROM; it < 4; ++it)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        q0[t][it] = cq[t][it - FROM];
+                        dk[t][it] = ck[t][it - FROM];
+                    }
+            }
+            {
+                constexpr int TO = 2 * s + 2;   // rows 32 s .. have something in columns up to 32 s + 31
+                uint4 b1[TO][LK], b2[TO][LK];
+                f32x4_t ck[2][TO];
+#pragma unroll
+                for (int jt = 0; jt < TO; ++jt) {
+#pragma unroll
+                    for (int j = 0; j < LK; ++j) {
+                        b1[jt][j] = transposed(w1 + j * W, jt, s, lane);
+                        b2[jt][j] = transposed(w2 + j * W, jt, s, lane);
+                    }
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        ck[t][jt] = dk[t][jt];
+                }
+                mma<LK>(ck, fq, b1);
+                mma<LK>(ck, fk, b2);
+#pragma unroll
+                for (int jt = 0; jt < TO; ++jt)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        dk[t][jt] = ck[t][jt];
+            }
+        });
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt) {
+            float x[8], y[8], dot = 0.0f, oe = 0.0f;
+            unpack8(load_raw8<TIn>(qb, (16 * nt + m) * qst + mine * (uint32_t)sizeof(TIn)), x);
+            unpack8(load_raw8<TIn>(kb, (16 * nt + m) * kst + mine * (uint32_t)sizeof(TIn)), y);
+#pragma unroll
+            for (int v = 0; v < NWV; ++v)
+                oe += sums[0][v][16 * nt + m];
+            oe *= beta[nt];   // W1's diagonal
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                dot = fmaf(x[j], q0[j / 4][nt][j % 4], dot);
+                dq[j / 4][nt][j % 4] += fmaf(oe, y[j], q0[j / 4][nt][j % 4]);
+                dk[j / 4][nt][j % 4] = fmaf(oe, x[j], dk[j / 4][nt][j % 4]);
+            }
+            dot += __shfl_xor(dot, 16);
+            dot += __shfl_xor(dot, 32);
+            if (g == 0)
+                sums[2][wave][16 * nt + m] = dot;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            float oe = 0.0f, own_terms = 0.0f, total = 0.0f, in = 0.0f, on = 0.0f;
+#pragma unroll
+            for (int v = 0; v < NWV; ++v) {
+                oe += sums[0][v][lane];
+                own_terms += sums[1][v][lane] + sums[2][v][lane];
+                total += square[v];
+            }
+            const float *parts = ga.part + unit * GRAD_PARTS + lane;
+#pragma unroll
+            for (int v = 0; v < D / (16 * NC); ++v) {
+                in += parts[v * 2 * SC];
+                on += parts[v * 2 * SC + SC];
+            }
+            const float b1 = gates[2 * SC + lane];
+            const float from_here = own_terms - b1 * in, before = b1 * on;   // (0 behind the chunk's end)
+            const double upto = sum_below((double)from_here), all = __shfl(upto, 63), ahead = sum_below((double)before) - before;
+            if (lane < at.n) {
+                const size_t to = (size_t)(at.first + lane) * a.Hv + hv;
+                ga.dbeta[to] = in + on + gates[3 * SC + lane] * oe;
+                ga.dg[to] = (float)(all - upto + from_here + ahead + total * last);
+            }
+        }
+        __syncthreads();
+    }
+    auto put = [&](void *to, int64_t stride, const f32x4_t (&x)[2][4]) {
+        TIn *rows = static_cast<TIn *>(to) + at.first * stride + hk * D + mine;
+#pragma unroll
+        for (int nt = 0; nt < 4; ++nt)
+            if (16 * nt + m < at.n) {
+                TIn *p = rows + (16 * nt + m) * stride;
+                if constexpr (sizeof(TIn) == 4) {
+                    *reinterpret_cast<float4 *>(p) = make_float4(x[0][nt][0], x[0][nt][1], x[0][nt][2], x[0][nt][3]);
+                    *reinterpret_cast<float4 *>(p + 4) = make_float4(x[1][nt][0], x[1][nt][1], x[1][nt][2], x[1][nt][3]);
+                } else {
+                    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_pair<TIn>(x[0][nt][0], x[0][nt][1]), pack_pair<TIn>(x[0][nt][2], x[0][nt][3]),
+                                                               pack_pair<TIn>(x[1][nt][0], x[1][nt][1]), pack_pair<TIn>(x[1][nt][2], x[1][nt][3]));
+                }
+            }
+    };
+    put(ga.dq, a.q_stride, dq);
+    put(ga.dk, a.k_stride, dk);
+}
+
+template <typename TIn, typename TOut, int D>
+void launch_scan_grad_sized(const GradArgs &a, hipStream_t stream)
+{
+    constexpr int NWV = D >= 64 ? 4 : 2;
+    const int64_t chunks = scan_chunks(a.f.n_tokens, a.f.B), blocks = (int64_t)a.f.B * a.f.Hv * (D / (16 * NWV));
+    if (a.f.n_tokens > 0) {
+        launch_part(kvb_scan_prep_kernel<TIn, D, true>, true, false, chunks * a.f.Hv, 256, stream, a.f);
+        launch_part(kvb_scan_kernel<TIn, float, D, 1, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
+    }
+    launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, 1, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, blocks, 64 * NWV, stream, a);
+    if (a.f.n_tokens > 0)
+        launch_part(kvb_scan_grad_kernel<TIn, TOut, D, 1>, false, true, chunks * a.f.Hk, 2 * D, stream, a);
+}
+template <typename TIn, typename TOut>
+void launch_scan_grad_typed(int d, const GradArgs &a, hipStream_t stream)
+{
+    if (d == 32)
+        launch_scan_grad_sized<TIn, TOut, 32>(a, stream);
+    else if (d == 64)
+        launch_scan_grad_sized<TIn, TOut, 64>(a, stream);
+    else
+        launch_scan_grad_sized<TIn, TOut, 128>(a, stream);
+}
+
+}  // namespace kvb_impl
+#endif  // KVB_SCAN_GRAD_KERNEL_H

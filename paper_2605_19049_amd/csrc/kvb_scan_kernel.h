@@ -10,11 +10,12 @@ namespace kvb_impl {
 // M = -(1 + G beta)^-1 G by 16 x 16 blocks: the diagonal blocks column by column in registers (each wave one), then wave J the
 // blocks below its own,  M_IJ = -(1 + M_II beta) (G_IJ + sum_K G_IK beta M_KJ),  on the fp32 matrix instruction: the sums'
 // registers are its second operand as they stand, if row 4 g + r is taken for what lane group g sums in its r-th step.
+// GRAD: M, M' and P' without its diagonal, which goes to the gates, instead of M and P.
 // c is summed in fp64, so that differences of it are good to fp32 whatever its size; a decay below exp(-1e5) counts as that (zero).
-template <typename TIn, int D>
+template <typename TIn, int D, bool GRAD>
 __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 {
-    constexpr int LD = SC + 4;
+    constexpr int LD = SC + 4, MATS = GRAD ? 3 : 2, PREP = MATS * SCAN_MAT + SCAN_GATES;
     __shared__ float gs[SC * LD], ps[SC * LD], td[4 * 16 * 20], beta[SC];
     __shared__ double cs[SC];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
@@ -46,16 +47,17 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
             mma(qk[nt], qa, b);
         }
     }
-    float *prep = a.prep + ((size_t)w * a.Hv + hv) * SCAN_PREP;
+    float *prep = a.prep + ((size_t)w * a.Hv + hv) * PREP;
     const double c = sum_below(lane < at.n ? log2_gate(g1) : 0.0);
     if (wave == 0) {
         const double last = __shfl(c, 63);
-        float *gates = prep + 2 * SCAN_MAT;
+        float *gates = prep + MATS * SCAN_MAT;
         const float bt = lane < at.n ? b1 : 0.0f;
         gates[lane] = decay(c);
         gates[SC + lane] = lane < at.n ? decay(last - c) : 0.0f;
         gates[2 * SC + lane] = bt;
-        gates[3 * SC + lane] = 0.0f;
+        if (!GRAD)
+            gates[3 * SC + lane] = 0.0f;
         cs[lane] = c;
         beta[lane] = bt;
     }
@@ -72,7 +74,9 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
                 const int i = 16 * wave + 4 * g + r;
                 const float d = decay(cs[i] - cj);
                 gr[r] = i > j ? d * kk[nt][r] : 0.0f;
-                pr[r] = i >= j ? d * qk[nt][r] : 0.0f;
+                pr[r] = (GRAD ? i > j : i >= j) ? d * qk[nt][r] : 0.0f;
+                if (GRAD && i == j)
+                    prep[MATS * SCAN_MAT + 3 * SC + i] = qk[nt][r];
             }
             if (nt == wave)
                 *reinterpret_cast<float4 *>(gt + m * 20 + 4 * g) = make_float4(gr[0], gr[1], gr[2], gr[3]);
@@ -153,14 +157,22 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
         for (int r = 0; r < 4; ++r)
             gs[(16 * I + 4 * g + r) * LD + 16 * wave + m] = mm[I][r];
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        const int u = tid + 256 * i, of = u >= SCAN_UNITS, t = (of ? u - SCAN_UNITS : u) / 64;
-        const int rt = t < 2 ? t : 1 + t / 2, s = t < 2 ? 0 : t % 2;
-        const float *from = (of ? ps : gs) + (16 * rt + m) * LD + 32 * s + 4 * g;
+    for (int u = tid; u < MATS * SCAN_UNITS; u += 256) {
+        const int of = u / SCAN_UNITS, t = (u - of * SCAN_UNITS) / 64;
+        const float *from = (of == MATS - 1 ? ps : gs);
         float4 *to = reinterpret_cast<float4 *>(prep + u * 8);
-        to[0] = *reinterpret_cast<const float4 *>(from);
-        to[1] = *reinterpret_cast<const float4 *>(from + 16);
+        if (GRAD && of > 0) {   // the transpose: tile t is tile_of<true>(rt, s)
+            const int rt = t < 4 ? t / 2 : t - 2, s = t < 4 ? t % 2 : 1;
+            from += (32 * s + 4 * g) * LD + 16 * rt + m;
+            to[0] = make_float4(from[0], from[LD], from[2 * LD], from[3 * LD]);
+            from += 16 * LD;
+            to[1] = make_float4(from[0], from[LD], from[2 * LD], from[3 * LD]);
+        } else {                // tile_of<false>(rt, s)
+            const int rt = t < 2 ? t : 1 + t / 2, s = t < 2 ? 0 : t % 2;
+            from += (16 * rt + m) * LD + 32 * s + 4 * g;
+            to[0] = *reinterpret_cast<const float4 *>(from);
+            to[1] = *reinterpret_cast<const float4 *>(from + 16);
+        }
     }
 }
 
@@ -168,13 +180,16 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 // A wave keeps its columns of the state in its sums' registers for the whole sequence; the chunk's
 // K S and Q S, E and the state's update follow from each other within the wave (paired order).  Lane l % 16 = n has the columns
 // NC n .. NC n + NC - 1 of the wave's.  What the next chunk needs from memory is requested a chunk ahead.
-template <typename TIn, typename TOut, int D, int NC, int NWV>
+// STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
+// than the decays, which a difference of E and V would lose).
+template <typename TIn, typename TOut, int D, int NC, int NWV, bool STATES>
 __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
 {
     constexpr int NTH = 64 * NWV, KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
     using Tok = TokenTile<TIn, D, NWV>;
-    using Mat = MatTile<2 * SCAN_UNITS, NTH>;
-    __shared__ uint4 kimg[Tok::WORDS], qimg[Tok::WORDS], mats[FULL * 2 * SCAN_UNITS];
+    constexpr int MATS = STATES ? 1 : 2, GATES_AT = (STATES ? 3 : 2) * SCAN_MAT, PREP = GATES_AT + SCAN_GATES;
+    using Mat = MatTile<MATS * SCAN_UNITS, NTH>;
+    __shared__ uint4 kimg[Tok::WORDS], qimg[STATES ? 1 : Tok::WORDS], mats[FULL * MATS * SCAN_UNITS];
     __shared__ float4 gate[SCAN_GATES / 4];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
@@ -206,8 +221,8 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
     const TIn *kp = static_cast<const TIn *>(a.k) + span.first * a.k_stride + hk * D;
     const TIn *qp = static_cast<const TIn *>(a.q) + span.first * a.q_stride + hk * D;
     const TIn *vp = static_cast<const TIn *>(a.v) + span.first * a.v_stride + hv * D;
-    const float *prep = a.prep + ((size_t)first_chunk(span, b) * a.Hv + hv) * SCAN_PREP;
-    const size_t prep_step = (size_t)a.Hv * SCAN_PREP;
+    const float *prep = a.prep + ((size_t)first_chunk(span, b) * a.Hv + hv) * PREP;
+    const size_t prep_step = (size_t)a.Hv * PREP;
     const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
     const uint32_t vown = 4 * g * vst + col * sizeof(TIn), oown = 4 * g * ost + col * sizeof(TOut);
 
@@ -218,16 +233,22 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
     auto request = [&](int c) {
         const int n = min(SC, span.len - c * SC);
         knext.load(head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n), kst, wave, lane);
-        qnext.load(head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n), qst, wave, lane);
-        const Buffer image(prep + c * prep_step, 4 * SCAN_PREP);
+        if constexpr (!STATES)
+            qnext.load(head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n), qst, wave, lane);
+        const Buffer image(prep + c * prep_step, 4 * PREP);
         mnext.load(image, tid);
 #pragma unroll
         for (int i = 0; i < SCAN_GATES / NTH; ++i)
-            gnext[i] = __uint_as_float(image.load4(8 * SCAN_MAT + 4 * (tid + NTH * i)));
+            gnext[i] = __uint_as_float(image.load4(4 * GATES_AT + 4 * (tid + NTH * i)));
         vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst);
     };
     f32x4_t O[4][NC];
-    auto put = [&](int c) {
+    const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
+    auto put = [&](int c) {   // (STATES: O holds Z)
+        if constexpr (STATES) {
+            put_rows<float, NC>(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), (4 * g * D + col) * 4, 4 * D, 1.0f, O);
+            return;
+        }
         TOut *p = static_cast<TOut *>(a.out) + ((size_t)(span.first + c * SC) * a.Hv + hv) * D;
         put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, min(SC, span.len - c * SC)), oown, ost, a.scale, O);
     };
@@ -235,7 +256,8 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
         request(0);
     for (int c = 0; c < chunks; ++c) {
         knext.store(kimg, wave, lane);
-        qnext.store(qimg, wave, lane);
+        if constexpr (!STATES)
+            qnext.store(qimg, wave, lane);
         mnext.store(mats, tid);
 #pragma unroll
         for (int i = 0; i < SCAN_GATES / NTH; ++i)
@@ -261,6 +283,19 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
 #pragma unroll
             for (int ct = 0; ct < NC; ++ct)
                 O[rt][ct] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (STATES) {
+            const Buffer to(a.s0 + (own_chunk + (size_t)c * a.Hv) * D * D, 4 * D * D);
+#pragma unroll
+            for (int t = 0; t < KT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t at = (state_row_of(t, g, r) * D + col) * 4;
+                    if constexpr (NC == 2)
+                        to.store8(at, make_uint2(__float_as_uint(S[t][0][r]), __float_as_uint(S[t][NC - 1][r])));
+                    else
+                        to.store4(at, __float_as_uint(S[t][0][r]));
+                }
+        }
         // y = K S, O = Q S
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -275,10 +310,12 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
                 Tok::rows(kimg, rt, ks, lane, fk[rt]);
-                Tok::rows(qimg, rt, ks, lane, fq[rt]);
+                if constexpr (!STATES)
+                    Tok::rows(qimg, rt, ks, lane, fq[rt]);
             }
             mma(y, fk, s);
-            mma(O, fq, s);
+            if constexpr (!STATES)
+                mma(O, fq, s);
         }
         // Y = V - gamma y, y = beta Y, E = Y + M y
 #pragma unroll
@@ -289,9 +326,14 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
             for (int ct = 0; ct < NC; ++ct)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    E[rt][ct][r] = fmaf(-gm[r], y[rt][ct][r], E[rt][ct][r]);
-                    O[rt][ct][r] *= gm[r];
-                    y[rt][ct][r] = bt[r] * E[rt][ct][r];
+                    if constexpr (STATES) {
+                        O[rt][ct][r] = -gm[r] * y[rt][ct][r];
+                        y[rt][ct][r] = bt[r] * (E[rt][ct][r] + O[rt][ct][r]);
+                    } else {
+                        E[rt][ct][r] = fmaf(-gm[r], y[rt][ct][r], E[rt][ct][r]);
+                        O[rt][ct][r] *= gm[r];
+                        y[rt][ct][r] = bt[r] * E[rt][ct][r];
+                    }
                 }
         }
         static_for<2>([&](auto step) {
@@ -303,8 +345,15 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
                 pair8(y[2 * s][ct], y[2 * s + 1][ct], x);
                 cut8(x, p[ct]);
             }
-            mma_triangle<false, s>(E, mats, 2 * SCAN_UNITS, lane, p);
+            mma_triangle<false, s>(STATES ? O : E, mats, MATS * SCAN_UNITS, lane, p);
         });
+        if constexpr (STATES) {
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+                for (int ct = 0; ct < NC; ++ct)
+                    E[rt][ct] += O[rt][ct];
+        }
         // O += P beta E, S = exp(c_last) S + K' rest beta E
         const float last = reinterpret_cast<const float *>(gate)[SC - 1];
 #pragma unroll
@@ -327,7 +376,8 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
                     x[4 * h + 2] *= be.z;
                     x[4 * h + 3] *= be.w;
                 }
-                cut8(x, p[ct]);
+                if constexpr (!STATES)
+                    cut8(x, p[ct]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const float4 re = gate[16 + 8 * s + 4 * h + g];
@@ -343,7 +393,8 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
             for (int t = 0; t < KT; ++t)
                 Tok::columns(kimg, t, s, lane, f[t]);
             mma(S, f, e);
-            mma_triangle<false, s>(O, mats + SCAN_UNITS, 2 * SCAN_UNITS, lane, p);
+            if constexpr (!STATES)
+                mma_triangle<false, s>(O, mats + SCAN_UNITS, MATS * SCAN_UNITS, lane, p);
         });
         lds_barrier();
     }
@@ -367,8 +418,8 @@ void launch_scan_sized(const ScanArgs &a, hipStream_t stream)
 {
     constexpr int NWV = D >= 64 ? 4 : 2;
     if (a.n_tokens > 0)
-        launch_part(kvb_scan_prep_kernel<TIn, D>, true, false, scan_chunks(a.n_tokens, a.B) * a.Hv, 256, stream, a);
-    launch_part(kvb_scan_kernel<TIn, TOut, D, 1, NWV>, a.n_tokens == 0, true, (int64_t)a.B * a.Hv * (D / (16 * NWV)), 64 * NWV, stream, a);
+        launch_part(kvb_scan_prep_kernel<TIn, D, false>, true, false, scan_chunks(a.n_tokens, a.B) * a.Hv, 256, stream, a);
+    launch_part(kvb_scan_kernel<TIn, TOut, D, 1, NWV, false>, a.n_tokens == 0, true, (int64_t)a.B * a.Hv * (D / (16 * NWV)), 64 * NWV, stream, a);
 }
 template <typename TIn, typename TOut>
 void launch_scan_typed(int d, const ScanArgs &a, hipStream_t stream)

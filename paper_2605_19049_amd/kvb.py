@@ -20,7 +20,7 @@ STORE_STREAM, STORE_RESIDENT, STORE_FILL_APART = 1, 2, 4
 FILL_APART = 32   # words from one slot's fill to the next with STORE_FILL_APART
 
 EXPORTS = ("kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact", "kvb_direct",
-           "kvb_scan_work", "kvb_scan", "kvb_accept_work", "kvb_accept",
+           "kvb_scan_work", "kvb_scan", "kvb_scan_backward_work", "kvb_scan_backward", "kvb_accept_work", "kvb_accept",
            "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read", "kvb_timer_destroy",
            "kvb_strerror", "kvb_version")
 
@@ -87,11 +87,14 @@ def lib():
         L.kvb_scan_work.argtypes = [sp, qp]
         L.kvb_scan.argtypes = [sp, qp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.kvb_scan_work.restype = ctypes.c_int64
+        L.kvb_scan_backward_work.argtypes = [sp, qp]
+        L.kvb_scan_backward.argtypes = [sp, qp] + [vp] * 16
+        L.kvb_scan_backward_work.restype = ctypes.c_int64
         op = ctypes.POINTER(KvbVocab)
         L.kvb_accept_work.argtypes = [op]
         L.kvb_accept.argtypes = [op] + [vp] * 12
         L.kvb_accept_work.restype = ctypes.c_int64
-        for name in ("kvb_scan", "kvb_accept", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
+        for name in ("kvb_scan", "kvb_scan_backward", "kvb_accept", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
                      "kvb_direct", "kvb_version",
                      "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read"):
             getattr(L, name).restype = ctypes.c_int
@@ -264,6 +267,18 @@ def kvb_scan(sh, sq, q, k, v, g, beta, state0, state1, out, work, stream=None, c
     rc = lib().kvb_scan(ctypes.byref(sh), ctypes.byref(sq), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state0),
                         _ptr(state1), _ptr(out), _ptr(work), _stream(stream))
     return _check(rc, "kvb_scan", check)
+
+
+def scan_backward_work(sh, sq):
+    """Bytes of workspace that kvb_scan_backward needs."""
+    return _work(lib().kvb_scan_backward_work(ctypes.byref(sh), ctypes.byref(sq)), "kvb_scan_backward_work")
+
+
+def kvb_scan_backward(sh, sq, q, k, v, g, beta, state0, dout, dstate1, dq, dk, dv, dg, dbeta, dstate0, work, stream=None, check=True):
+    """dq, dk, dv lie as q, k, v do (the strides in sq)."""
+    rc = lib().kvb_scan_backward(ctypes.byref(sh), ctypes.byref(sq), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state0), _ptr(dout),
+                                 _ptr(dstate1), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg), _ptr(dbeta), _ptr(dstate0), _ptr(work), _stream(stream))
+    return _check(rc, "kvb_scan_backward", check)
 
 
 def vocab(B, T, V, dtype, stride=0):

@@ -76,3 +76,22 @@ def test_strides_of_tensors():
     for bad in (q.transpose(0, 1).contiguous().transpose(0, 1), q[:, :, ::2], torch.zeros(1, 2, 64).expand(10, 2, 64)):
         with pytest.raises(ValueError):
             kvb.seqs(A, 10, 1, q=bad)
+
+
+def _backward(sh, sq, **kw):
+    d = dict(q=A, k=A, v=A, g=A, beta=A, state0=A, dout=A, dstate1=A, dq=A, dk=A, dv=A, dg=A, dbeta=A, dstate0=A, work=A)
+    d.update(kw)
+    return kvb.kvb_scan_backward(sh, sq, *d.values(), stream=0, check=False)
+
+
+@pytest.mark.parametrize("bad", [dict(q=A + 8), dict(dout=None), dict(dout=A + 8), dict(dq=None), dict(dk=A + 2), dict(dv=None), dict(dg=None), dict(dbeta=A + 2),
+                                 dict(dstate1=A + 8), dict(dstate0=A + 4), dict(work=None), dict(beta=None)])
+def test_bad_pointers_of_the_backward_pass(bad):
+    assert _backward(kvb.shape(**GOOD), _seqs(), **bad) == kvb.EINVAL
+
+
+def test_backward_pass_refuses_what_the_forward_pass_does():
+    assert _backward(kvb.shape(**{**GOOD, "dk": 96, "dv": 96}), _seqs()) == kvb.EUNSUPPORTED
+    assert _backward(kvb.shape(**GOOD), _seqs(q_stride=255)) == kvb.EINVAL
+    assert _backward(kvb.shape(**{**GOOD, "B": 0}), _seqs()) == kvb.OK
+    assert kvb.scan_backward_work(kvb.shape(**GOOD), _seqs()) > kvb.scan_work(kvb.shape(**GOOD), _seqs())
