@@ -17,20 +17,21 @@ namespace kvb_impl {
 
 namespace {
 
-// Where the walk ended, as scalars: drafts accepted on the way and drafts rejected at the end (bit i: draft i), both in the order
-// of the drafts; mass (in LDS): the sum of what was left before each of those was.
-struct Walk {
-    int place;
-    uint32_t accepted, rejected;
-};
+using Walk = AcceptWalk;
 template <typename T>
 struct Probs {
     const T *p;              // the place's row of the target
     const T *q;              // the request's draft rows, or nullptr
     const int32_t *tokens;   // the request's
-    const float *mass;
+    const float *mass;       // the sum of what was left before each draft that was rejected there (in LDS)
     int64_t stride;
 };
+template <typename T>
+__device__ __forceinline__ Probs<T> probs_of(const AcceptArgs &a, int b, int place, const float *mass)
+{
+    return Probs<T>{static_cast<const T *>(a.target) + ((int64_t)b * (a.T + 1) + place + 1) * a.stride,
+                    a.draft ? static_cast<const T *>(a.draft) + (int64_t)b * a.T * a.stride : nullptr, a.tokens + (int64_t)b * a.T, mass, a.stride};
+}
 
 // what is left of r when as much as `taken` is not there
 __device__ __forceinline__ float less(float r, float taken)
@@ -139,19 +140,19 @@ __device__ double sum_row(const Probs<T> &rows, const Walk &w, int lo, int hi, d
     return total;
 }
 
-// The first token of lo .. hi-1 whose running sum exceeds aim (which is below the range's sum): a run of neighbours a
-// thread.  The thread that has it writes it.
+// The first token of lo .. hi-1 whose running sum exceeds aim (which is below the range's sum), hi - lo some hundreds: a few neighbours
+// a thread.  The thread that has it writes it.
 template <bool TREE, int WAVES, typename T>
 __device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, double *part, int32_t *to)
 {
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, each = (hi - lo + 64 * WAVES - 1) / (64 * WAVES);
     const int from = min(hi, lo + (int)threadIdx.x * each), end = min(hi, from + each);
-    double own = 0.0;
     auto at = [&](int j) {
         float r[1];
         left_at<TREE>(rows, w, j, r);
         return weight(r[0]);
     };
+    double own = 0.0;
     for (int j = from; j < end; ++j)
         own += at(j);
     double upto = own;
@@ -176,6 +177,23 @@ __device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, dou
             }
         }
 }
+// The same for a range of any length whose waves' sums are in `part`: on to the wave's range that has it, until that is short.
+template <bool TREE, int WAVES, typename T>
+__device__ void find_long(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, double *part, int32_t *to)
+{
+    for (;;) {
+        int v = 0;
+        for (; v + 1 < WAVES && part[v] <= aim; ++v)
+            aim -= part[v];
+        const int from = bound_of(lo, hi, v, WAVES), end = bound_of(lo, hi, v + 1, WAVES);
+        lo = from;
+        hi = end;
+        if (hi - lo <= 128 * WAVES)
+            break;
+        sum_row<TREE, WAVES>(rows, w, lo, hi, part);
+    }
+    find_in<TREE, WAVES>(rows, w, lo, hi, aim, part, to);
+}
 
 // floor(s total), below total
 __device__ __forceinline__ double aim_of(float s, double total)
@@ -197,10 +215,7 @@ __device__ Walk walk(const AcceptArgs &a, int b, Probs<T> &rows, float *mass_at,
 {
     const int lane = threadIdx.x % 64, i0 = min(lane % 8, a.T - 1), m0 = min(lane / 8, a.T - 1);
     const T *target = static_cast<const T *>(a.target) + (int64_t)b * (a.T + 1) * a.stride;
-    rows.q = a.draft ? static_cast<const T *>(a.draft) + (int64_t)b * a.T * a.stride : nullptr;
-    rows.tokens = a.tokens + (int64_t)b * a.T;
-    rows.stride = a.stride;
-    rows.mass = mass_at;
+    rows = probs_of<T>(a, b, -1, mass_at);
     const int n = __builtin_amdgcn_readfirstlane(a.n_drafts ? min(max(a.n_drafts[b], 0), a.T) : a.T);
     const int x = rows.tokens[i0], up = TREE && a.parent ? a.parent[(int64_t)b * a.T + i0] : i0 - 1;
     const float u = a.u[(int64_t)b * a.T + i0];
@@ -287,11 +302,7 @@ __device__ void find_row(const AcceptArgs &a, int b, const Probs<T> &rows, Walk 
             a.token[b] = -1;
         return;
     }
-    double aim = aim_of(a.s[b], total);
-    int v = 0;
-    for (; v + 1 < WAVES && part[v] <= aim; ++v)
-        aim -= part[v];
-    find_in<TREE, WAVES>(rows, w, bound_of(0, a.V, v, WAVES), bound_of(0, a.V, v + 1, WAVES), aim, part, a.token + b);
+    find_long<TREE, WAVES>(rows, w, 0, a.V, aim_of(a.s[b], total), part, a.token + b);
 }
 
 }  // namespace
@@ -319,8 +330,13 @@ __global__ __launch_bounds__(256) void kvb_accept_sum_kernel(const AcceptArgs a)
     Probs<T> rows;
     const Walk w = walk<TREE, false, 4>(a, b, rows, nullptr, part);
     const double sum = sum_row<TREE, 4>(rows, w, min(a.V, s * a.segment), min(a.V, (s + 1) * a.segment), part);
-    if (threadIdx.x == 0)
+    if (threadIdx.x == 0) {
         a.sums[(int64_t)b * a.segments + s] = sum;
+        if (s == 0)
+            a.walks[b] = w;
+    }
+    if (s == 0)
+        write_walk(a, b, w);
 }
 
 // The token from the segments' sums
@@ -329,9 +345,8 @@ __global__ __launch_bounds__(1024) void kvb_accept_find_kernel(const AcceptArgs 
 {
     __shared__ double part[16];
     const int b = blockIdx.x;
-    Probs<T> rows;
-    Walk w = walk<TREE, false, 16>(a, b, rows, nullptr, part);
-    write_walk(a, b, w);
+    Walk w = a.walks[b];
+    Probs<T> rows = probs_of<T>(a, b, w.place, nullptr);
     const double *sums = a.sums + (int64_t)b * a.segments;
     double total = 0.0;
     for (int s = 0; s < a.segments; ++s)
@@ -344,7 +359,9 @@ __global__ __launch_bounds__(1024) void kvb_accept_find_kernel(const AcceptArgs 
     int s = 0;
     for (; s + 1 < a.segments && sums[s] <= aim; ++s)
         aim -= sums[s];
-    find_in<TREE, 16>(rows, w, min(a.V, s * a.segment), min(a.V, (s + 1) * a.segment), aim, part, a.token + b);
+    const int lo = min(a.V, s * a.segment), hi = min(a.V, (s + 1) * a.segment);
+    sum_row<TREE, 16>(rows, w, lo, hi, part);
+    find_long<TREE, 16>(rows, w, lo, hi, aim, part, a.token + b);
 }
 
 namespace {

@@ -6,6 +6,13 @@
 
 namespace kvb_impl {
 
+// Where the walk ended, as scalars: drafts accepted on the way and drafts rejected at the end (bit i: draft i), both in the order
+// of the drafts.
+struct AcceptWalk {
+    int place;
+    uint32_t accepted, rejected;
+};
+
 struct AcceptArgs {
     const int32_t *n_drafts;   // [B] or nullptr: T
     const int32_t *parent;     // [B][T] or nullptr: a chain
@@ -15,6 +22,7 @@ struct AcceptArgs {
     const float *u, *s;        // [B][T], [B]
     int32_t *path, *accepted, *token;
     double *sums;              // [B][segments]
+    AcceptWalk *walks;         // [B]
     int64_t stride;
     int32_t B, T, V, segments, segment;
 };

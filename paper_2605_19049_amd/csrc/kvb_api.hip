@@ -225,7 +225,10 @@ extern "C" {
 int64_t kvb_accept_work(const kvb_vocab *vocab)
 {
     const int rc = check_vocab(vocab);
-    return rc != KVB_OK ? rc : 8 * (int64_t)vocab->B * accept_segments(vocab->B, vocab->V);
+    if (rc != KVB_OK)
+        return rc;
+    const int segments = accept_segments(vocab->B, vocab->V);
+    return (int64_t)vocab->B * (8 * segments + (segments > 1 ? 16 : 0));
 }
 
 int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *parent, const int32_t *tokens, const void *target,
@@ -244,7 +247,7 @@ int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *p
         !aligned(u, 4) || !aligned(s, 4) || !aligned(path, 4) || !aligned(accepted, 4) || !aligned(token, 4) || !aligned(work, 8))
         return KVB_EINVAL;
     const int segments = accept_segments(vocab->B, vocab->V);
-    const AcceptArgs a{n_drafts, parent, tokens, target, draft, u, s, path, accepted, token, static_cast<double *>(work),
+    const AcceptArgs a{n_drafts, parent, tokens, target, draft, u, s, path, accepted, token, static_cast<double *>(work), reinterpret_cast<AcceptWalk *>(static_cast<double *>(work) + (int64_t)vocab->B * segments),
                        vocab->stride ? vocab->stride : vocab->V, vocab->B, vocab->T, vocab->V, segments, accept_segment(vocab->V, segments)};
     g_launch_status = hipSuccess;
     launch_accept(vocab->dtype, a, static_cast<hipStream_t>(stream));

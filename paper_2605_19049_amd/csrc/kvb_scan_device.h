@@ -392,6 +392,29 @@ struct TokenTile {
     }
 };
 
+// S += (the tile's transpose, tokens 32 s ..) e, for a state's columns; a group of its row tiles at a time, as registers allow
+template <typename Tok, int KT, int NC>
+__device__ __forceinline__ void mma_columns(f32x4_t (&S)[KT][NC], const uint4 *img, int s, int lane, const uint4 (&e)[NC][FULL])
+{
+    constexpr int G = Tok::NP == 1 || KT < 4 ? KT : KT / 2;
+#pragma unroll
+    for (int t0 = 0; t0 < KT; t0 += G) {
+        uint4 f[G][Tok::NP];
+#pragma unroll
+        for (int t = 0; t < G; ++t)
+            Tok::columns(img, t0 + t, s, lane, f[t]);
+#pragma unroll
+        for (int i = 0; i < Tok::NP; ++i)
+#pragma unroll
+            for (int j = 0; i + j < FULL; ++j)
+#pragma unroll
+                for (int t = 0; t < G; ++t)
+#pragma unroll
+                    for (int n = 0; n < NC; ++n)
+                        S[t0 + t][n] = mfma16x32<bf16_t>(f[t][i], e[n][j], S[t0 + t][n]);
+    }
+}
+
 // Images of triangular matrices: tile (16 rows rt, 32 columns s) has number tile_of(rt, s); in LDS three pieces of it, 16 bytes a lane.
 template <bool UPPER>
 __host__ __device__ constexpr int tile_of(int rt, int s)

@@ -155,8 +155,8 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
             }
             mma_triangle<true, s>(X, mats + SCAN_UNITS, 2 * SCAN_UNITS, lane, p);
         });
-        // D' = scale P' dO + M' beta X, kd = rest kd, X = scale P' dO + rest kd + scale q.k dO
-        float bt[4][4], own_share[4][4];
+        // D' = scale P' dO + M' beta X, kd = rest kd + scale q.k dO, X = scale P' dO + kd; outer: of E rest kd
+        float bt[4][4], inner[16], outer[16];
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {
             const float4 re = gate[16 + 4 * rt + g], be = gate[32 + 4 * rt + g], di = gate[48 + 4 * rt + g];
@@ -164,15 +164,20 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 bt[rt][r] = bs[r];
-                own_share[rt][r] = a.scale * dg[r];
+                float on = 0.0f;
 #pragma unroll
                 for (int ct = 0; ct < NC; ++ct) {
-                    kd[rt][ct][r] *= rs[r];
+                    const float back = rs[r] * kd[rt][ct][r];
+                    on = fmaf(E[rt][ct][r], back, on);
+                    kd[rt][ct][r] = fmaf(a.scale * dg[r], dO[rt][ct][r], back);
                     y[rt][ct][r] = a.scale * X[rt][ct][r];
-                    X[rt][ct][r] = y[rt][ct][r] + kd[rt][ct][r] + own_share[rt][r] * dO[rt][ct][r];
+                    X[rt][ct][r] = y[rt][ct][r] + kd[rt][ct][r];
                 }
+                outer[4 * rt + r] = on;
             }
         }
+        float *sums = ga.part + (own_chunk + (size_t)c * a.Hv) * GRAD_PARTS + (part * NWV + wave) * 2 * SC + 16 * (m / 4) + 4 * g + m % 4;
+        sums[SC] = sum_rows16(outer, m);
         static_for<2>([&](auto step) {
             constexpr int s = step();
             uint4 p[NC][FULL];
@@ -187,25 +192,20 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
             }
             mma_triangle<true, s>(y, mats, 2 * SCAN_UNITS, lane, p);
         });
-        // the tokens' sums of E D' and E rest kd over the wave's columns, and D
-        float inner[16], outer[16];
+        // the tokens' sums of E D' over the wave's columns, and D
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                float in = 0.0f, on = 0.0f;
+                float in = 0.0f;
 #pragma unroll
                 for (int ct = 0; ct < NC; ++ct) {
                     in = fmaf(E[rt][ct][r], y[rt][ct][r], in);
-                    on = fmaf(E[rt][ct][r], kd[rt][ct][r], on);
-                    y[rt][ct][r] += kd[rt][ct][r] + own_share[rt][r] * dO[rt][ct][r];
+                    y[rt][ct][r] += kd[rt][ct][r];
                 }
                 inner[4 * rt + r] = in;
-                outer[4 * rt + r] = on;
             }
-        float *sums = ga.part + (own_chunk + (size_t)c * a.Hv) * GRAD_PARTS + (part * NWV + wave) * 2 * SC + 16 * (m / 4) + 4 * g + m % 4;
         sums[0] = sum_rows16(inner, m);
-        sums[SC] = sum_rows16(outer, m);
         // dS = exp(c_last) dS + Q' scale gamma dO - K' gamma beta D
         const float last = reinterpret_cast<const float *>(gate)[SC - 1];
 #pragma unroll
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
         f32x4_t dv[4][NC];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            uint4 o[NC][FULL], d[NC][FULL], f[KT][PIECES<TIn>];
+            uint4 o[NC][FULL], d[NC][FULL];
 #pragma unroll
             for (int ct = 0; ct < NC; ++ct) {
                 float x[8], z[8];
@@ -232,14 +232,8 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
                 cut8(x, o[ct]);
                 cut8(z, d[ct]);
             }
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-                Tok::columns(qimg, t, s, lane, f[t]);
-            mma(S, f, o);
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-                Tok::columns(kimg, t, s, lane, f[t]);
-            mma(S, f, d);
+            mma_columns<Tok>(S, qimg, s, lane, o);
+            mma_columns<Tok>(S, kimg, s, lane, d);
         }
         put_rows<TIn, NC>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst, 1.0f, dv);
         put(c);

@@ -388,11 +388,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
                 }
                 cut8(x, e[ct]);
             }
-            uint4 f[KT][PIECES<TIn>];
-#pragma unroll
-            for (int t = 0; t < KT; ++t)
-                Tok::columns(kimg, t, s, lane, f[t]);
-            mma(S, f, e);
+            mma_columns<Tok>(S, kimg, s, lane, e);
             if constexpr (!STATES)
                 mma_triangle<false, s>(O, mats + SCAN_UNITS, MATS * SCAN_UNITS, lane, p);
         });
