@@ -240,7 +240,17 @@ __device__ __forceinline__ void pair8(const f32x4_t &a, const f32x4_t &b, float 
 // test and no branch.  Offsets in bytes, 32 bits, from a scalar address.
 struct Buffer {
     __amdgpu_buffer_rsrc_t r;
-    __device__ __forceinline__ Buffer(const void *p, uint32_t bytes) : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, bytes, 0x00020000)) {}
+    // (all scalars, said so: where the compiler is not sure it loops over the lanes)
+    __device__ __forceinline__ Buffer(const void *p, uint32_t bytes)
+        : r(__builtin_amdgcn_make_buffer_rsrc(scalar(p), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000))
+    {
+    }
+    static __device__ __forceinline__ void *scalar(const void *p)
+    {
+        const uint64_t x = reinterpret_cast<uint64_t>(p);
+        const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+        return reinterpret_cast<void *>((uint64_t)hi << 32 | lo);
+    }
     __device__ __forceinline__ uint4 load16(uint32_t at) const { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0)); }
     __device__ __forceinline__ uint2 load8(uint32_t at) const { return __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0)); }
     __device__ __forceinline__ uint32_t load4(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0); }
@@ -261,11 +271,21 @@ __device__ __forceinline__ Raw8<T> load_raw8(const Buffer &b, uint32_t at)
     else
         return Raw8<T>{b.load16(at)};
 }
-// the rows of one head in n tokens (the stride in elements, at most 2^26 bytes: 64 rows in 32 bits)
+// the rows of one head in n tokens, 0 among them (the stride in elements, at most 2^26 bytes: 64 rows in 32 bits)
 template <typename T, int D>
 __device__ __forceinline__ Buffer head_rows(const T *p, int64_t stride, int n)
 {
-    return Buffer(p, (uint32_t)(n - 1) * (uint32_t)(stride * sizeof(T)) + D * (uint32_t)sizeof(T));
+    return Buffer(p, n == 0 ? 0u : (uint32_t)(n - 1) * (uint32_t)(stride * sizeof(T)) + D * (uint32_t)sizeof(T));
+}
+// Here and no later: what the values come from has been waited for, and is not waited for behind the stores and loads that follow.
+template <int N>
+__device__ __forceinline__ void settled(f32x4_t (&x)[4][N])
+{
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            asm volatile("" : "+v"(x[rt][n]));
 }
 
 // A barrier of the workgroup that orders what it has in LDS and leaves loads and stores of memory in flight.

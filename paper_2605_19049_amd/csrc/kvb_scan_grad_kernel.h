@@ -124,10 +124,11 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
                     kd[rt][ct][r] = 0.0f;
                     X[rt][ct][r] = 0.0f;
                 }
+        settled(dO);
+        settled(E);
         lds_barrier();
         store_state(ga.ds + (own_chunk + (size_t)c * a.Hv) * D * D);
-        if (c > 0)
-            request(c - 1);
+        request(max(c - 1, 0));
         // kd = K dS
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {

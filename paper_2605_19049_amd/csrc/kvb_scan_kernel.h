@@ -242,15 +242,15 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
             gnext[i] = __uint_as_float(image.load4(4 * GATES_AT + 4 * (tid + NTH * i)));
         vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst);
     };
-    f32x4_t O[4][NC];
+    f32x4_t O[4][NC] = {};
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
     auto put = [&](int c) {   // (STATES: O holds Z)
         if constexpr (STATES) {
-            put_rows<float, NC>(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), (4 * g * D + col) * 4, 4 * D, 1.0f, O);
+            put_rows<float, NC>(head_rows<float, D>(a.z + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, c < 0 ? 0 : SC), (4 * g * D + col) * 4, 4 * D, 1.0f, O);
             return;
         }
-        TOut *p = static_cast<TOut *>(a.out) + ((size_t)(span.first + c * SC) * a.Hv + hv) * D;
-        put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, min(SC, span.len - c * SC)), oown, ost, a.scale, O);
+        TOut *p = static_cast<TOut *>(a.out) + ((int64_t)(span.first + c * SC) * a.Hv + hv) * D;
+        put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), oown, ost, a.scale, O);
     };
     if (chunks > 0)
         request(0);
@@ -272,12 +272,12 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
                     E[rt][ct][r] = vnext.value(rt, r, ct);
                     y[rt][ct][r] = 0.0f;
                 }
+        settled(E);
         lds_barrier();
-        // the outputs of the chunk before leave here: what a wave waits for at its end is then not a store just made
-        if (c > 0)
-            put(c - 1);
-        if (c + 1 < chunks)
-            request(c + 1);
+        // The outputs of the chunk before leave here: what a wave waits for at the chunk's end is then not a store just made.  (Nothing
+        // for the first, and the last chunk's inputs once more behind it: branches would make the waits wait for everything.)
+        put(c - 1);
+        request(min(c + 1, chunks - 1));
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
