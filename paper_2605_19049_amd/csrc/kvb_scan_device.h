@@ -26,15 +26,16 @@
 namespace kvb_impl {
 
 constexpr int SC = 64;                      // tokens of a chunk
+constexpr int FULL = 3;                     // bf16 pieces of a fp32 value
 constexpr int SCAN_TILES = 6;               // 16 x 32 tiles with something in them of a triangular 64 x 64 matrix
-constexpr int SCAN_UNITS = SCAN_TILES * 64; // of 8 floats each: what a lane holds of a tile as the matrix instruction's first operand
-constexpr int SCAN_MAT = SCAN_UNITS * 8;    // floats of a matrix's image
+constexpr int SCAN_UNITS = SCAN_TILES * 64; // what a lane holds of a tile as the matrix instruction's first operand: 16 bytes of each piece
+constexpr int SCAN_MAT = FULL * SCAN_UNITS; // 16-byte words of a matrix's image: piece, tile, lane
 constexpr int SCAN_GATES = 4 * SC;          // gamma = exp(c), rest = exp(c_last - c), beta, for the gradients q.k; behind a chunk's end
                                             // beta, rest and q.k are 0
 
-// floats of workspace for each (chunk, v-head): M, P and the gates; for the gradients M, M', P' and the gates
-constexpr int SCAN_PREP = 2 * SCAN_MAT + SCAN_GATES;
-constexpr int GRAD_PREP = 3 * SCAN_MAT + SCAN_GATES;
+// floats of workspace for each (chunk, v-head): the gates, M and P; for the gradients the gates, M, M' and P'
+constexpr int SCAN_PREP = SCAN_GATES + 2 * 4 * SCAN_MAT;
+constexpr int GRAD_PREP = SCAN_GATES + 3 * 4 * SCAN_MAT;
 
 struct ScanArgs {
     const void *q, *k, *v;
@@ -145,10 +146,9 @@ __device__ __forceinline__ float sum_rows16(float (&x)[16], int m)
     return x[0];
 }
 
-// bf16 pieces of an input value, and the most that any fp32 value is cut into
+// bf16 pieces of an input value
 template <typename T>
 constexpr int PIECES = __is_same(T, bf16_t) ? 1 : __is_same(T, f16_t) ? 2 : 3;
-constexpr int FULL = 3;
 
 // (both at once: the conversion of a pair is one instruction)
 __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi)
@@ -239,11 +239,21 @@ __device__ __forceinline__ void pair8(const f32x4_t &a, const f32x4_t &b, float 
 // A stretch of memory: loads behind its end give zeros and stores there do nothing, so that a chunk's missing tokens need no
 // test and no branch.  Offsets in bytes, 32 bits, from a scalar address.
 struct Buffer {
+    typedef int Words __attribute__((ext_vector_type(4)));
     __amdgpu_buffer_rsrc_t r;
+    Words words;   // the same, for what there is no builtin of that fits (to_lds)
     // (all scalars, said so: where the compiler is not sure it loops over the lanes)
     __device__ __forceinline__ Buffer(const void *p, uint32_t bytes)
-        : r(__builtin_amdgcn_make_buffer_rsrc(scalar(p), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000))
+        : r(__builtin_amdgcn_make_buffer_rsrc(scalar(p), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000)),
+          words{(int)(uint32_t) reinterpret_cast<uint64_t>(scalar(p)), (int)(reinterpret_cast<uint64_t>(scalar(p)) >> 32 & 0xFFFF),
+                (int)__builtin_amdgcn_readfirstlane(bytes), 0x00020000}
     {
+    }
+    // 16 bytes for each lane of the wave straight to LDS, to `to` (lds_at; the same in all lanes) + 16 lane.  Written by hand: behind
+    // the builtin the compiler makes any read of LDS wait for it, also of another buffer.  lds_loads_done() is the wait.
+    __device__ __forceinline__ void to_lds(uint32_t to, uint32_t at) const
+    {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(words) : "memory", "m0");
     }
     static __device__ __forceinline__ void *scalar(const void *p)
     {
@@ -263,6 +273,14 @@ struct Buffer {
     __device__ __forceinline__ void store4(uint32_t at, uint32_t x) const { __builtin_amdgcn_raw_buffer_store_b32(x, r, at, 0, 0); }
     __device__ __forceinline__ void store2(uint32_t at, uint16_t x) const { __builtin_amdgcn_raw_buffer_store_b16(x, r, at, 0, 0); }
 };
+__device__ __forceinline__ uint32_t lds_at(const uint4 *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint4 *)p; }
+// x, anew: what is worked out from it inside a loop stays there and takes no register around it
+__device__ __forceinline__ uint32_t anew(uint32_t x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ void lds_loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 template <typename T>
 __device__ __forceinline__ Raw8<T> load_raw8(const Buffer &b, uint32_t at)
 {
@@ -392,6 +410,17 @@ struct TokenTile {
                 img[(j * 4 * STEPS + u) * 64 + lane] = p[j];
         }
     }
+    // the same without registers between, for what is one piece as it comes
+    static __device__ __forceinline__ void to_lds(const Buffer &b, uint32_t stride_bytes, uint32_t img, int wave, int lane)
+    {
+        static_assert(NP == 1);
+        const uint32_t own = anew(lane % 16) * stride_bytes + 8 * (lane / 16) * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int u = wave + NWV * i;
+            b.to_lds(img + u * 1024, own + 16 * (u / STEPS) * stride_bytes + 32 * (u % STEPS) * (uint32_t)sizeof(T));
+        }
+    }
     // rows of tokens as the first operand: tile rt, columns 32 ks ..
     static __device__ __forceinline__ void rows(const uint4 *img, int rt, int ks, int lane, uint4 (&a)[NP])
     {
@@ -442,35 +471,37 @@ __host__ __device__ constexpr int tile_of(int rt, int s)
     return UPPER ? (rt < 2 ? 2 * rt + s : 2 + rt) : (rt < 2 ? rt : 2 * rt - 2 + s);
 }
 
-// N units of 8 floats from a workspace into pieces in LDS, by all NTH threads of the workgroup
-template <int N, int NTH>
-struct MatTile {
-    static constexpr int EACH = (N + NTH - 1) / NTH;
-    Raw8<float> x[EACH];
-    __device__ __forceinline__ void load(const Buffer &b, int tid)   // (of N units)
+// N 16-byte words (blocks of 64) from a workspace to LDS as they are, by the NWV waves of the workgroup: through registers, or without
+template <int N, int NWV>
+struct Words {
+    static_assert(N % 64 == 0);
+    static constexpr int BLOCKS = N / 64, EACH = (BLOCKS + NWV - 1) / NWV;
+    uint4 x[EACH];
+    static __device__ __forceinline__ bool has(int i, int wave) { return NWV * (i + 1) <= BLOCKS || wave + NWV * i < BLOCKS; }
+    __device__ __forceinline__ void load(const Buffer &b, int wave, int lane)   // (of N words: zeros behind them)
     {
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            x[i] = load_raw8<float>(b, (tid + NTH * i) * 32);
+            x[i] = b.load16((wave + NWV * i) * 1024 + lane * 16);
     }
-    __device__ __forceinline__ void store(uint4 *to, int tid) const
+    __device__ __forceinline__ void store(uint4 *to, int wave, int lane) const
     {
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (N % NTH == 0 || tid + NTH * i < N) {
-                float f[8];
-                uint4 p[FULL];
-                unpack8(x[i], f);
-                cut8(f, p);
+            if (has(i, wave))
+                to[(wave + NWV * i) * 64 + lane] = x[i];
+    }
+    static __device__ __forceinline__ void to_lds(const Buffer &b, uint32_t to, int wave, int lane)
+    {
 #pragma unroll
-                for (int j = 0; j < FULL; ++j)
-                    to[j * N + tid + NTH * i] = p[j];
-            }
+        for (int i = 0; i < EACH; ++i)
+            if (has(i, wave))
+                b.to_lds(to + (wave + NWV * i) * 1024, (wave + NWV * i) * 1024 + lane * 16);
     }
 };
-// c += (matrix) (b), of which b holds rows 32 s .. of the second operand: img is the image in LDS, its pieces `apart` units from each other
+// c += (matrix) (b), of which b holds rows 32 s .. of the second operand; img: the matrix's image in LDS
 template <bool UPPER, int S, int NC, int NB>
-__device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *img, int apart, int lane, const uint4 (&b)[NC][NB])
+__device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *img, int lane, const uint4 (&b)[NC][NB])
 {
     constexpr int FROM = !UPPER && S == 1 ? 2 : 0, TO = UPPER && S == 0 ? 2 : 4;
     uint4 a[TO - FROM][FULL];
@@ -478,7 +509,7 @@ __device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *i
     for (int rt = FROM; rt < TO; ++rt)
 #pragma unroll
         for (int j = 0; j < FULL; ++j)
-            a[rt - FROM][j] = img[j * apart + tile_of<UPPER>(rt, S) * 64 + lane];
+            a[rt - FROM][j] = img[j * SCAN_UNITS + tile_of<UPPER>(rt, S) * 64 + lane];
 #pragma unroll
     for (int i = 0; i < FULL; ++i)
 #pragma unroll
@@ -488,6 +519,31 @@ __device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *i
 #pragma unroll
                 for (int n = 0; n < NC; ++n)
                     c[rt][n] = mfma16x32<bf16_t>(a[rt - FROM][i], b[n][j], c[rt][n]);
+}
+
+// Threads that a kernel over the chunks is built for.  With DMA a wave needs less than 256 registers; built for 8 waves a workgroup, the
+// compiler keeps to that, and does without moves to and from the accumulation registers.
+template <typename TIn>
+constexpr int scan_bound(int waves) { return PIECES<TIn> == 1 ? 512 : 64 * waves; }
+
+// How a head's columns are split over workgroups, 16 a wave: f<waves of a workgroup>(workgroups).
+#ifndef WIDE_FROM
+#define WIDE_FROM 256
+#endif
+template <typename TIn, int D, typename F>
+void scan_split(const ScanArgs &a, F &&f)
+{
+    const int64_t heads = (int64_t)a.B * a.Hv;
+    if constexpr (D == 32) {
+        f.template operator()<2>(heads);
+    } else if constexpr (D == 64 || PIECES<TIn> > 1) {
+        f.template operator()<4>(heads * (D / 64));
+    } else {
+        if (heads >= WIDE_FROM)
+            f.template operator()<8>(heads);
+        else
+            f.template operator()<4>(heads * 2);
+    }
 }
 
 // One kernel of a call that makes several; an armed timer spans them from the first one's start to the last one's end.

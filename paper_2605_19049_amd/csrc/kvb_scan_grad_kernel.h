@@ -22,13 +22,15 @@
 namespace kvb_impl {
 
 template <typename TIn, typename TOut, int D, int NC, int NWV>
-__global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const GradArgs ga)
+__global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(const GradArgs ga)
 {
-    constexpr int NTH = 64 * NWV, KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
+    constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
     using Tok = TokenTile<TIn, D, NWV>;
-    using Mat = MatTile<2 * SCAN_UNITS, NTH>;
-    __shared__ uint4 kimg[Tok::WORDS], qimg[Tok::WORDS], mats[FULL * 2 * SCAN_UNITS];
-    __shared__ float4 gate[SCAN_GATES / 4];
+    constexpr bool DMA = Tok::NP == 1;   // (as in kvb_scan_kernel)
+    constexpr int BUF = DMA ? 2 : 1;
+    using Gates = Words<SCAN_GATES / 4, NWV>;
+    using Mats = Words<2 * SCAN_MAT, NWV>;
+    __shared__ uint4 kimgs[BUF][Tok::WORDS], qimgs[BUF][Tok::WORDS], matss[BUF][2 * SCAN_MAT], gatess[BUF][SCAN_GATES / 4];
     const ScanArgs &a = ga.f;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
@@ -79,39 +81,52 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
     const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
     const uint32_t vown = 4 * g * vst + col * sizeof(TIn), oown = 4 * g * ost + col * sizeof(TOut), eown = (4 * g * D + col) * 4;
 
-    Tok knext, qnext;
-    Mat mnext;
-    float gnext[SCAN_GATES / NTH];
+    const uint32_t kat = lds_at(kimgs[0]), qat = lds_at(qimgs[0]), mat = lds_at(matss[0]), gat = lds_at(gatess[0]);
+    Tok knext, qnext;   // (without DMA)
+    Mats mnext;
+    Gates gnext;
     Rows64<TOut, NC> onext;
     Rows64<float, NC> znext;
     Rows64<TIn, NC> vnext;
-    auto request = [&](int c) {
+    auto request = [&](int c, int buf) {
         const int n = min(SC, span.len - c * SC);
-        knext.load(head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n), kst, wave, lane);
-        qnext.load(head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n), qst, wave, lane);
-        const Buffer image(a.prep + (own_chunk + (size_t)c * a.Hv) * GRAD_PREP + SCAN_MAT, 4 * (GRAD_PREP - SCAN_MAT));
-        mnext.load(image, tid);
-#pragma unroll
-        for (int i = 0; i < SCAN_GATES / NTH; ++i)
-            gnext[i] = __uint_as_float(image.load4(8 * SCAN_MAT + 4 * (tid + NTH * i)));
-        onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), oown, ost);
-        znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), eown, 4 * D);
-        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst);
+        const Buffer kb = head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n);
+        const Buffer qb = head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n);
+        const float *prep = a.prep + (own_chunk + (size_t)c * a.Hv) * GRAD_PREP;
+        const Buffer gates(prep, 4 * SCAN_GATES), images(prep + SCAN_GATES + 4 * SCAN_MAT, 2 * 16 * SCAN_MAT);
+        onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), anew(oown), ost);
+        znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D);
+        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
+        if constexpr (DMA) {
+            Tok::to_lds(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
+            Tok::to_lds(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
+            Mats::to_lds(images, mat + buf * 32 * SCAN_MAT, wave, lane);
+            Gates::to_lds(gates, gat + buf * 4 * SCAN_GATES, wave, lane);
+        } else {
+            knext.load(kb, kst, wave, lane);
+            qnext.load(qb, qst, wave, lane);
+            mnext.load(images, wave, lane);
+            gnext.load(gates, wave, lane);
+        }
     };
     f32x4_t y[4][NC];   // D of the chunk
     auto put = [&](int c) {
-        put_rows<float, NC>(head_rows<float, D>(ga.dd + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), eown, 4 * D, 1.0f, y);
+        put_rows<float, NC>(head_rows<float, D>(ga.dd + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D, 1.0f, y);
     };
     if (chunks > 0)
-        request(chunks - 1);
-    for (int c = chunks - 1; c >= 0; --c) {
+        request(chunks - 1, 0);
+    for (int c = chunks - 1, buf = 0; c >= 0; --c, buf = DMA ? buf ^ 1 : 0) {
         const int n = min(SC, span.len - c * SC);
-        knext.store(kimg, wave, lane);
-        qnext.store(qimg, wave, lane);
-        mnext.store(mats, tid);
-#pragma unroll
-        for (int i = 0; i < SCAN_GATES / NTH; ++i)
-            reinterpret_cast<float *>(gate)[tid + NTH * i] = gnext[i];
+        const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = matss[buf];
+        const float4 *gate = reinterpret_cast<const float4 *>(gatess[buf]);
+        if constexpr (DMA) {
+            lds_loads_done();
+        } else {
+            knext.store(kimgs[0], wave, lane);
+            qnext.store(qimgs[0], wave, lane);
+            mnext.store(matss[0], wave, lane);
+            gnext.store(gatess[0], wave, lane);
+        }
         f32x4_t dO[4][NC], E[4][NC], kd[4][NC], X[4][NC];
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
@@ -128,7 +143,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
         settled(E);
         lds_barrier();
         store_state(ga.ds + (own_chunk + (size_t)c * a.Hv) * D * D);
-        request(max(c - 1, 0));
+        request(max(c - 1, 0), buf ^ 1);
         // kd = K dS
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -154,7 +169,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
                 pair8(dO[2 * s][ct], dO[2 * s + 1][ct], x);
                 cut8(x, p[ct]);
             }
-            mma_triangle<true, s>(X, mats + SCAN_UNITS, 2 * SCAN_UNITS, lane, p);
+            mma_triangle<true, s>(X, mats + SCAN_MAT, lane, p);
         });
         // D' = scale P' dO + M' beta X, kd = rest kd + scale q.k dO, X = scale P' dO + kd; outer: of E rest kd
         float bt[4][4], inner[16], outer[16];
@@ -191,7 +206,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
                     x[j] *= bt[2 * s + j / 4][j % 4];
                 cut8(x, p[ct]);
             }
-            mma_triangle<true, s>(y, mats, 2 * SCAN_UNITS, lane, p);
+            mma_triangle<true, s>(y, mats, lane, p);
         });
         // the tokens' sums of E D' over the wave's columns, and D
 #pragma unroll
@@ -236,9 +251,10 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_reverse_kernel(const Gra
             mma_columns<Tok>(S, qimg, s, lane, o);
             mma_columns<Tok>(S, kimg, s, lane, d);
         }
-        put_rows<TIn, NC>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst, 1.0f, dv);
+        put_rows<TIn, NC>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst, 1.0f, dv);
         put(c);
-        lds_barrier();
+        if constexpr (!DMA)
+            lds_barrier();
     }
     if (ga.dstate0)
         store_state(ga.dstate0 + own);
@@ -283,7 +299,7 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
     for (int h = 0; h < a.r; ++h) {
         const int hv = hk * a.r + h;
         const size_t unit = (size_t)w * a.Hv + hv;
-        const float *gates = a.prep + unit * GRAD_PREP + 3 * SCAN_MAT;
+        const float *gates = a.prep + unit * GRAD_PREP;
         float gamma[4], rest[4], beta[4];   // of token 16 nt + m
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
@@ -611,13 +627,14 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
 template <typename TIn, typename TOut, int D>
 void launch_scan_grad_sized(const GradArgs &a, hipStream_t stream)
 {
-    constexpr int NWV = D >= 64 ? 4 : 2;
-    const int64_t chunks = scan_chunks(a.f.n_tokens, a.f.B), blocks = (int64_t)a.f.B * a.f.Hv * (D / (16 * NWV));
-    if (a.f.n_tokens > 0) {
+    const int64_t chunks = scan_chunks(a.f.n_tokens, a.f.B);
+    if (a.f.n_tokens > 0)
         launch_part(kvb_scan_prep_kernel<TIn, D, true>, true, false, chunks * a.f.Hv, 256, stream, a.f);
-        launch_part(kvb_scan_kernel<TIn, float, D, 1, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
-    }
-    launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, 1, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, blocks, 64 * NWV, stream, a);
+    scan_split<TIn, D>(a.f, [&]<int NWV>(int64_t blocks) {
+        if (a.f.n_tokens > 0)
+            launch_part(kvb_scan_kernel<TIn, float, D, 1, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
+        launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, 1, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, blocks, 64 * NWV, stream, a);
+    });
     if (a.f.n_tokens > 0)
         launch_part(kvb_scan_grad_kernel<TIn, TOut, D, 1>, false, true, chunks * a.f.Hk, 2 * D, stream, a);
 }

@@ -15,7 +15,7 @@ namespace kvb_impl {
 template <typename TIn, int D, bool GRAD>
 __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 {
-    constexpr int LD = SC + 4, MATS = GRAD ? 3 : 2, PREP = MATS * SCAN_MAT + SCAN_GATES;
+    constexpr int LD = SC + 4, MATS = GRAD ? 3 : 2, PREP = GRAD ? GRAD_PREP : SCAN_PREP;
     __shared__ float gs[SC * LD], ps[SC * LD], td[4 * 16 * 20], beta[SC];
     __shared__ double cs[SC];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
     const double c = sum_below(lane < at.n ? log2_gate(g1) : 0.0);
     if (wave == 0) {
         const double last = __shfl(c, 63);
-        float *gates = prep + MATS * SCAN_MAT;
+        float *gates = prep;
         const float bt = lane < at.n ? b1 : 0.0f;
         gates[lane] = decay(c);
         gates[SC + lane] = lane < at.n ? decay(last - c) : 0.0f;
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
                 gr[r] = i > j ? d * kk[nt][r] : 0.0f;
                 pr[r] = (GRAD ? i > j : i >= j) ? d * qk[nt][r] : 0.0f;
                 if (GRAD && i == j)
-                    prep[MATS * SCAN_MAT + 3 * SC + i] = qk[nt][r];
+                    prep[3 * SC + i] = qk[nt][r];
             }
             if (nt == wave)
                 *reinterpret_cast<float4 *>(gt + m * 20 + 4 * g) = make_float4(gr[0], gr[1], gr[2], gr[3]);
@@ -160,19 +160,25 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
     for (int u = tid; u < MATS * SCAN_UNITS; u += 256) {
         const int of = u / SCAN_UNITS, t = (u - of * SCAN_UNITS) / 64;
         const float *from = (of == MATS - 1 ? ps : gs);
-        float4 *to = reinterpret_cast<float4 *>(prep + u * 8);
+        float x[8];
         if (GRAD && of > 0) {   // the transpose: tile t is tile_of<true>(rt, s)
             const int rt = t < 4 ? t / 2 : t - 2, s = t < 4 ? t % 2 : 1;
             from += (32 * s + 4 * g) * LD + 16 * rt + m;
-            to[0] = make_float4(from[0], from[LD], from[2 * LD], from[3 * LD]);
-            from += 16 * LD;
-            to[1] = make_float4(from[0], from[LD], from[2 * LD], from[3 * LD]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                x[j] = from[(16 * (j / 4) + j % 4) * LD];
         } else {                // tile_of<false>(rt, s)
             const int rt = t < 2 ? t : 1 + t / 2, s = t < 2 ? 0 : t % 2;
             from += (16 * rt + m) * LD + 32 * s + 4 * g;
-            to[0] = *reinterpret_cast<const float4 *>(from);
-            to[1] = *reinterpret_cast<const float4 *>(from + 16);
+            const float4 lo = *reinterpret_cast<const float4 *>(from), hi = *reinterpret_cast<const float4 *>(from + 16);
+            pair8(f32x4_t{lo.x, lo.y, lo.z, lo.w}, f32x4_t{hi.x, hi.y, hi.z, hi.w}, x);
         }
+        uint4 p[FULL];
+        cut8(x, p);
+        uint4 *to = reinterpret_cast<uint4 *>(prep + SCAN_GATES) + of * SCAN_MAT + u - of * SCAN_UNITS;
+#pragma unroll
+        for (int j = 0; j < FULL; ++j)
+            to[j * SCAN_UNITS] = p[j];
     }
 }
 
@@ -183,14 +189,15 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 // STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
 // than the decays, which a difference of E and V would lose).
 template <typename TIn, typename TOut, int D, int NC, int NWV, bool STATES>
-__global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
+__global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const ScanArgs a)
 {
-    constexpr int NTH = 64 * NWV, KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
+    constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
     using Tok = TokenTile<TIn, D, NWV>;
-    constexpr int MATS = STATES ? 1 : 2, GATES_AT = (STATES ? 3 : 2) * SCAN_MAT, PREP = GATES_AT + SCAN_GATES;
-    using Mat = MatTile<MATS * SCAN_UNITS, NTH>;
-    __shared__ uint4 kimg[Tok::WORDS], qimg[STATES ? 1 : Tok::WORDS], mats[FULL * MATS * SCAN_UNITS];
-    __shared__ float4 gate[SCAN_GATES / 4];
+    constexpr bool DMA = Tok::NP == 1;   // keys and queries are operands as they come: all images go to LDS without passing registers, into
+    constexpr int BUF = DMA ? 2 : 1;     // one buffer while the other is in use
+    constexpr int WORDS = SCAN_GATES / 4 + (STATES ? 1 : 2) * SCAN_MAT, PREP = STATES ? GRAD_PREP : SCAN_PREP;
+    using Prep = Words<WORDS, NWV>;
+    __shared__ uint4 kimgs[BUF][Tok::WORDS], qimgs[BUF][STATES ? 1 : Tok::WORDS], preps[BUF][WORDS];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
     const int b = unit / a.Hv, hv = unit - b * a.Hv, hk = hv / a.r;
@@ -226,21 +233,27 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
     const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
     const uint32_t vown = 4 * g * vst + col * sizeof(TIn), oown = 4 * g * ost + col * sizeof(TOut);
 
-    Tok knext, qnext;
-    Mat mnext;
-    float gnext[SCAN_GATES / NTH];
+    const uint32_t kat = lds_at(kimgs[0]), qat = lds_at(qimgs[0]), pat = lds_at(preps[0]);
+    Tok knext, qnext;   // (without DMA)
+    Prep pnext;
     Rows64<TIn, NC> vnext;
-    auto request = [&](int c) {
+    auto request = [&](int c, int buf) {
         const int n = min(SC, span.len - c * SC);
-        knext.load(head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n), kst, wave, lane);
-        if constexpr (!STATES)
-            qnext.load(head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n), qst, wave, lane);
-        const Buffer image(prep + c * prep_step, 4 * PREP);
-        mnext.load(image, tid);
-#pragma unroll
-        for (int i = 0; i < SCAN_GATES / NTH; ++i)
-            gnext[i] = __uint_as_float(image.load4(4 * GATES_AT + 4 * (tid + NTH * i)));
-        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), vown, vst);
+        const Buffer kb = head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n);
+        const Buffer qb = head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n);
+        const Buffer image(prep + c * prep_step, 16 * WORDS);
+        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
+        if constexpr (DMA) {
+            Tok::to_lds(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
+            if constexpr (!STATES)
+                Tok::to_lds(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
+            Prep::to_lds(image, pat + buf * 16 * WORDS, wave, lane);
+        } else {
+            knext.load(kb, kst, wave, lane);
+            if constexpr (!STATES)
+                qnext.load(qb, qst, wave, lane);
+            pnext.load(image, wave, lane);
+        }
     };
     f32x4_t O[4][NC] = {};
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
@@ -250,18 +263,22 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
             return;
         }
         TOut *p = static_cast<TOut *>(a.out) + ((int64_t)(span.first + c * SC) * a.Hv + hv) * D;
-        put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), oown, ost, a.scale, O);
+        put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), anew(oown), ost, a.scale, O);
     };
     if (chunks > 0)
-        request(0);
+        request(0, 0);
     for (int c = 0; c < chunks; ++c) {
-        knext.store(kimg, wave, lane);
-        if constexpr (!STATES)
-            qnext.store(qimg, wave, lane);
-        mnext.store(mats, tid);
-#pragma unroll
-        for (int i = 0; i < SCAN_GATES / NTH; ++i)
-            reinterpret_cast<float *>(gate)[tid + NTH * i] = gnext[i];
+        const int buf = DMA ? c & 1 : 0;
+        const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = preps[buf] + SCAN_GATES / 4;
+        const float4 *gate = reinterpret_cast<const float4 *>(preps[buf]);
+        if constexpr (DMA) {
+            lds_loads_done();
+        } else {
+            knext.store(kimgs[0], wave, lane);
+            if constexpr (!STATES)
+                qnext.store(qimgs[0], wave, lane);
+            pnext.store(preps[0], wave, lane);
+        }
         f32x4_t E[4][NC], y[4][NC];
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
@@ -277,7 +294,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
         // The outputs of the chunk before leave here: what a wave waits for at the chunk's end is then not a store just made.  (Nothing
         // for the first, and the last chunk's inputs once more behind it: branches would make the waits wait for everything.)
         put(c - 1);
-        request(min(c + 1, chunks - 1));
+        request(min(c + 1, chunks - 1), buf ^ 1);
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
@@ -345,7 +362,7 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
                 pair8(y[2 * s][ct], y[2 * s + 1][ct], x);
                 cut8(x, p[ct]);
             }
-            mma_triangle<false, s>(STATES ? O : E, mats, MATS * SCAN_UNITS, lane, p);
+            mma_triangle<false, s>(STATES ? O : E, mats, lane, p);
         });
         if constexpr (STATES) {
 #pragma unroll
@@ -390,9 +407,10 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
             }
             mma_columns<Tok>(S, kimg, s, lane, e);
             if constexpr (!STATES)
-                mma_triangle<false, s>(O, mats + SCAN_UNITS, MATS * SCAN_UNITS, lane, p);
+                mma_triangle<false, s>(O, mats + SCAN_MAT, lane, p);
         });
-        lds_barrier();
+        if constexpr (!DMA)
+            lds_barrier();
     }
     if (chunks > 0)
         put(chunks - 1);
@@ -412,10 +430,11 @@ __global__ __launch_bounds__(64 * NWV, 1) void kvb_scan_kernel(const ScanArgs a)
 template <typename TIn, typename TOut, int D>
 void launch_scan_sized(const ScanArgs &a, hipStream_t stream)
 {
-    constexpr int NWV = D >= 64 ? 4 : 2;
     if (a.n_tokens > 0)
         launch_part(kvb_scan_prep_kernel<TIn, D, false>, true, false, scan_chunks(a.n_tokens, a.B) * a.Hv, 256, stream, a);
-    launch_part(kvb_scan_kernel<TIn, TOut, D, 1, NWV, false>, a.n_tokens == 0, true, (int64_t)a.B * a.Hv * (D / (16 * NWV)), 64 * NWV, stream, a);
+    scan_split<TIn, D>(a, [&]<int NWV>(int64_t blocks) {
+        launch_part(kvb_scan_kernel<TIn, TOut, D, 1, NWV, false>, a.n_tokens == 0, true, blocks, 64 * NWV, stream, a);
+    });
 }
 template <typename TIn, typename TOut>
 void launch_scan_typed(int d, const ScanArgs &a, hipStream_t stream)
