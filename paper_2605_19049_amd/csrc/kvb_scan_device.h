@@ -250,10 +250,11 @@ struct Buffer {
     {
     }
     // 16 bytes for each lane of the wave straight to LDS, to `to` (lds_at; the same in all lanes) + 16 lane.  Written by hand: behind
-    // the builtin the compiler makes any read of LDS wait for it, also of another buffer.  lds_loads_done() is the wait.
+    // the builtin the compiler makes any read of LDS wait for it, also of another buffer.  lds_loads_done() is the wait.  (No clobber
+    // of memory either, for reads of the other buffer may pass: those of this one are behind a barrier on both sides.)
     __device__ __forceinline__ void to_lds(uint32_t to, uint32_t at) const
     {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(words) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(at), "s"(words) : "m0");
     }
     static __device__ __forceinline__ void *scalar(const void *p)
     {
@@ -410,13 +411,14 @@ struct TokenTile {
                 img[(j * 4 * STEPS + u) * 64 + lane] = p[j];
         }
     }
-    // the same without registers between, for what is one piece as it comes
+    // the same without registers between, for what is one piece as it comes; part PART of OF
+    template <int PART, int OF>
     static __device__ __forceinline__ void to_lds(const Buffer &b, uint32_t stride_bytes, uint32_t img, int wave, int lane)
     {
         static_assert(NP == 1);
         const uint32_t own = anew(lane % 16) * stride_bytes + 8 * (lane / 16) * (uint32_t)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
+        for (int i = N * PART / OF; i < N * (PART + 1) / OF; ++i) {
             const int u = wave + NWV * i;
             b.to_lds(img + u * 1024, own + 16 * (u / STEPS) * stride_bytes + 32 * (u % STEPS) * (uint32_t)sizeof(T));
         }
@@ -491,10 +493,11 @@ struct Words {
             if (has(i, wave))
                 to[(wave + NWV * i) * 64 + lane] = x[i];
     }
+    template <int PART, int OF>
     static __device__ __forceinline__ void to_lds(const Buffer &b, uint32_t to, int wave, int lane)
     {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i)
+        for (int i = EACH * PART / OF; i < EACH * (PART + 1) / OF; ++i)
             if (has(i, wave))
                 b.to_lds(to + (wave + NWV * i) * 1024, (wave + NWV * i) * 1024 + lane * 16);
     }

@@ -88,25 +88,28 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     Rows64<TOut, NC> onext;
     Rows64<float, NC> znext;
     Rows64<TIn, NC> vnext;
-    auto request = [&](int c, int buf) {
+    auto request = [&](auto step, int c, int buf) {   // (in parts: kvb_scan_kernel)
+        constexpr int PART = step();
         const int n = min(SC, span.len - c * SC);
         const Buffer kb = head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n);
         const Buffer qb = head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n);
         const float *prep = a.prep + (own_chunk + (size_t)c * a.Hv) * GRAD_PREP;
         const Buffer gates(prep, 4 * SCAN_GATES), images(prep + SCAN_GATES + 4 * SCAN_MAT, 2 * 16 * SCAN_MAT);
-        onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), anew(oown), ost);
-        znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D);
-        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
         if constexpr (DMA) {
-            Tok::to_lds(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
-            Tok::to_lds(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
-            Mats::to_lds(images, mat + buf * 32 * SCAN_MAT, wave, lane);
-            Gates::to_lds(gates, gat + buf * 4 * SCAN_GATES, wave, lane);
-        } else {
+            Tok::template to_lds<PART, KS>(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
+            Tok::template to_lds<PART, KS>(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
+            Mats::template to_lds<PART, KS>(images, mat + buf * 32 * SCAN_MAT, wave, lane);
+            Gates::template to_lds<PART, KS>(gates, gat + buf * 4 * SCAN_GATES, wave, lane);
+        } else if constexpr (PART == 0) {
             knext.load(kb, kst, wave, lane);
             qnext.load(qb, qst, wave, lane);
             mnext.load(images, wave, lane);
             gnext.load(gates, wave, lane);
+        }
+        if constexpr (PART == KS - 1) {
+            onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), anew(oown), ost);
+            znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D);
+            vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
         }
     };
     f32x4_t y[4][NC];   // D of the chunk
@@ -114,7 +117,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
         put_rows<float, NC>(head_rows<float, D>(ga.dd + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D, 1.0f, y);
     };
     if (chunks > 0)
-        request(chunks - 1, 0);
+        static_for<KS>([&](auto step) { request(step, chunks - 1, 0); });
     for (int c = chunks - 1, buf = 0; c >= 0; --c, buf = DMA ? buf ^ 1 : 0) {
         const int n = min(SC, span.len - c * SC);
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = matss[buf];
@@ -143,10 +146,10 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
         settled(E);
         lds_barrier();
         store_state(ga.ds + (own_chunk + (size_t)c * a.Hv) * D * D);
-        request(max(c - 1, 0), buf ^ 1);
         // kd = K dS
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
+        static_for<KS>([&](auto step) {
+            constexpr int ks = step();
+            request(step, max(c - 1, 0), buf ^ 1);
             uint4 s[NC][FULL], f[4][PIECES<TIn>];
 #pragma unroll
             for (int ct = 0; ct < NC; ++ct) {
@@ -158,7 +161,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
             for (int rt = 0; rt < 4; ++rt)
                 Tok::rows(kimg, rt, ks, lane, f[rt]);
             mma(kd, f, s);
-        }
+        });
         // X = scale P' dO + rest kd
         static_for<2>([&](auto step) {
             constexpr int s = step();

@@ -237,23 +237,27 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     Tok knext, qnext;   // (without DMA)
     Prep pnext;
     Rows64<TIn, NC> vnext;
-    auto request = [&](int c, int buf) {
+    // What chunk c needs, asked for in KS parts, one for each step of the products with the state: at once, the requests would
+    // wait for each other at the memory unit and the wave with them.
+    auto request = [&](auto step, int c, int buf) {
+        constexpr int PART = step();
         const int n = min(SC, span.len - c * SC);
         const Buffer kb = head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n);
         const Buffer qb = head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n);
         const Buffer image(prep + c * prep_step, 16 * WORDS);
-        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
         if constexpr (DMA) {
-            Tok::to_lds(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
+            Tok::template to_lds<PART, KS>(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
             if constexpr (!STATES)
-                Tok::to_lds(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
-            Prep::to_lds(image, pat + buf * 16 * WORDS, wave, lane);
-        } else {
+                Tok::template to_lds<PART, KS>(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
+            Prep::template to_lds<PART, KS>(image, pat + buf * 16 * WORDS, wave, lane);
+        } else if constexpr (PART == 0) {
             knext.load(kb, kst, wave, lane);
             if constexpr (!STATES)
                 qnext.load(qb, qst, wave, lane);
             pnext.load(image, wave, lane);
         }
+        if constexpr (PART == KS - 1)
+            vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
     };
     f32x4_t O[4][NC] = {};
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
@@ -266,7 +270,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), anew(oown), ost, a.scale, O);
     };
     if (chunks > 0)
-        request(0, 0);
+        static_for<KS>([&](auto step) { request(step, 0, 0); });
     for (int c = 0; c < chunks; ++c) {
         const int buf = DMA ? c & 1 : 0;
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = preps[buf] + SCAN_GATES / 4;
@@ -294,7 +298,6 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         // The outputs of the chunk before leave here: what a wave waits for at the chunk's end is then not a store just made.  (Nothing
         // for the first, and the last chunk's inputs once more behind it: branches would make the waits wait for everything.)
         put(c - 1);
-        request(min(c + 1, chunks - 1), buf ^ 1);
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
@@ -314,8 +317,9 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                 }
         }
         // y = K S, O = Q S
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
+        static_for<KS>([&](auto step) {
+            constexpr int ks = step();
+            request(step, min(c + 1, chunks - 1), buf ^ 1);
             uint4 s[NC][FULL];
 #pragma unroll
             for (int ct = 0; ct < NC; ++ct) {
@@ -333,7 +337,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
             mma(y, fk, s);
             if constexpr (!STATES)
                 mma(O, fq, s);
-        }
+        });
         // Y = V - gamma y, y = beta Y, E = Y + M y
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {
