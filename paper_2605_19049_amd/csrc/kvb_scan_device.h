@@ -158,26 +158,89 @@ __device__ __forceinline__ uint32_t pair_bf16(float lo, float hi)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{lo, hi}, v2b));
 }
 
-// Eight values in N pieces, to nearest: each piece has 8 bits of what the ones before left.
+// Values in N pieces, to nearest: each piece has 8 bits of what the ones before left.  Two values are a word of each piece, eight an
+// operand's 16 bytes.
+template <int N>
+__device__ __forceinline__ void cut2(float x, float y, uint32_t (&p)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p[i] = pair_bf16(x, y);
+        x -= __uint_as_float(p[i] << 16);
+        y -= __uint_as_float(p[i] & 0xFFFF0000u);
+    }
+}
 template <int N>
 __device__ __forceinline__ void cut8(const float (&x)[8], uint4 (&p)[N])
 {
-    float rest[8];
+    uint32_t w[4][N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        rest[j] = x[j];
+    for (int j = 0; j < 4; ++j)
+        cut2(x[2 * j], x[2 * j + 1], w[j]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            w[j] = pair_bf16(rest[2 * j], rest[2 * j + 1]);
-            rest[2 * j] -= __uint_as_float(w[j] << 16);
-            rest[2 * j + 1] -= __uint_as_float(w[j] & 0xFFFF0000u);
-        }
-        p[i] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int i = 0; i < N; ++i)
+        p[i] = make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]);
 }
+// An operand's pieces put together word by word
+template <int N>
+struct Pieces {
+    uint32_t w[4][N];
+    // words 2 h, 2 h + 1 from the four rows of a sum's tile; or one of them
+    __device__ __forceinline__ void half(int h, const f32x4_t &x)
+    {
+        cut2(x[0], x[1], w[2 * h]);
+        cut2(x[2], x[3], w[2 * h + 1]);
+    }
+    __device__ __forceinline__ void word(int j, const f32x4_t &lo, const f32x4_t &hi)
+    {
+        const f32x4_t &x = j < 2 ? lo : hi;
+        cut2(x[2 * (j % 2)], x[2 * (j % 2) + 1], w[j]);
+    }
+    __device__ __forceinline__ uint4 piece(int i) const { return make_uint4(w[0][i], w[1][i], w[2][i], w[3][i]); }
+};
+// c += a b on their pieces (the products that are left out are below 2^-24)
+template <int NA, int NB>
+__device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const uint4 (&b)[NB])
+{
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (i + j < FULL)
+                c = mfma16x32<bf16_t>(a[i], b[j], c);
+}
+template <int NA, int NB>
+__device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const Pieces<NB> &b)
+{
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (i + j < FULL)
+                c = mfma16x32<bf16_t>(a[i], b.piece(j), c);
+}
+
+// Products and what else there is to do, in turns.  A wave issues in order: products in a row wait for each other, 16 cycles
+// each, while three other instructions fit between two of them.  So the steps of a phase alternate, the rest of a phase being work
+// for the next one, and stay as they are written.
+template <int N, typename F, typename G>
+__device__ __forceinline__ void weave(F &&products, G &&rest)
+{
+    static_for<N>([&](auto i) {
+        products(i);
+        rest(i);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+}
+// items of M that belong to step I of N
+template <int M, int N, int I, typename F>
+__device__ __forceinline__ void share(F &&f)
+{
+    constexpr int LO = M * I / N, HI = M * (I + 1) / N;
+    static_for<HI - LO>([&](auto j) { f(std::integral_constant<int, LO + j()>{}); });
+}
+__device__ __forceinline__ f32x4_t as_f32x4(const float4 &x) { return f32x4_t{x.x, x.y, x.z, x.w}; }
+
 template <typename T>
 __device__ __forceinline__ void cut_raw(const Raw8<T> &r, uint4 (&p)[PIECES<T>])
 {
@@ -190,18 +253,7 @@ __device__ __forceinline__ void cut_raw(const Raw8<T> &r, uint4 (&p)[PIECES<T>])
     }
 }
 
-// c += a b on their pieces (the products that are left out are below 2^-24)
-template <int NA, int NB>
-__device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const uint4 (&b)[NB])
-{
-#pragma unroll
-    for (int i = 0; i < NA; ++i)
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-            if (i + j < FULL)
-                c = mfma16x32<bf16_t>(a[i], b[j], c);
-}
-// The same for M x N sums, each product of pieces for all of them in turn: a sum is not added to again before the others were.
+// The same for M x N sums, each product of pieces for all of them in turn.
 // LIM: the pieces i and j with i + j < LIM; what is left out is below 2^-16 of a term with 2, which is for what nothing but a
 // result of 16 bits depends on.
 template <int LIM = FULL, int M, int N, int NA, int NB>
@@ -263,14 +315,8 @@ struct Buffer {
         return reinterpret_cast<void *>((uint64_t)hi << 32 | lo);
     }
     __device__ __forceinline__ uint4 load16(uint32_t at) const { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0)); }
-    __device__ __forceinline__ uint2 load8(uint32_t at) const { return __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, 0)); }
     __device__ __forceinline__ uint32_t load4(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0); }
     __device__ __forceinline__ uint16_t load2(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0); }
-    __device__ __forceinline__ void store8(uint32_t at, uint2 x) const
-    {
-        typedef uint32_t v2 __attribute__((ext_vector_type(2)));
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2, x), r, at, 0, 0);
-    }
     __device__ __forceinline__ void store4(uint32_t at, uint32_t x) const { __builtin_amdgcn_raw_buffer_store_b32(x, r, at, 0, 0); }
     __device__ __forceinline__ void store2(uint32_t at, uint16_t x) const { __builtin_amdgcn_raw_buffer_store_b16(x, r, at, 0, 0); }
 };
@@ -297,14 +343,11 @@ __device__ __forceinline__ Buffer head_rows(const T *p, int64_t stride, int n)
     return Buffer(p, n == 0 ? 0u : (uint32_t)(n - 1) * (uint32_t)(stride * sizeof(T)) + D * (uint32_t)sizeof(T));
 }
 // Here and no later: what the values come from has been waited for, and is not waited for behind the stores and loads that follow.
-template <int N>
-__device__ __forceinline__ void settled(f32x4_t (&x)[4][N])
+__device__ __forceinline__ void settled(f32x4_t (&x)[4])
 {
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-        for (int n = 0; n < N; ++n)
-            asm volatile("" : "+v"(x[rt][n]));
+        asm volatile("" : "+v"(x[rt]));
 }
 
 // A barrier of the workgroup that orders what it has in LDS and leaves loads and stores of memory in flight.
@@ -315,10 +358,10 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// NC adjacent columns of the wave's 64 rows 16 rt + 4 g + r of a token array (g = lane / 16), untouched bits
-template <typename T, int NC>
+// The lane's column of the wave's 64 rows 16 rt + 4 g + r of a token array (g = lane / 16), untouched bits
+template <typename T>
 struct Rows64 {
-    using Raw = std::conditional_t<sizeof(T) * NC == 8, uint2, std::conditional_t<sizeof(T) * NC == 4, uint32_t, uint16_t>>;
+    using Raw = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
     Raw x[4][4];
     // own: the lane's offset, that of its column in row 4 g
     __device__ __forceinline__ void load(const Buffer &b, uint32_t own, uint32_t stride_bytes)
@@ -326,42 +369,25 @@ struct Rows64 {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const uint32_t at = own + (16 * (i / 4) + i % 4) * stride_bytes;
-            if constexpr (sizeof(Raw) == 8)
-                x[i / 4][i % 4] = b.load8(at);
-            else if constexpr (sizeof(Raw) == 4)
+            if constexpr (sizeof(T) == 4)
                 x[i / 4][i % 4] = b.load4(at);
             else
                 x[i / 4][i % 4] = b.load2(at);
         }
     }
-    __device__ __forceinline__ float value(int rt, int r, int ct) const
-    {
-        if constexpr (NC == 1) {
-            return to_f32(__builtin_bit_cast(T, x[rt][r]));
-        } else if constexpr (sizeof(T) == 4) {
-            return __uint_as_float(ct ? x[rt][r].y : x[rt][r].x);
-        } else {
-            const float2 v = unpack_pair<T>(x[rt][r]);
-            return ct ? v.y : v.x;
-        }
-    }
+    __device__ __forceinline__ float value(int rt, int r) const { return to_f32(__builtin_bit_cast(T, x[rt][r])); }
 };
 // The same rows of a result
-template <typename T, int NC>
-__device__ __forceinline__ void put_rows(const Buffer &b, uint32_t own, uint32_t stride_bytes, float scale, const f32x4_t (&x)[4][NC])
+template <typename T>
+__device__ __forceinline__ void put_rows(const Buffer &b, uint32_t own, uint32_t stride_bytes, float scale, const f32x4_t (&x)[4])
 {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const int rt = i / 4, r = i % 4;
-        const uint32_t at = own + (16 * rt + r) * stride_bytes;
-        if constexpr (NC == 1 && sizeof(T) == 4)
-            b.store4(at, __float_as_uint(scale * x[rt][0][r]));
-        else if constexpr (NC == 1)
-            b.store2(at, from_f32<T>(scale * x[rt][0][r]).bits);
-        else if constexpr (sizeof(T) == 4)
-            b.store8(at, make_uint2(__float_as_uint(scale * x[rt][0][r]), __float_as_uint(scale * x[rt][NC - 1][r])));
+        const uint32_t at = own + (16 * (i / 4) + i % 4) * stride_bytes;
+        if constexpr (sizeof(T) == 4)
+            b.store4(at, __float_as_uint(scale * x[i / 4][i % 4]));
         else
-            b.store4(at, pack_pair<T>(scale * x[rt][0][r], scale * x[rt][NC - 1][r]));
+            b.store2(at, from_f32<T>(scale * x[i / 4][i % 4]).bits);
     }
 }
 
@@ -443,29 +469,6 @@ struct TokenTile {
     }
 };
 
-// S += (the tile's transpose, tokens 32 s ..) e, for a state's columns; a group of its row tiles at a time, as registers allow
-template <typename Tok, int KT, int NC>
-__device__ __forceinline__ void mma_columns(f32x4_t (&S)[KT][NC], const uint4 *img, int s, int lane, const uint4 (&e)[NC][FULL])
-{
-    constexpr int G = Tok::NP == 1 || KT < 4 ? KT : KT / 2;
-#pragma unroll
-    for (int t0 = 0; t0 < KT; t0 += G) {
-        uint4 f[G][Tok::NP];
-#pragma unroll
-        for (int t = 0; t < G; ++t)
-            Tok::columns(img, t0 + t, s, lane, f[t]);
-#pragma unroll
-        for (int i = 0; i < Tok::NP; ++i)
-#pragma unroll
-            for (int j = 0; i + j < FULL; ++j)
-#pragma unroll
-                for (int t = 0; t < G; ++t)
-#pragma unroll
-                    for (int n = 0; n < NC; ++n)
-                        S[t0 + t][n] = mfma16x32<bf16_t>(f[t][i], e[n][j], S[t0 + t][n]);
-    }
-}
-
 // Images of triangular matrices: tile (16 rows rt, 32 columns s) has number tile_of(rt, s); in LDS three pieces of it, 16 bytes a lane.
 template <bool UPPER>
 __host__ __device__ constexpr int tile_of(int rt, int s)
@@ -502,26 +505,18 @@ struct Words {
                 b.to_lds(to + (wave + NWV * i) * 1024, (wave + NWV * i) * 1024 + lane * 16);
     }
 };
-// c += (matrix) (b), of which b holds rows 32 s .. of the second operand; img: the matrix's image in LDS
-template <bool UPPER, int S, int NC, int NB>
-__device__ __forceinline__ void mma_triangle(f32x4_t (&c)[4][NC], const uint4 *img, int lane, const uint4 (&b)[NC][NB])
+// The tiles of such an image in an order in which those of rows 32 s .. follow each other: tile i is (tile_row, tile_step).
+template <bool UPPER>
+__host__ __device__ constexpr int tile_row(int i) { return UPPER ? (i < 2 ? i : i - 2) : (i < 4 ? i : i - 2); }
+template <bool UPPER>
+__host__ __device__ constexpr int tile_step(int i) { return UPPER ? i >= 2 : i >= 4; }
+// its pieces
+template <bool UPPER>
+__device__ __forceinline__ void load_tile(const uint4 *img, int i, int lane, uint4 (&a)[FULL])
 {
-    constexpr int FROM = !UPPER && S == 1 ? 2 : 0, TO = UPPER && S == 0 ? 2 : 4;
-    uint4 a[TO - FROM][FULL];
 #pragma unroll
-    for (int rt = FROM; rt < TO; ++rt)
-#pragma unroll
-        for (int j = 0; j < FULL; ++j)
-            a[rt - FROM][j] = img[j * SCAN_UNITS + tile_of<UPPER>(rt, S) * 64 + lane];
-#pragma unroll
-    for (int i = 0; i < FULL; ++i)
-#pragma unroll
-        for (int j = 0; j < NB && i + j < FULL; ++j)
-#pragma unroll
-            for (int rt = FROM; rt < TO; ++rt)
-#pragma unroll
-                for (int n = 0; n < NC; ++n)
-                    c[rt][n] = mfma16x32<bf16_t>(a[rt - FROM][i], b[n][j], c[rt][n]);
+    for (int j = 0; j < FULL; ++j)
+        a[j] = img[j * SCAN_UNITS + tile_of<UPPER>(tile_row<UPPER>(i), tile_step<UPPER>(i)) * 64 + lane];
 }
 
 // Threads that a kernel over the chunks is built for.  With DMA a wave needs less than 256 registers; built for 8 waves a workgroup, the

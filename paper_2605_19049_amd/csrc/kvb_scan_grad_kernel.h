@@ -21,12 +21,13 @@
 
 namespace kvb_impl {
 
-template <typename TIn, typename TOut, int D, int NC, int NWV>
+template <typename TIn, typename TOut, int D, int NWV>
 __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(const GradArgs ga)
 {
-    constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
+    constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NWV);
     using Tok = TokenTile<TIn, D, NWV>;
-    constexpr bool DMA = Tok::NP == 1;   // (as in kvb_scan_kernel)
+    constexpr int NP = Tok::NP;
+    constexpr bool DMA = NP == 1;   // (as in kvb_scan_kernel)
     constexpr int BUF = DMA ? 2 : 1;
     using Gates = Words<SCAN_GATES / 4, NWV>;
     using Mats = Words<2 * SCAN_MAT, NWV>;
@@ -39,38 +40,27 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     if (row < 0)
         return;
     const Span span = span_of(a.start, a.n_tokens, b);
-    const int chunks = (span.len + SC - 1) / SC, col = (part * NWV + wave) * 16 * NC + NC * m;
+    const int chunks = (span.len + SC - 1) / SC, col = (part * NWV + wave) * 16 + m;
     const size_t own = ((size_t)row * a.Hv + hv) * D * D;
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
 
-    f32x4_t S[KT][NC] = {};   // the gradient of the state
+    f32x4_t S[KT] = {};   // the gradient of the state
     auto state_at = [&](int t, int r) { return (uint32_t)(state_row_of(t, g, r) * D + col) * 4; };
     auto store_state = [&](float *p) {
         const Buffer to(p, 4 * D * D);
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if constexpr (NC == 2)
-                    to.store8(state_at(t, r), make_uint2(__float_as_uint(S[t][0][r]), __float_as_uint(S[t][NC - 1][r])));
-                else
-                    to.store4(state_at(t, r), __float_as_uint(S[t][0][r]));
-            }
+            for (int r = 0; r < 4; ++r)
+                to.store4(state_at(t, r), __float_as_uint(S[t][r]));
     };
     if (ga.dstate1) {
         const Buffer from(ga.dstate1 + own, 4 * D * D);
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                if constexpr (NC == 2) {
-                    const uint2 x = from.load8(state_at(t, r));
-                    S[t][0][r] = __uint_as_float(x.x);
-                    S[t][NC - 1][r] = __uint_as_float(x.y);
-                } else {
-                    S[t][0][r] = __uint_as_float(from.load4(state_at(t, r)));
-                }
-            }
+            for (int r = 0; r < 4; ++r)
+                S[t][r] = __uint_as_float(from.load4(state_at(t, r)));
     }
 
     const TIn *kp = static_cast<const TIn *>(a.k) + span.first * a.k_stride + hk * D;
@@ -85,9 +75,9 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     Tok knext, qnext;   // (without DMA)
     Mats mnext;
     Gates gnext;
-    Rows64<TOut, NC> onext;
-    Rows64<float, NC> znext;
-    Rows64<TIn, NC> vnext;
+    Rows64<TOut> onext;
+    Rows64<float> znext;
+    Rows64<TIn> vnext;
     auto request = [&](auto step, int c, int buf) {   // (in parts: kvb_scan_kernel)
         constexpr int PART = step();
         const int n = min(SC, span.len - c * SC);
@@ -106,20 +96,24 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
             mnext.load(images, wave, lane);
             gnext.load(gates, wave, lane);
         }
-        if constexpr (PART == KS - 1) {
-            onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), anew(oown), ost);
-            znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D);
-            vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
-        }
     };
-    f32x4_t y[4][NC];   // D of the chunk
-    auto put = [&](int c) {
-        put_rows<float, NC>(head_rows<float, D>(ga.dd + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D, 1.0f, y);
-    };
-    if (chunks > 0)
-        static_for<KS>([&](auto step) { request(step, chunks - 1, 0); });
-    for (int c = chunks - 1, buf = 0; c >= 0; --c, buf = DMA ? buf ^ 1 : 0) {
+    auto request_rows = [&](int c) {
         const int n = min(SC, span.len - c * SC);
+        onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), anew(oown), ost);
+        znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D);
+        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
+    };
+    if (chunks > 0) {
+        static_for<KS>([&](auto step) { request(step, chunks - 1, 0); });
+        request_rows(chunks - 1);
+    }
+    f32x4_t X[4] = {}, dn[4] = {};   // from a chunk's end on dV and D
+    auto put = [&](int c) {
+        const bool none = c >= chunks;
+        put_rows<TIn>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, none ? 0 : min(SC, span.len - c * SC)), anew(vown), vst, 1.0f, X);
+        put_rows<float>(head_rows<float, D>(ga.dd + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, none ? 0 : SC), anew(eown), 4 * D, 1.0f, dn);
+    };
+    for (int c = chunks - 1, buf = 0; c >= 0; --c, buf = DMA ? buf ^ 1 : 0) {
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = matss[buf];
         const float4 *gate = reinterpret_cast<const float4 *>(gatess[buf]);
         if constexpr (DMA) {
@@ -130,135 +124,136 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
             mnext.store(matss[0], wave, lane);
             gnext.store(gatess[0], wave, lane);
         }
-        f32x4_t dO[4][NC], E[4][NC], kd[4][NC], X[4][NC];
+        f32x4_t dO[4], E[4], kd[4] = {};
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    dO[rt][ct][r] = onext.value(rt, r, ct);
-                    E[rt][ct][r] = vnext.value(rt, r, ct) + znext.value(rt, r, ct);
-                    kd[rt][ct][r] = 0.0f;
-                    X[rt][ct][r] = 0.0f;
-                }
+            for (int r = 0; r < 4; ++r) {
+                dO[rt][r] = onext.value(rt, r);
+                E[rt][r] = vnext.value(rt, r) + znext.value(rt, r);
+            }
         settled(dO);
         settled(E);
         lds_barrier();
+        put(c + 1);   // (here for the reasons of kvb_scan_kernel)
         store_state(ga.ds + (own_chunk + (size_t)c * a.Hv) * D * D);
-        // kd = K dS
-        static_for<KS>([&](auto step) {
-            constexpr int ks = step();
-            request(step, max(c - 1, 0), buf ^ 1);
-            uint4 s[NC][FULL], f[4][PIECES<TIn>];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8];
-                pair8(S[2 * ks][ct], S[2 * ks + 1][ct], x);
-                cut8(x, s[ct]);
-            }
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt)
-                Tok::rows(kimg, rt, ks, lane, f[rt]);
-            mma(kd, f, s);
-        });
-        // X = scale P' dO + rest kd
-        static_for<2>([&](auto step) {
-            constexpr int s = step();
-            uint4 p[NC][PIECES<TOut>];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8];
-                pair8(dO[2 * s][ct], dO[2 * s + 1][ct], x);
-                cut8(x, p[ct]);
-            }
-            mma_triangle<true, s>(X, mats + SCAN_MAT, lane, p);
-        });
-        // D' = scale P' dO + M' beta X, kd = rest kd + scale q.k dO, X = scale P' dO + kd; outer: of E rest kd
-        float bt[4][4], inner[16], outer[16];
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            const float4 re = gate[16 + 4 * rt + g], be = gate[32 + 4 * rt + g], di = gate[48 + 4 * rt + g];
-            const float rs[4] = {re.x, re.y, re.z, re.w}, dg[4] = {di.x, di.y, di.z, di.w}, bs[4] = {be.x, be.y, be.z, be.w};
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                bt[rt][r] = bs[r];
-                float on = 0.0f;
-#pragma unroll
-                for (int ct = 0; ct < NC; ++ct) {
-                    const float back = rs[r] * kd[rt][ct][r];
-                    on = fmaf(E[rt][ct][r], back, on);
-                    kd[rt][ct][r] = fmaf(a.scale * dg[r], dO[rt][ct][r], back);
-                    y[rt][ct][r] = a.scale * X[rt][ct][r];
-                    X[rt][ct][r] = y[rt][ct][r] + kd[rt][ct][r];
-                }
-                outer[4 * rt + r] = on;
-            }
-        }
-        float *sums = ga.part + (own_chunk + (size_t)c * a.Hv) * GRAD_PARTS + (part * NWV + wave) * 2 * SC + 16 * (m / 4) + 4 * g + m % 4;
-        sums[SC] = sum_rows16(outer, m);
-        static_for<2>([&](auto step) {
-            constexpr int s = step();
-            uint4 p[NC][FULL];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8];
-                pair8(X[2 * s][ct], X[2 * s + 1][ct], x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    x[j] *= bt[2 * s + j / 4][j % 4];
-                cut8(x, p[ct]);
-            }
-            mma_triangle<true, s>(y, mats, lane, p);
-        });
-        // the tokens' sums of E D' over the wave's columns, and D
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
+            X[rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        // kd = K dS; the pieces of dS
+        Pieces<FULL> sp[KS], oq[2], xp[2], zp[2];
+        Pieces<PIECES<TOut>> od[2];
+        uint4 fr[2][4][NP], ft[2][NP], fm[2][FULL];
+        auto gate_at = [&](int which, int rt) { return as_f32x4(gate[16 * which + 4 * rt + g]); };
+        auto rows = [&](int ks) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float in = 0.0f;
+            for (int rt = 0; rt < 4; ++rt)
+                Tok::rows(kimg, rt, ks, lane, fr[ks % 2][rt]);
+        };
+        rows(0);
 #pragma unroll
-                for (int ct = 0; ct < NC; ++ct) {
-                    in = fmaf(E[rt][ct][r], y[rt][ct][r], in);
-                    y[rt][ct][r] += kd[rt][ct][r];
-                }
-                inner[4 * rt + r] = in;
-            }
-        sums[0] = sum_rows16(inner, m);
-        // dS = exp(c_last) dS + Q' scale gamma dO - K' gamma beta D
+        for (int j = 0; j < 4; ++j)
+            sp[0].word(j, S[0], S[1]);
+        weave<4 * KS>([&](auto i) { mma(kd[i() % 4], fr[i() / 4 % 2][i() % 4], sp[i() / 4]); },
+                      [&](auto i) {
+                          constexpr int ks = i() / 4, rt = i() % 4;
+                          if constexpr (ks + 1 < KS) {
+                              sp[ks + 1].word(rt, S[2 * ks + 2], S[2 * ks + 3]);
+                              if constexpr (rt == 0)
+                                  rows(ks + 1);
+                          } else {
+                              od[rt / 2].half(rt % 2, dO[rt]);
+                              if constexpr (rt == 3)
+                                  load_tile<true>(mats + SCAN_MAT, 0, lane, fm[0]);
+                          }
+                          if constexpr (rt == 3)
+                              request(std::integral_constant<int, ks>{}, max(c - 1, 0), buf ^ 1);
+                      });
+        // X = P' dO (without P's diagonal); dS decays, the pieces of scale gamma dO
         const float last = reinterpret_cast<const float *>(gate)[SC - 1];
+        weave<SCAN_TILES>([&](auto i) { mma(X[tile_row<true>(i())], fm[i() % 2], od[tile_step<true>(i())]); },
+                          [&](auto i) {
+                              if constexpr (i() + 1 < SCAN_TILES)
+                                  load_tile<true>(mats + SCAN_MAT, i() + 1, lane, fm[(i() + 1) % 2]);
+                              else
+                                  Tok::columns(qimg, 0, 0, lane, ft[0]);
+                              if constexpr (i() < 4)
+                                  oq[i() / 2].half(i() % 2, a.scale * gate_at(0, i()) * dO[i()]);
+                              else
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
+                                  for (int t = (i() - 4) * KT / 2; t < (i() - 3) * KT / 2; ++t)
+                                      S[t] *= last;
+                          });
+        // dS += Q' scale gamma dO; kd = rest kd + scale q.k dO, dn = scale P' dO, the pieces of beta X, X = dn + kd; E rest kd
+        float inner[16], outer[16];
+        auto join = [&](auto i) {
+            constexpr int rt = i() / 3;
+            if constexpr (i() % 3 == 0) {
+                const f32x4_t back = gate_at(1, rt) * kd[rt], own_share = a.scale * gate_at(3, rt);
+                kd[rt] = own_share * dO[rt] + back;
+                dn[rt] = a.scale * X[rt];
+                X[rt] = gate_at(2, rt) * (dn[rt] + kd[rt]);
 #pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-                S[t][ct] *= last;
-        f32x4_t dv[4][NC];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            uint4 o[NC][FULL], d[NC][FULL];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8], z[8];
-                pair8(dO[2 * s][ct], dO[2 * s + 1][ct], x);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int rt = 2 * s + j / 4;
-                    const float gm = reinterpret_cast<const float *>(gate)[16 * rt + 4 * g + j % 4];
-                    dv[rt][ct][j % 4] = bt[rt][j % 4] * y[rt][ct][j % 4];
-                    x[j] *= a.scale * gm;
-                    z[j] = -gm * dv[rt][ct][j % 4];
-                }
-                cut8(x, o[ct]);
-                cut8(z, d[ct]);
+                for (int r = 0; r < 4; ++r)
+                    outer[4 * rt + r] = E[rt][r] * back[r];
+            } else {
+                xp[rt / 2].word(2 * (rt % 2) + i() % 3 - 1, X[rt], X[rt]);
             }
-            mma_columns<Tok>(S, qimg, s, lane, o);
-            mma_columns<Tok>(S, kimg, s, lane, d);
-        }
-        put_rows<TIn, NC>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst, 1.0f, dv);
-        put(c);
+        };
+        weave<2 * KT>([&](auto i) { mma(S[i() % KT], ft[i() % 2], oq[i() / KT]); },
+                      [&](auto i) {
+                          if constexpr (i() + 1 < 2 * KT)
+                              Tok::columns(qimg, (i() + 1) % KT, (i() + 1) / KT, lane, ft[(i() + 1) % 2]);
+                          else
+                              load_tile<true>(mats, 0, lane, fm[0]);
+                          share<12, 2 * KT, i()>(join);
+                      });
+        // dn += M' beta X: what D has that decays.  Then the tokens' sums of E dn and E rest kd over the wave's columns, D = dn + kd,
+        // dV = beta D, and the pieces of -gamma dV
+        request_rows(max(c - 1, 0));
+        float *sums = ga.part + (own_chunk + (size_t)c * a.Hv) * GRAD_PARTS + (part * NWV + wave) * 2 * SC + 16 * (m / 4) + 4 * g + m % 4;
+        auto end = [&](auto s, auto i) {
+            constexpr int lo = 2 * s();
+            if constexpr (i() == 0) {
+#pragma unroll
+                for (int rt = lo; rt < lo + 2; ++rt) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        inner[4 * rt + r] = E[rt][r] * dn[rt][r];
+                    dn[rt] += kd[rt];
+                    X[rt] = gate_at(2, rt) * dn[rt];
+                    kd[rt] = -gate_at(0, rt) * X[rt];
+                }
+            } else {
+                zp[s()].word(i() - 1, kd[lo], kd[lo + 1]);
+            }
+        };
+        weave<SCAN_TILES>([&](auto i) { mma(dn[tile_row<true>(i())], fm[i() % 2], xp[tile_step<true>(i())]); },
+                          [&](auto i) {
+                              if constexpr (i() + 1 < SCAN_TILES)
+                                  load_tile<true>(mats, i() + 1, lane, fm[(i() + 1) % 2]);
+                              else
+                                  Tok::columns(kimg, 0, 0, lane, ft[0]);
+                              if constexpr (i() == 1)
+                                  sums[SC] = sum_rows16(outer, m);
+                              if constexpr (i() >= 4)
+                                  share<5, 2, i() - 4>([&](auto j) { end(std::integral_constant<int, 0>{}, j); });
+                          });
+        // dS -= K' gamma dV
+        weave<2 * KT>([&](auto i) { mma(S[i() % KT], ft[i() % 2], zp[i() / KT]); },
+                      [&](auto i) {
+                          if constexpr (i() + 1 < 2 * KT)
+                              Tok::columns(kimg, (i() + 1) % KT, (i() + 1) / KT, lane, ft[(i() + 1) % 2]);
+                          if constexpr (i() < KT)
+                              share<5, KT, i()>([&](auto j) { end(std::integral_constant<int, 1>{}, j); });
+                          else if constexpr (i() == KT)
+                              sums[0] = sum_rows16(inner, m);
+                      });
         if constexpr (!DMA)
             lds_barrier();
     }
+    if (chunks > 0)
+        put(0);
     if (ga.dstate0)
         store_state(ga.dstate0 + own);
 }
@@ -268,7 +263,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
 // the tokens' rows (dO, E, dV) as second, from LDS.  The two 64 x 64 matrices are worked out a tile column a
 // wave, transposed; their sums' registers, two tiles together, are a second operand for W K, and read back transposed one for W' Q.
 // Products that only dK depends on keep 2^-16 of a term for 16-bit dK; dQ is needed to fp32 for dg.
-template <typename TIn, typename TOut, int D, int NC>   // (NC: of kvb_scan_reverse_kernel)
+template <typename TIn, typename TOut, int D>
 __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs ga)
 {
     constexpr int NWV = D / 32, KS = D / 32, NP = PIECES<TIn>, NO = PIECES<TOut>, LK = sizeof(TIn) == 2 ? 2 : FULL, ITS = 4 / NWV;
@@ -593,7 +588,7 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
             }
             const float *parts = ga.part + unit * GRAD_PARTS + lane;
 #pragma unroll
-            for (int v = 0; v < D / (16 * NC); ++v) {
+            for (int v = 0; v < D / 16; ++v) {
                 in += parts[v * 2 * SC];
                 on += parts[v * 2 * SC + SC];
             }
@@ -635,11 +630,11 @@ void launch_scan_grad_sized(const GradArgs &a, hipStream_t stream)
         launch_part(kvb_scan_prep_kernel<TIn, D, true>, true, false, chunks * a.f.Hv, 256, stream, a.f);
     scan_split<TIn, D>(a.f, [&]<int NWV>(int64_t blocks) {
         if (a.f.n_tokens > 0)
-            launch_part(kvb_scan_kernel<TIn, float, D, 1, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
-        launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, 1, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, blocks, 64 * NWV, stream, a);
+            launch_part(kvb_scan_kernel<TIn, float, D, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
+        launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, blocks, 64 * NWV, stream, a);
     });
     if (a.f.n_tokens > 0)
-        launch_part(kvb_scan_grad_kernel<TIn, TOut, D, 1>, false, true, chunks * a.f.Hk, 2 * D, stream, a);
+        launch_part(kvb_scan_grad_kernel<TIn, TOut, D>, false, true, chunks * a.f.Hk, 2 * D, stream, a);
 }
 template <typename TIn, typename TOut>
 void launch_scan_grad_typed(int d, const GradArgs &a, hipStream_t stream)

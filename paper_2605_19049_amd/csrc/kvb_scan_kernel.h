@@ -182,18 +182,19 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
     }
 }
 
-// The state from chunk to chunk: a workgroup has NWV waves of 16 NC columns each of one (sequence, v-head).
+// The state from chunk to chunk: a workgroup has NWV waves of 16 columns each of one (sequence, v-head).
 // A wave keeps its columns of the state in its sums' registers for the whole sequence; the chunk's
-// K S and Q S, E and the state's update follow from each other within the wave (paired order).  Lane l % 16 = n has the columns
-// NC n .. NC n + NC - 1 of the wave's.  What the next chunk needs from memory is requested a chunk ahead.
+// K S and Q S, E and the state's update follow from each other within the wave.  What the next chunk needs from memory is
+// requested a chunk ahead.
 // STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
 // than the decays, which a difference of E and V would lose).
-template <typename TIn, typename TOut, int D, int NC, int NWV, bool STATES>
+template <typename TIn, typename TOut, int D, int NWV, bool STATES>
 __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const ScanArgs a)
 {
-    constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NC * NWV);
+    constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NWV);
     using Tok = TokenTile<TIn, D, NWV>;
-    constexpr bool DMA = Tok::NP == 1;   // keys and queries are operands as they come: all images go to LDS without passing registers, into
+    constexpr int NP = Tok::NP;
+    constexpr bool DMA = NP == 1;   // keys and queries are operands as they come: all images go to LDS without passing registers, into
     constexpr int BUF = DMA ? 2 : 1;     // one buffer while the other is in use
     constexpr int WORDS = SCAN_GATES / 4 + (STATES ? 1 : 2) * SCAN_MAT, PREP = STATES ? GRAD_PREP : SCAN_PREP;
     using Prep = Words<WORDS, NWV>;
@@ -205,25 +206,16 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     if (row < 0)
         return;
     const Span span = span_of(a.start, a.n_tokens, b);
-    const int chunks = (span.len + SC - 1) / SC, col = (part * NWV + wave) * 16 * NC + NC * m;
+    const int chunks = (span.len + SC - 1) / SC, col = (part * NWV + wave) * 16 + m;
     const size_t own = ((size_t)row * a.Hv + hv) * D * D + col;
 
-    f32x4_t S[KT][NC] = {};
-    if (a.state0) {
+    f32x4_t S[KT] = {};
+    if (a.state0)
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float *from = a.state0 + own + state_row_of(t, g, r) * D;
-                if constexpr (NC == 2) {
-                    const float2 x = *reinterpret_cast<const float2 *>(from);
-                    S[t][0][r] = x.x;
-                    S[t][1][r] = x.y;
-                } else {
-                    S[t][0][r] = *from;
-                }
-            }
-    }
+            for (int r = 0; r < 4; ++r)
+                S[t][r] = a.state0[own + state_row_of(t, g, r) * D];
 
     const TIn *kp = static_cast<const TIn *>(a.k) + span.first * a.k_stride + hk * D;
     const TIn *qp = static_cast<const TIn *>(a.q) + span.first * a.q_stride + hk * D;
@@ -236,7 +228,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     const uint32_t kat = lds_at(kimgs[0]), qat = lds_at(qimgs[0]), pat = lds_at(preps[0]);
     Tok knext, qnext;   // (without DMA)
     Prep pnext;
-    Rows64<TIn, NC> vnext;
+    Rows64<TIn> vnext;
     // What chunk c needs, asked for in KS parts, one for each step of the products with the state: at once, the requests would
     // wait for each other at the memory unit and the wave with them.
     auto request = [&](auto step, int c, int buf) {
@@ -259,15 +251,15 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         if constexpr (PART == KS - 1)
             vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
     };
-    f32x4_t O[4][NC] = {};
+    f32x4_t O[4] = {};
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
     auto put = [&](int c) {   // (STATES: O holds Z)
         if constexpr (STATES) {
-            put_rows<float, NC>(head_rows<float, D>(a.z + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, c < 0 ? 0 : SC), (4 * g * D + col) * 4, 4 * D, 1.0f, O);
+            put_rows<float>(head_rows<float, D>(a.z + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, c < 0 ? 0 : SC), (4 * g * D + col) * 4, 4 * D, 1.0f, O);
             return;
         }
         TOut *p = static_cast<TOut *>(a.out) + ((int64_t)(span.first + c * SC) * a.Hv + hv) * D;
-        put_rows<TOut, NC>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), anew(oown), ost, a.scale, O);
+        put_rows<TOut>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), anew(oown), ost, a.scale, O);
     };
     if (chunks > 0)
         static_for<KS>([&](auto step) { request(step, 0, 0); });
@@ -283,16 +275,12 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                 qnext.store(qimgs[0], wave, lane);
             pnext.store(preps[0], wave, lane);
         }
-        f32x4_t E[4][NC], y[4][NC];
+        f32x4_t E[4], y[4] = {};
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    E[rt][ct][r] = vnext.value(rt, r, ct);
-                    y[rt][ct][r] = 0.0f;
-                }
+            for (int r = 0; r < 4; ++r)
+                E[rt][r] = vnext.value(rt, r);
         settled(E);
         lds_barrier();
         // The outputs of the chunk before leave here: what a wave waits for at the chunk's end is then not a store just made.  (Nothing
@@ -300,118 +288,137 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         put(c - 1);
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-                O[rt][ct] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+            O[rt] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (STATES) {
             const Buffer to(a.s0 + (own_chunk + (size_t)c * a.Hv) * D * D, 4 * D * D);
 #pragma unroll
             for (int t = 0; t < KT; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t at = (state_row_of(t, g, r) * D + col) * 4;
-                    if constexpr (NC == 2)
-                        to.store8(at, make_uint2(__float_as_uint(S[t][0][r]), __float_as_uint(S[t][NC - 1][r])));
-                    else
-                        to.store4(at, __float_as_uint(S[t][0][r]));
-                }
+                for (int r = 0; r < 4; ++r)
+                    to.store4((state_row_of(t, g, r) * D + col) * 4, __float_as_uint(S[t][r]));
         }
-        // y = K S, O = Q S
-        static_for<KS>([&](auto step) {
-            constexpr int ks = step();
-            request(step, min(c + 1, chunks - 1), buf ^ 1);
-            uint4 s[NC][FULL];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8];
-                pair8(S[2 * ks][ct], S[2 * ks + 1][ct], x);
-                cut8(x, s[ct]);
-            }
-            uint4 fk[4][PIECES<TIn>], fq[4][PIECES<TIn>];
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                Tok::rows(kimg, rt, ks, lane, fk[rt]);
-                if constexpr (!STATES)
-                    Tok::rows(qimg, rt, ks, lane, fq[rt]);
-            }
-            mma(y, fk, s);
-            if constexpr (!STATES)
-                mma(O, fq, s);
-        });
-        // Y = V - gamma y, y = beta Y, E = Y + M y
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            const float4 ga = gate[4 * rt + g], be = gate[32 + 4 * rt + g];
-            const float gm[4] = {ga.x, ga.y, ga.z, ga.w}, bt[4] = {be.x, be.y, be.z, be.w};
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if constexpr (STATES) {
-                        O[rt][ct][r] = -gm[r] * y[rt][ct][r];
-                        y[rt][ct][r] = bt[r] * (E[rt][ct][r] + O[rt][ct][r]);
-                    } else {
-                        E[rt][ct][r] = fmaf(-gm[r], y[rt][ct][r], E[rt][ct][r]);
-                        O[rt][ct][r] *= gm[r];
-                        y[rt][ct][r] = bt[r] * E[rt][ct][r];
-                    }
-                }
-        }
-        static_for<2>([&](auto step) {
-            constexpr int s = step();
-            uint4 p[NC][FULL];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8];
-                pair8(y[2 * s][ct], y[2 * s + 1][ct], x);
-                cut8(x, p[ct]);
-            }
-            mma_triangle<false, s>(STATES ? O : E, mats, lane, p);
-        });
-        if constexpr (STATES) {
+        // y = K S; the state's pieces
+        Pieces<FULL> sp[KS], yp[2], up[2], ep[2];
+        uint4 fr[2][4][NP], ft[2][NP], fm[2][FULL];
+        f32x4_t gm[4], bt[4], re[4];
+        auto rows = [&](const uint4 *img, int ks, uint4 (&f)[4][NP]) {
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt)
+                Tok::rows(img, rt, ks, lane, f[rt]);
+        };
+        rows(kimg, 0, fr[0]);
 #pragma unroll
-                for (int ct = 0; ct < NC; ++ct)
-                    E[rt][ct] += O[rt][ct];
-        }
-        // O += P beta E, S = exp(c_last) S + K' rest beta E
+        for (int j = 0; j < 4; ++j)
+            sp[0].word(j, S[0], S[1]);
+        weave<4 * KS>([&](auto i) { mma(y[i() % 4], fr[i() / 4 % 2][i() % 4], sp[i() / 4]); },
+                      [&](auto i) {
+                          constexpr int ks = i() / 4, rt = i() % 4;
+                          if constexpr (ks + 1 < KS)
+                              sp[ks + 1].word(rt, S[2 * ks + 2], S[2 * ks + 3]);
+                          if constexpr (rt == 0 && ks + 1 < KS)
+                              rows(kimg, ks + 1, fr[(ks + 1) % 2]);
+                          if constexpr (rt == 0 && ks + 1 == KS && !STATES)
+                              rows(qimg, 0, fr[KS % 2]);
+                          if constexpr (ks + 1 == KS) {
+                              gm[rt] = as_f32x4(gate[4 * rt + g]);
+                              bt[rt] = as_f32x4(gate[32 + 4 * rt + g]);
+                          }
+                          if constexpr (rt == 3)
+                              request(std::integral_constant<int, ks>{}, min(c + 1, chunks - 1), buf ^ 1);
+                      });
+        // O = Q S; Y = V - gamma y, the pieces of beta Y
+        auto residual = [&](auto i) {
+            constexpr int rt = i() / 3;
+            if constexpr (i() % 3 == 0) {
+                if constexpr (STATES) {
+                    O[rt] = -gm[rt] * y[rt];
+                    y[rt] = bt[rt] * (E[rt] + O[rt]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        E[rt][r] = fmaf(-gm[rt][r], y[rt][r], E[rt][r]);
+                    y[rt] = bt[rt] * E[rt];
+                }
+            } else {
+                yp[rt / 2].word(2 * (rt % 2) + i() % 3 - 1, y[rt], y[rt]);
+            }
+        };
+        if constexpr (STATES)
+            static_for<12>(residual);
+        else
+            weave<4 * KS>([&](auto i) { mma(O[i() % 4], fr[(KS + i() / 4) % 2][i() % 4], sp[i() / 4]); },
+                          [&](auto i) {
+                              constexpr int ks = i() / 4, rt = i() % 4;
+                              if constexpr (rt == 0 && ks + 1 < KS)
+                                  rows(qimg, ks + 1, fr[(KS + ks + 1) % 2]);
+                              share<12, 4 * KS, i()>(residual);
+                          });
+        // E = Y + M beta Y (STATES: Z); the state and O decay, and the pieces of beta E and rest beta E of the first 32 tokens
         const float last = reinterpret_cast<const float *>(gate)[SC - 1];
+        f32x4_t(&sum)[4] = STATES ? O : E;
+        // item i of two tiles' ten: beta E, its words, rest beta E, its words
+        auto weigh = [&](auto s, auto i) {
+            constexpr int lo = 2 * s(), hi = lo + 1;
+            if constexpr (i() == 0) {
+                if constexpr (STATES) {
+                    E[lo] += O[lo];
+                    E[hi] += O[hi];
+                }
+                y[lo] = bt[lo] * E[lo];
+                y[hi] = bt[hi] * E[hi];
+            } else if constexpr (i() < 5) {
+                if constexpr (!STATES)
+                    up[s()].word(i() - 1, y[lo], y[hi]);
+            } else if constexpr (i() == 5) {
+                y[lo] *= re[lo];
+                y[hi] *= re[hi];
+            } else {
+                ep[s()].word(i() - 6, y[lo], y[hi]);
+            }
+        };
+        load_tile<false>(mats, 0, lane, fm[0]);
+        weave<SCAN_TILES>([&](auto i) { mma(sum[tile_row<false>(i())], fm[i() % 2], yp[tile_step<false>(i())]); },
+                          [&](auto i) {
+                              if constexpr (i() + 1 < SCAN_TILES)
+                                  load_tile<false>(mats, i() + 1, lane, fm[(i() + 1) % 2]);
+                              if constexpr (i() < 2) {
+                                  re[2 * i()] = as_f32x4(gate[16 + 8 * i() + g]);
+                                  re[2 * i() + 1] = as_f32x4(gate[16 + 8 * i() + 4 + g]);
+                                  if constexpr (!STATES) {
+                                      O[2 * i()] *= gm[2 * i()];
+                                      O[2 * i() + 1] *= gm[2 * i() + 1];
+                                  }
+                              } else if constexpr (i() < 4) {
+                                  share<10, 2, i() - 2>([&](auto j) { weigh(std::integral_constant<int, 0>{}, j); });
+                              } else {
 #pragma unroll
-        for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
-                S[t][ct] *= last;
+                                  for (int t = (i() - 4) * KT / 2; t < (i() - 3) * KT / 2; ++t)
+                                      S[t] *= last;
+                              }
+                              if constexpr (i() + 1 == SCAN_TILES)
+                                  Tok::columns(kimg, 0, 0, lane, ft[0]);
+                          });
+        // S += K' rest beta E, O += P beta E, 32 tokens and then the others, whose pieces are made on the way
         static_for<2>([&](auto step) {
             constexpr int s = step();
-            uint4 p[NC][FULL], e[NC][FULL];
-#pragma unroll
-            for (int ct = 0; ct < NC; ++ct) {
-                float x[8];
-                pair8(E[2 * s][ct], E[2 * s + 1][ct], x);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 be = gate[32 + 8 * s + 4 * h + g];
-                    x[4 * h] *= be.x;
-                    x[4 * h + 1] *= be.y;
-                    x[4 * h + 2] *= be.z;
-                    x[4 * h + 3] *= be.w;
-                }
-                if constexpr (!STATES)
-                    cut8(x, p[ct]);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 re = gate[16 + 8 * s + 4 * h + g];
-                    x[4 * h] *= re.x;
-                    x[4 * h + 1] *= re.y;
-                    x[4 * h + 2] *= re.z;
-                    x[4 * h + 3] *= re.w;
-                }
-                cut8(x, e[ct]);
-            }
-            mma_columns<Tok>(S, kimg, s, lane, e);
+            weave<KT>([&](auto t) { mma(S[t()], ft[t() % 2], ep[s]); },
+                      [&](auto t) {
+                          if constexpr (t() + 1 < KT)
+                              Tok::columns(kimg, t() + 1, s, lane, ft[(t() + 1) % 2]);
+                          else if constexpr (s == 0)
+                              Tok::columns(kimg, 0, 1, lane, ft[KT % 2]);
+                          if constexpr (t() + 1 == KT && !STATES)
+                              load_tile<false>(mats + SCAN_MAT, 4 * s, lane, fm[0]);
+                          if constexpr (s == 0)
+                              share<10, KT, t()>([&](auto j) { weigh(std::integral_constant<int, 1>{}, j); });
+                      });
+            static_assert(KT % 2 == 0);
             if constexpr (!STATES)
-                mma_triangle<false, s>(O, mats + SCAN_MAT, lane, p);
+                weave<4 - 2 * s>([&](auto i) { mma(O[2 * s + i()], fm[i() % 2], up[s]); },
+                                 [&](auto i) {
+                                     if constexpr (i() + 1 < 4 - 2 * s)
+                                         load_tile<false>(mats + SCAN_MAT, 4 * s + i() + 1, lane, fm[(i() + 1) % 2]);
+                                 });
         });
         if constexpr (!DMA)
             lds_barrier();
@@ -422,13 +429,8 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float *to = a.state1 + own + state_row_of(t, g, r) * D;
-                if constexpr (NC == 2)
-                    *reinterpret_cast<float2 *>(to) = make_float2(S[t][0][r], S[t][1][r]);
-                else
-                    *to = S[t][0][r];
-            }
+            for (int r = 0; r < 4; ++r)
+                a.state1[own + state_row_of(t, g, r) * D] = S[t][r];
 }
 
 template <typename TIn, typename TOut, int D>
@@ -437,7 +439,7 @@ void launch_scan_sized(const ScanArgs &a, hipStream_t stream)
     if (a.n_tokens > 0)
         launch_part(kvb_scan_prep_kernel<TIn, D, false>, true, false, scan_chunks(a.n_tokens, a.B) * a.Hv, 256, stream, a);
     scan_split<TIn, D>(a, [&]<int NWV>(int64_t blocks) {
-        launch_part(kvb_scan_kernel<TIn, TOut, D, 1, NWV, false>, a.n_tokens == 0, true, blocks, 64 * NWV, stream, a);
+        launch_part(kvb_scan_kernel<TIn, TOut, D, NWV, false>, a.n_tokens == 0, true, blocks, 64 * NWV, stream, a);
     });
 }
 template <typename TIn, typename TOut>
