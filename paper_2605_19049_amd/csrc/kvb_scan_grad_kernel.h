@@ -270,14 +270,15 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
     constexpr int ROWS = 4 * KS * 64;   // 16-byte words of a piece of 64 rows of D
     constexpr int ONE = (NO + FULL + LK) * ROWS, W = 512, TWO = (FULL + LK) * W + 2 * NP * ROWS;
     using Tok = TokenTile<TIn, D, NWV>;
-    // (d = 32: the matrices beside the rows, for its one wave has four tile columns to get rid of)
-    constexpr bool APART = D == 32;
+    // (d < 128: the matrices beside the rows, for the few waves have several tile columns to get rid of)
+    constexpr bool APART = D < 128;
+    constexpr int BESIDE = ONE > 2 * NP * ROWS ? ONE : 2 * NP * ROWS;
     constexpr int UNROLL = NP == FULL ? 1 : KS;   // (registers)
-    __shared__ uint4 lds[APART ? ONE + TWO : ONE > TWO ? ONE : TWO];
-    __shared__ float sums[3][4][SC], square[4];   // the tokens' dO'.E, Z.dV and Q.dQ', and <dS1, S0>, by waves
+    __shared__ uint4 lds[APART ? BESIDE + (FULL + LK) * W : ONE > TWO ? ONE : TWO];
+    __shared__ float sums[5][4][SC], square[4];   // the tokens' dO'.E, Z.dV and Q.dQ', E.D' and E.(rest K dS1), and <dS1, S0>, by waves
     __shared__ double cs[SC];
     uint4 *oimg = lds, *eimg = oimg + NO * ROWS, *vimg = eimg + FULL * ROWS;
-    uint4 *w1 = lds + (APART ? ONE : 0), *w2 = w1 + FULL * W, *kimg = w2 + LK * W, *qimg = kimg + NP * ROWS;
+    uint4 *w1 = lds + (APART ? BESIDE : 0), *w2 = w1 + FULL * W, *kimg = APART ? lds : w2 + LK * W, *qimg = kimg + NP * ROWS;
     const ScanArgs &a = ga.f;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int w = blockIdx.x / a.Hk, hk = blockIdx.x - w * a.Hk;
@@ -288,42 +289,70 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
     const Buffer kb = head_rows<TIn, D>(static_cast<const TIn *>(a.k) + at.first * a.k_stride + hk * D, a.k_stride, at.n);
     const Buffer qb = head_rows<TIn, D>(static_cast<const TIn *>(a.q) + at.first * a.q_stride + hk * D, a.q_stride, at.n);
     Tok kt, qt;
-    if constexpr (NP == 1) {   // (several pieces: no registers to hold them in)
-        kt.load(kb, kst, wave, lane);
-        qt.load(qb, qst, wave, lane);
-    }
     f32x4_t dq[2][4] = {}, dk[2][4] = {};
     const int mine = 32 * wave + 8 * g;   // the lane's first column: of the rows it stages and of what it stores
+    // What the next v-head's start needs from memory is asked for while this one's products with matrices run (bf16: with more
+    // pieces there are no registers for it), and its states a step ahead (fp32: when they are needed).
+    constexpr bool AHEAD = NP == 1 && NO == 1;
+    Raw8<TIn> v[4];
+    Raw8<TOut> o[4];
+    Raw8<float> z[4], d[4], sraw[2][2], draw[2][2];
+    float gamma[4], rest[4], beta[4], g1, parts[2][(D / 16 + NWV - 1) / NWV];   // (gamma .. of token 16 nt + m)
+    auto load_head = [&](int h) {
+        const int hv = hk * a.r + h;
+        const size_t unit = (size_t)w * a.Hv + hv;
+        const Buffer vb = head_rows<TIn, D>(static_cast<const TIn *>(a.v) + at.first * a.v_stride + hv * D, a.v_stride, at.n);
+        const Buffer ob = head_rows<TOut, D>(static_cast<const TOut *>(ga.dout) + ((size_t)at.first * a.Hv + hv) * D, (int64_t)a.Hv * D, at.n);
+        const Buffer zb(a.z + unit * SC * D, 4 * SC * D), db(ga.dd + unit * SC * D, 4 * SC * D), gb(a.prep + unit * GRAD_PREP, 4 * SCAN_GATES);
+        const Buffer pb(ga.part + unit * GRAD_PARTS, 4 * GRAD_PARTS);
+        g1 = a.g[(size_t)(at.first + min(lane, at.n - 1)) * a.Hv + hv];
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+            const int i = 16 * rt + m;
+            gamma[rt] = __uint_as_float(gb.load4(4 * i));
+            rest[rt] = __uint_as_float(gb.load4(4 * (SC + i)));
+            beta[rt] = __uint_as_float(gb.load4(4 * (2 * SC + i)));
+            z[rt] = load_raw8<float>(zb, (i * D + mine) * 4);
+            d[rt] = load_raw8<float>(db, (i * D + mine) * 4);
+            v[rt] = load_raw8<TIn>(vb, i * vst + mine * (uint32_t)sizeof(TIn));
+            o[rt] = load_raw8<TOut>(ob, i * ost + mine * (uint32_t)sizeof(TOut));
+        }
+#pragma unroll
+        for (int i = 0; i < (D / 16 + NWV - 1) / NWV; ++i)   // (D / 16 is a multiple of NWV)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                parts[j][i] = __uint_as_float(pb.load4(4 * (((wave + NWV * i) * 2 + j) * SC + lane)));
+    };
+    auto load_states = [&](size_t unit, int ks, int to) {
+        const Buffer sb(a.s0 + unit * D * D, 4 * D * D), dsb(ga.ds + unit * D * D, 4 * D * D);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t from = (state_row_of(2 * wave + t, m / 4, m % 4) * D + 32 * ks + 8 * g) * 4;
+            sraw[to][t] = load_raw8<float>(sb, from);
+            draw[to][t] = load_raw8<float>(dsb, from);
+        }
+    };
+    if constexpr (AHEAD)
+        load_head(0);
     for (int h = 0; h < a.r; ++h) {
         const int hv = hk * a.r + h;
         const size_t unit = (size_t)w * a.Hv + hv;
         const float *gates = a.prep + unit * GRAD_PREP;
-        float gamma[4], rest[4], beta[4];   // of token 16 nt + m
-#pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
-            gamma[nt] = gates[16 * nt + m];
-            rest[nt] = gates[SC + 16 * nt + m];
-            beta[nt] = gates[2 * SC + 16 * nt + m];
-        }
-        const float last = gates[SC - 1];
-        if (wave == 0) {
-            const float g1 = a.g[(size_t)(at.first + min(lane, at.n - 1)) * a.Hv + hv];
+        if constexpr (!AHEAD)
+            load_head(h);
+        const float last = __shfl(gamma[3], 15);   // (of token 63)
+        if constexpr (NP < FULL)
+            load_states(unit, 0, 0);
+        if (wave == 0)
             cs[lane] = sum_below(lane < at.n ? log2_gate(g1) : 0.0);
-        }
         {   // the tokens' rows: 16 columns of 32 a lane group, tile by tile
-            const Buffer vb = head_rows<TIn, D>(static_cast<const TIn *>(a.v) + at.first * a.v_stride + hv * D, a.v_stride, at.n);
-            const Buffer ob = head_rows<TOut, D>(static_cast<const TOut *>(ga.dout) + ((size_t)at.first * a.Hv + hv) * D, (int64_t)a.Hv * D, at.n);
-            const Buffer zb(a.z + unit * SC * D, 4 * SC * D), db(ga.dd + unit * SC * D, 4 * SC * D);
-            Raw8<TIn> v[4];
-            Raw8<TOut> o[4];
-            Raw8<float> z[4], d[4];
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                const int i = 16 * rt + m;
-                z[rt] = load_raw8<float>(zb, (i * D + mine) * 4);
-                d[rt] = load_raw8<float>(db, (i * D + mine) * 4);
-                v[rt] = load_raw8<TIn>(vb, i * vst + mine * (uint32_t)sizeof(TIn));
-                o[rt] = load_raw8<TOut>(ob, i * ost + mine * (uint32_t)sizeof(TOut));
+            for (int j = 0; j < 2; ++j) {
+                float x = 0.0f;
+#pragma unroll
+                for (int i = 0; i < (D / 16 + NWV - 1) / NWV; ++i)
+                    x += parts[j][i];
+                sums[3 + j][wave][lane] = x;
             }
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
@@ -363,20 +392,22 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
                 }
             }
         }
-        __syncthreads();
+        lds_barrier();
         // against the states: S0 dO', S0 dV', dS1 E'
         f32x4_t q0[2][4] = {}, k0[2][4] = {}, k1[2][4] = {};
         float sq = 0.0f;
-        const Buffer sb(a.s0 + unit * D * D, 4 * D * D), dsb(ga.ds + unit * D * D, 4 * D * D);
-#pragma unroll UNROLL
+#pragma unroll UNROLL   // (the register sets take turns)
         for (int ks = 0; ks < KS; ++ks) {
+            if constexpr (NP == FULL)
+                load_states(unit, ks, 0);
+            else if (ks + 1 < KS)
+                load_states(unit, ks + 1, (ks + 1) % 2);
             uint4 ps[2][FULL], pd[2][LK];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const uint32_t from = (state_row_of(2 * wave + t, m / 4, m % 4) * D + 32 * ks + 8 * g) * 4;
                 float x[8], y[8];
-                unpack8(load_raw8<float>(sb, from), x);
-                unpack8(load_raw8<float>(dsb, from), y);
+                unpack8(sraw[NP == FULL ? 0 : ks % 2][t], x);
+                unpack8(draw[NP == FULL ? 0 : ks % 2][t], y);
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     sq = fmaf(x[j], y[j], sq);
@@ -414,6 +445,10 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
             sq += __shfl_xor(sq, s);
         if (lane == 0)
             square[wave] = sq;
+        if constexpr (AHEAD) {
+            kt.load(kb, kst, wave, lane);
+            qt.load(qb, qst, wave, lane);
+        }
         auto put_matrices = [&](int it, const f32x4_t (&y1)[4], const f32x4_t (&y2)[4]) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -483,19 +518,22 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
             if constexpr (APART)
                 put_matrices(it, x1[it], x2[it]);
         }
+        lds_barrier();
         if constexpr (!APART) {
-            __syncthreads();
 #pragma unroll
             for (int it = 0; it < ITS; ++it)
                 put_matrices(it, x1[it], x2[it]);
         }
-        if constexpr (NP > 1) {
+        if constexpr (!AHEAD) {
             kt.load(kb, kst, wave, lane);
             qt.load(qb, qst, wave, lane);
         }
         kt.store(kimg, wave, lane);
         qt.store(qimg, wave, lane);
-        __syncthreads();
+        const float beta_now[4] = {beta[0], beta[1], beta[2], beta[3]};
+        if constexpr (AHEAD)
+            load_head(min(h + 1, a.r - 1));
+        lds_barrier();
         // dQ' += K' W1', dK' -= K' W2' (summed over j); dK' += Q' W1 - K' W2 (summed over i)
         static_for<2>([&](auto step) {
             constexpr int s = step(), FROM = 2 * s;   // columns from 32 s on have something in rows 32 s ..
@@ -565,7 +603,7 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
 #pragma unroll
             for (int v = 0; v < NWV; ++v)
                 oe += sums[0][v][16 * nt + m];
-            oe *= beta[nt];   // W1's diagonal
+            oe *= beta_now[nt];   // W1's diagonal
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 dot = fmaf(x[j], q0[j / 4][nt][j % 4], dot);
@@ -577,7 +615,7 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
             if (g == 0)
                 sums[2][wave][16 * nt + m] = dot;
         }
-        __syncthreads();
+        lds_barrier();
         if (wave == 0) {
             float oe = 0.0f, own_terms = 0.0f, total = 0.0f, in = 0.0f, on = 0.0f;
 #pragma unroll
@@ -585,12 +623,8 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
                 oe += sums[0][v][lane];
                 own_terms += sums[1][v][lane] + sums[2][v][lane];
                 total += square[v];
-            }
-            const float *parts = ga.part + unit * GRAD_PARTS + lane;
-#pragma unroll
-            for (int v = 0; v < D / 16; ++v) {
-                in += parts[v * 2 * SC];
-                on += parts[v * 2 * SC + SC];
+                in += sums[3][v][lane];
+                on += sums[4][v][lane];
             }
             const float b1 = gates[2 * SC + lane];
             const float from_here = own_terms - b1 * in, before = b1 * on;   // (0 behind the chunk's end)
@@ -601,7 +635,7 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
                 ga.dg[to] = (float)(all - upto + from_here + ahead + total * last);
             }
         }
-        __syncthreads();
+        lds_barrier();
     }
     auto put = [&](void *to, int64_t stride, const f32x4_t (&x)[2][4]) {
         TIn *rows = static_cast<TIn *>(to) + at.first * stride + hk * D + mine;
