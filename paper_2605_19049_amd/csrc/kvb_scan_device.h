@@ -209,15 +209,18 @@ __device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const uint
             if (i + j < FULL)
                 c = mfma16x32<bf16_t>(a[i], b[j], c);
 }
+// two sums at a time, in turns: a product waits for the one before on the same sum
 template <int NA, int NB>
-__device__ __forceinline__ void mma(f32x4_t &c, const uint4 (&a)[NA], const Pieces<NB> &b)
+__device__ __forceinline__ void mma2(f32x4_t &c, f32x4_t &d, const uint4 (&a)[NA], const uint4 (&a2)[NA], const Pieces<NB> &b)
 {
 #pragma unroll
     for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j)
-            if (i + j < FULL)
+            if (i + j < FULL) {
                 c = mfma16x32<bf16_t>(a[i], b.piece(j), c);
+                d = mfma16x32<bf16_t>(a2[i], b.piece(j), d);
+            }
 }
 
 // Products and what else there is to do, in turns.  A wave issues in order: products in a row wait for each other, 16 cycles
@@ -505,18 +508,20 @@ struct Words {
                 b.to_lds(to + (wave + NWV * i) * 1024, (wave + NWV * i) * 1024 + lane * 16);
     }
 };
-// The tiles of such an image in an order in which those of rows 32 s .. follow each other: tile i is (tile_row, tile_step).
+// The tiles of such an image in pairs of one step: pair i has the tiles of rows pair_row(i) and the next, step pair_step(i).
+constexpr int SCAN_PAIRS = SCAN_TILES / 2;
 template <bool UPPER>
-__host__ __device__ constexpr int tile_row(int i) { return UPPER ? (i < 2 ? i : i - 2) : (i < 4 ? i : i - 2); }
+__host__ __device__ constexpr int pair_row(int i) { return UPPER ? (i == 2 ? 2 : 0) : (i == 0 ? 0 : 2); }
 template <bool UPPER>
-__host__ __device__ constexpr int tile_step(int i) { return UPPER ? i >= 2 : i >= 4; }
-// its pieces
+__host__ __device__ constexpr int pair_step(int i) { return UPPER ? i > 0 : i > 1; }
 template <bool UPPER>
-__device__ __forceinline__ void load_tile(const uint4 *img, int i, int lane, uint4 (&a)[FULL])
+__device__ __forceinline__ void load_pair(const uint4 *img, int i, int lane, uint4 (&a)[2][FULL])
 {
 #pragma unroll
-    for (int j = 0; j < FULL; ++j)
-        a[j] = img[j * SCAN_UNITS + tile_of<UPPER>(tile_row<UPPER>(i), tile_step<UPPER>(i)) * 64 + lane];
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < FULL; ++j)
+            a[h][j] = img[j * SCAN_UNITS + tile_of<UPPER>(pair_row<UPPER>(i) + h, pair_step<UPPER>(i)) * 64 + lane];
 }
 
 // Threads that a kernel over the chunks is built for.  With DMA a wave needs less than 256 registers; built for 8 waves a workgroup, the

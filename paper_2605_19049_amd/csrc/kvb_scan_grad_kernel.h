@@ -143,7 +143,13 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
         // kd = K dS; the pieces of dS
         Pieces<FULL> sp[KS], oq[2], xp[2], zp[2];
         Pieces<PIECES<TOut>> od[2];
-        uint4 fr[2][4][NP], ft[2][NP], fm[2][FULL];
+        uint4 fr[2][4][NP], ft[2][2][NP], fm[2][2][FULL];
+        auto columns = [&](const uint4 *img, auto i) {   // pair i of KT
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                Tok::columns(img, (2 * i() + h) % KT, 2 * i() / KT, lane, ft[i() % 2][h]);
+        };
+        auto update = [&](auto i, const Pieces<FULL> (&p)[2]) { constexpr int t = 2 * i() % KT; mma2(S[t], S[t + 1], ft[i() % 2][0], ft[i() % 2][1], p[2 * i() / KT]); };
         auto gate_at = [&](int which, int rt) { return as_f32x4(gate[16 * which + 4 * rt + g]); };
         auto rows = [&](int ks) {
 #pragma unroll
@@ -154,35 +160,39 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             sp[0].word(j, S[0], S[1]);
-        weave<4 * KS>([&](auto i) { mma(kd[i() % 4], fr[i() / 4 % 2][i() % 4], sp[i() / 4]); },
+        weave<2 * KS>([&](auto i) { constexpr int rt = 2 * (i() % 2); mma2(kd[rt], kd[rt + 1], fr[i() / 2 % 2][rt], fr[i() / 2 % 2][rt + 1], sp[i() / 2]); },
                       [&](auto i) {
-                          constexpr int ks = i() / 4, rt = i() % 4;
+                          constexpr int ks = i() / 2, rt = 2 * (i() % 2);
                           if constexpr (ks + 1 < KS) {
                               sp[ks + 1].word(rt, S[2 * ks + 2], S[2 * ks + 3]);
+                              sp[ks + 1].word(rt + 1, S[2 * ks + 2], S[2 * ks + 3]);
                               if constexpr (rt == 0)
                                   rows(ks + 1);
                           } else {
-                              od[rt / 2].half(rt % 2, dO[rt]);
-                              if constexpr (rt == 3)
-                                  load_tile<true>(mats + SCAN_MAT, 0, lane, fm[0]);
+                              od[rt / 2].half(0, dO[rt]);
+                              od[rt / 2].half(1, dO[rt + 1]);
+                              if constexpr (rt == 2)
+                                  load_pair<true>(mats + SCAN_MAT, 0, lane, fm[0]);
                           }
-                          if constexpr (rt == 3)
+                          if constexpr (rt == 2)
                               request(std::integral_constant<int, ks>{}, max(c - 1, 0), buf ^ 1);
                       });
         // X = P' dO (without P's diagonal); dS decays, the pieces of scale gamma dO
         const float last = reinterpret_cast<const float *>(gate)[SC - 1];
-        weave<SCAN_TILES>([&](auto i) { mma(X[tile_row<true>(i())], fm[i() % 2], od[tile_step<true>(i())]); },
+        weave<SCAN_PAIRS>([&](auto i) { constexpr int rt = pair_row<true>(i()); mma2(X[rt], X[rt + 1], fm[i() % 2][0], fm[i() % 2][1], od[pair_step<true>(i())]); },
                           [&](auto i) {
-                              if constexpr (i() + 1 < SCAN_TILES)
-                                  load_tile<true>(mats + SCAN_MAT, i() + 1, lane, fm[(i() + 1) % 2]);
+                              if constexpr (i() + 1 < SCAN_PAIRS)
+                                  load_pair<true>(mats + SCAN_MAT, i() + 1, lane, fm[(i() + 1) % 2]);
                               else
-                                  Tok::columns(qimg, 0, 0, lane, ft[0]);
-                              if constexpr (i() < 4)
-                                  oq[i() / 2].half(i() % 2, a.scale * gate_at(0, i()) * dO[i()]);
-                              else
+                                  columns(qimg, std::integral_constant<int, 0>{});
+                              if constexpr (i() < 2) {
+                                  oq[i()].half(0, a.scale * gate_at(0, 2 * i()) * dO[2 * i()]);
+                                  oq[i()].half(1, a.scale * gate_at(0, 2 * i() + 1) * dO[2 * i() + 1]);
+                              } else {
 #pragma unroll
-                                  for (int t = (i() - 4) * KT / 2; t < (i() - 3) * KT / 2; ++t)
+                                  for (int t = 0; t < KT; ++t)
                                       S[t] *= last;
+                              }
                           });
         // dS += Q' scale gamma dO; kd = rest kd + scale q.k dO, dn = scale P' dO, the pieces of beta X, X = dn + kd; E rest kd
         float inner[16], outer[16];
@@ -200,14 +210,14 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
                 xp[rt / 2].word(2 * (rt % 2) + i() % 3 - 1, X[rt], X[rt]);
             }
         };
-        weave<2 * KT>([&](auto i) { mma(S[i() % KT], ft[i() % 2], oq[i() / KT]); },
-                      [&](auto i) {
-                          if constexpr (i() + 1 < 2 * KT)
-                              Tok::columns(qimg, (i() + 1) % KT, (i() + 1) / KT, lane, ft[(i() + 1) % 2]);
-                          else
-                              load_tile<true>(mats, 0, lane, fm[0]);
-                          share<12, 2 * KT, i()>(join);
-                      });
+        weave<KT>([&](auto i) { update(i, oq); },
+                  [&](auto i) {
+                      if constexpr (i() + 1 < KT)
+                          columns(qimg, std::integral_constant<int, i() + 1>{});
+                      else
+                          load_pair<true>(mats, 0, lane, fm[0]);
+                      share<12, KT, i()>(join);
+                  });
         // dn += M' beta X: what D has that decays.  Then the tokens' sums of E dn and E rest kd over the wave's columns, D = dn + kd,
         // dV = beta D, and the pieces of -gamma dV
         request_rows(max(c - 1, 0));
@@ -228,27 +238,27 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
                 zp[s()].word(i() - 1, kd[lo], kd[lo + 1]);
             }
         };
-        weave<SCAN_TILES>([&](auto i) { mma(dn[tile_row<true>(i())], fm[i() % 2], xp[tile_step<true>(i())]); },
+        weave<SCAN_PAIRS>([&](auto i) { constexpr int rt = pair_row<true>(i()); mma2(dn[rt], dn[rt + 1], fm[i() % 2][0], fm[i() % 2][1], xp[pair_step<true>(i())]); },
                           [&](auto i) {
-                              if constexpr (i() + 1 < SCAN_TILES)
-                                  load_tile<true>(mats, i() + 1, lane, fm[(i() + 1) % 2]);
+                              if constexpr (i() + 1 < SCAN_PAIRS)
+                                  load_pair<true>(mats, i() + 1, lane, fm[(i() + 1) % 2]);
                               else
-                                  Tok::columns(kimg, 0, 0, lane, ft[0]);
-                              if constexpr (i() == 1)
+                                  columns(kimg, std::integral_constant<int, 0>{});
+                              if constexpr (i() == 0)
                                   sums[SC] = sum_rows16(outer, m);
-                              if constexpr (i() >= 4)
-                                  share<5, 2, i() - 4>([&](auto j) { end(std::integral_constant<int, 0>{}, j); });
+                              if constexpr (i() == 2)
+                                  static_for<5>([&](auto j) { end(std::integral_constant<int, 0>{}, j); });
                           });
         // dS -= K' gamma dV
-        weave<2 * KT>([&](auto i) { mma(S[i() % KT], ft[i() % 2], zp[i() / KT]); },
-                      [&](auto i) {
-                          if constexpr (i() + 1 < 2 * KT)
-                              Tok::columns(kimg, (i() + 1) % KT, (i() + 1) / KT, lane, ft[(i() + 1) % 2]);
-                          if constexpr (i() < KT)
-                              share<5, KT, i()>([&](auto j) { end(std::integral_constant<int, 1>{}, j); });
-                          else if constexpr (i() == KT)
-                              sums[0] = sum_rows16(inner, m);
-                      });
+        weave<KT>([&](auto i) { update(i, zp); },
+                  [&](auto i) {
+                      if constexpr (i() + 1 < KT)
+                          columns(kimg, std::integral_constant<int, i() + 1>{});
+                      if constexpr (i() < KT / 2)
+                          share<5, KT / 2, i()>([&](auto j) { end(std::integral_constant<int, 1>{}, j); });
+                      else if constexpr (i() == KT / 2)
+                          sums[0] = sum_rows16(inner, m);
+                  });
         if constexpr (!DMA)
             lds_barrier();
     }

@@ -229,14 +229,12 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     Tok knext, qnext;   // (without DMA)
     Prep pnext;
     Rows64<TIn> vnext;
-    // What chunk c needs, asked for in KS parts, one for each step of the products with the state: at once, the requests would
+    int next = min(SC, span.len);   // tokens of the chunk to be asked for, which kp .. prep point to
+    // What that needs, asked for in KS parts, one for each step of the products with the state: at once, the requests would
     // wait for each other at the memory unit and the wave with them.
-    auto request = [&](auto step, int c, int buf) {
+    auto request = [&](auto step, int buf) {
         constexpr int PART = step();
-        const int n = min(SC, span.len - c * SC);
-        const Buffer kb = head_rows<TIn, D>(kp + (int64_t)c * SC * a.k_stride, a.k_stride, n);
-        const Buffer qb = head_rows<TIn, D>(qp + (int64_t)c * SC * a.q_stride, a.q_stride, n);
-        const Buffer image(prep + c * prep_step, 16 * WORDS);
+        const Buffer kb = head_rows<TIn, D>(kp, a.k_stride, next), qb = head_rows<TIn, D>(qp, a.q_stride, next), image(prep, 16 * WORDS);
         if constexpr (DMA) {
             Tok::template to_lds<PART, KS>(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
             if constexpr (!STATES)
@@ -249,8 +247,12 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
             pnext.load(image, wave, lane);
         }
         if constexpr (PART == KS - 1)
-            vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
+            vnext.load(head_rows<TIn, D>(vp, a.v_stride, next), anew(vown), vst);
     };
+    Pieces<FULL> sp[KS];   // of the state
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        sp[0].word(j, S[0], S[1]);
     f32x4_t O[4] = {};
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
     auto put = [&](int c) {   // (STATES: O holds Z)
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         put_rows<TOut>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), anew(oown), ost, a.scale, O);
     };
     if (chunks > 0)
-        static_for<KS>([&](auto step) { request(step, 0, 0); });
+        static_for<KS>([&](auto step) { request(step, 0); });
     for (int c = 0; c < chunks; ++c) {
         const int buf = DMA ? c & 1 : 0;
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = preps[buf] + SCAN_GATES / 4;
@@ -283,6 +285,13 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                 E[rt][r] = vnext.value(rt, r);
         settled(E);
         lds_barrier();
+        if (c + 1 < chunks) {   // (the last chunk is asked for once more behind it)
+            kp += SC * a.k_stride;
+            qp += SC * a.q_stride;
+            vp += SC * a.v_stride;
+            prep += prep_step;
+            next = min(SC, span.len - (c + 1) * SC);
+        }
         // The outputs of the chunk before leave here: what a wave waits for at the chunk's end is then not a store just made.  (Nothing
         // for the first, and the last chunk's inputs once more behind it: branches would make the waits wait for everything.)
         put(c - 1);
@@ -298,33 +307,39 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                     to.store4((state_row_of(t, g, r) * D + col) * 4, __float_as_uint(S[t][r]));
         }
         // y = K S; the state's pieces
-        Pieces<FULL> sp[KS], yp[2], up[2], ep[2];
-        uint4 fr[2][4][NP], ft[2][NP], fm[2][FULL];
+        Pieces<FULL> yp[2], up[2], ep[2];
+        uint4 fr[2][4][NP], ft[2][2][NP], fm[2][2][FULL];
         f32x4_t gm[4], bt[4], re[4];
+        auto columns = [&](auto i) {   // pair i of KT
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                Tok::columns(kimg, (2 * i() + h) % KT, 2 * i() / KT, lane, ft[i() % 2][h]);
+        };
         auto rows = [&](const uint4 *img, int ks, uint4 (&f)[4][NP]) {
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt)
                 Tok::rows(img, rt, ks, lane, f[rt]);
         };
         rows(kimg, 0, fr[0]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            sp[0].word(j, S[0], S[1]);
-        weave<4 * KS>([&](auto i) { mma(y[i() % 4], fr[i() / 4 % 2][i() % 4], sp[i() / 4]); },
+        weave<2 * KS>([&](auto i) { constexpr int rt = 2 * (i() % 2); mma2(y[rt], y[rt + 1], fr[i() / 2 % 2][rt], fr[i() / 2 % 2][rt + 1], sp[i() / 2]); },
                       [&](auto i) {
-                          constexpr int ks = i() / 4, rt = i() % 4;
-                          if constexpr (ks + 1 < KS)
+                          constexpr int ks = i() / 2, rt = 2 * (i() % 2);
+                          if constexpr (ks + 1 < KS) {
                               sp[ks + 1].word(rt, S[2 * ks + 2], S[2 * ks + 3]);
-                          if constexpr (rt == 0 && ks + 1 < KS)
-                              rows(kimg, ks + 1, fr[(ks + 1) % 2]);
-                          if constexpr (rt == 0 && ks + 1 == KS && !STATES)
-                              rows(qimg, 0, fr[KS % 2]);
-                          if constexpr (ks + 1 == KS) {
-                              gm[rt] = as_f32x4(gate[4 * rt + g]);
-                              bt[rt] = as_f32x4(gate[32 + 4 * rt + g]);
+                              sp[ks + 1].word(rt + 1, S[2 * ks + 2], S[2 * ks + 3]);
+                              if constexpr (rt == 0)
+                                  rows(kimg, ks + 1, fr[(ks + 1) % 2]);
+                          } else {
+                              if constexpr (rt == 0 && !STATES)
+                                  rows(qimg, 0, fr[KS % 2]);
+#pragma unroll
+                              for (int h = rt; h < rt + 2; ++h) {
+                                  gm[h] = as_f32x4(gate[4 * h + g]);
+                                  bt[h] = as_f32x4(gate[32 + 4 * h + g]);
+                              }
                           }
-                          if constexpr (rt == 3)
-                              request(std::integral_constant<int, ks>{}, min(c + 1, chunks - 1), buf ^ 1);
+                          if constexpr (rt == 2)
+                              request(std::integral_constant<int, ks>{}, buf ^ 1);
                       });
         // O = Q S; Y = V - gamma y, the pieces of beta Y
         auto residual = [&](auto i) {
@@ -346,12 +361,11 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         if constexpr (STATES)
             static_for<12>(residual);
         else
-            weave<4 * KS>([&](auto i) { mma(O[i() % 4], fr[(KS + i() / 4) % 2][i() % 4], sp[i() / 4]); },
+            weave<2 * KS>([&](auto i) { constexpr int rt = 2 * (i() % 2); mma2(O[rt], O[rt + 1], fr[(KS + i() / 2) % 2][rt], fr[(KS + i() / 2) % 2][rt + 1], sp[i() / 2]); },
                           [&](auto i) {
-                              constexpr int ks = i() / 4, rt = i() % 4;
-                              if constexpr (rt == 0 && ks + 1 < KS)
-                                  rows(qimg, ks + 1, fr[(KS + ks + 1) % 2]);
-                              share<12, 4 * KS, i()>(residual);
+                              if constexpr (i() % 2 == 0 && i() / 2 + 1 < KS)
+                                  rows(qimg, i() / 2 + 1, fr[(KS + i() / 2 + 1) % 2]);
+                              share<12, 2 * KS, i()>(residual);
                           });
         // E = Y + M beta Y (STATES: Z); the state and O decay, and the pieces of beta E and rest beta E of the first 32 tokens
         const float last = reinterpret_cast<const float *>(gate)[SC - 1];
@@ -376,50 +390,52 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                 ep[s()].word(i() - 6, y[lo], y[hi]);
             }
         };
-        load_tile<false>(mats, 0, lane, fm[0]);
-        weave<SCAN_TILES>([&](auto i) { mma(sum[tile_row<false>(i())], fm[i() % 2], yp[tile_step<false>(i())]); },
+        load_pair<false>(mats, 0, lane, fm[0]);
+        weave<SCAN_PAIRS>([&](auto i) { constexpr int rt = pair_row<false>(i()); mma2(sum[rt], sum[rt + 1], fm[i() % 2][0], fm[i() % 2][1], yp[pair_step<false>(i())]); },
                           [&](auto i) {
-                              if constexpr (i() + 1 < SCAN_TILES)
-                                  load_tile<false>(mats, i() + 1, lane, fm[(i() + 1) % 2]);
-                              if constexpr (i() < 2) {
-                                  re[2 * i()] = as_f32x4(gate[16 + 8 * i() + g]);
-                                  re[2 * i() + 1] = as_f32x4(gate[16 + 8 * i() + 4 + g]);
-                                  if constexpr (!STATES) {
-                                      O[2 * i()] *= gm[2 * i()];
-                                      O[2 * i() + 1] *= gm[2 * i() + 1];
+                              if constexpr (i() + 1 < SCAN_PAIRS)
+                                  load_pair<false>(mats, i() + 1, lane, fm[(i() + 1) % 2]);
+                              else
+                                  columns(std::integral_constant<int, 0>{});
+                              if constexpr (i() == 0) {
+#pragma unroll
+                                  for (int rt = 0; rt < 4; ++rt) {
+                                      re[rt] = as_f32x4(gate[16 + 4 * rt + g]);
+                                      if constexpr (!STATES)
+                                          O[rt] *= gm[rt];
                                   }
-                              } else if constexpr (i() < 4) {
-                                  share<10, 2, i() - 2>([&](auto j) { weigh(std::integral_constant<int, 0>{}, j); });
+                              } else if constexpr (i() == 1) {
+                                  static_for<10>([&](auto j) { weigh(std::integral_constant<int, 0>{}, j); });
                               } else {
 #pragma unroll
-                                  for (int t = (i() - 4) * KT / 2; t < (i() - 3) * KT / 2; ++t)
+                                  for (int t = 0; t < KT; ++t)
                                       S[t] *= last;
                               }
-                              if constexpr (i() + 1 == SCAN_TILES)
-                                  Tok::columns(kimg, 0, 0, lane, ft[0]);
                           });
-        // S += K' rest beta E, O += P beta E, 32 tokens and then the others, whose pieces are made on the way
-        static_for<2>([&](auto step) {
-            constexpr int s = step();
-            weave<KT>([&](auto t) { mma(S[t()], ft[t() % 2], ep[s]); },
-                      [&](auto t) {
-                          if constexpr (t() + 1 < KT)
-                              Tok::columns(kimg, t() + 1, s, lane, ft[(t() + 1) % 2]);
-                          else if constexpr (s == 0)
-                              Tok::columns(kimg, 0, 1, lane, ft[KT % 2]);
-                          if constexpr (t() + 1 == KT && !STATES)
-                              load_tile<false>(mats + SCAN_MAT, 4 * s, lane, fm[0]);
-                          if constexpr (s == 0)
-                              share<10, KT, t()>([&](auto j) { weigh(std::integral_constant<int, 1>{}, j); });
-                      });
-            static_assert(KT % 2 == 0);
-            if constexpr (!STATES)
-                weave<4 - 2 * s>([&](auto i) { mma(O[2 * s + i()], fm[i() % 2], up[s]); },
-                                 [&](auto i) {
-                                     if constexpr (i() + 1 < 4 - 2 * s)
-                                         load_tile<false>(mats + SCAN_MAT, 4 * s + i() + 1, lane, fm[(i() + 1) % 2]);
-                                 });
+        // S += K' rest beta E, O += P beta E: the state from the first 32 tokens, while the others' pieces are made, O, the state from the others
+        auto update = [&](auto i) { constexpr int t = 2 * i() % KT; mma2(S[t], S[t + 1], ft[i() % 2][0], ft[i() % 2][1], ep[2 * i() / KT]); };
+        weave<KT / 2>(update, [&](auto i) {
+            columns(std::integral_constant<int, i() + 1>{});
+            if constexpr (!STATES && i() + 1 == KT / 2)
+                load_pair<false>(mats + SCAN_MAT, 0, lane, fm[0]);
+            share<10, KT / 2, i()>([&](auto j) { weigh(std::integral_constant<int, 1>{}, j); });
         });
+        if constexpr (!STATES)
+            weave<SCAN_PAIRS>([&](auto i) { constexpr int rt = pair_row<false>(i()); mma2(O[rt], O[rt + 1], fm[i() % 2][0], fm[i() % 2][1], up[pair_step<false>(i())]); },
+                              [&](auto i) {
+                                  if constexpr (i() + 1 < SCAN_PAIRS)
+                                      load_pair<false>(mats + SCAN_MAT, i() + 1, lane, fm[(i() + 1) % 2]);
+                              });
+        weave<KT / 2>([&](auto i) { update(std::integral_constant<int, KT / 2 + i()>{}); },
+                      [&](auto i) {
+                          if constexpr (i() + 1 < KT / 2)
+                              columns(std::integral_constant<int, KT / 2 + i() + 1>{});
+                          // the first pieces of the next chunk's state
+                          if constexpr (i() > 0)
+                              share<4, KT / 2 - 1, i() - 1>([&](auto j) { sp[0].word(j(), S[0], S[1]); });
+                      });
+        if constexpr (KT == 2)
+            static_for<4>([&](auto j) { sp[0].word(j(), S[0], S[1]); });
         if constexpr (!DMA)
             lds_barrier();
     }
