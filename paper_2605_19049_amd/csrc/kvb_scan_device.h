@@ -319,9 +319,12 @@ struct Buffer {
     }
     __device__ __forceinline__ uint4 load16(uint32_t at) const { return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0)); }
     __device__ __forceinline__ uint32_t load4(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, 0); }
-    __device__ __forceinline__ uint16_t load2(uint32_t at) const { return __builtin_amdgcn_raw_buffer_load_b16(r, at, 0, 0); }
+    __device__ __forceinline__ void store8(uint32_t at, uint2 x) const
+    {
+        typedef uint32_t v2 __attribute__((ext_vector_type(2)));
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(v2, x), r, at, 0, 0);
+    }
     __device__ __forceinline__ void store4(uint32_t at, uint32_t x) const { __builtin_amdgcn_raw_buffer_store_b32(x, r, at, 0, 0); }
-    __device__ __forceinline__ void store2(uint32_t at, uint16_t x) const { __builtin_amdgcn_raw_buffer_store_b16(x, r, at, 0, 0); }
 };
 __device__ __forceinline__ uint32_t lds_at(const uint4 *p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint4 *)p; }
 // x, anew: what is worked out from it inside a loop stays there and takes no register around it
@@ -361,47 +364,100 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// The lane's column of the wave's 64 rows 16 rt + 4 g + r of a token array (g = lane / 16), untouched bits
+// ds_read_b64_tr_b16: 16 lanes read four rows of 16 (8 bytes a lane, rows in turn) and get a column of four each
+__device__ __forceinline__ uint2 transposed_four(const uint2 *p)
+{
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) v4s *Lds;
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p));
+}
+
+// A wave's 16 columns of a chunk's 64 rows of a 16-bit array on their way in or out, in 2 KB of LDS of its own: two requests bring
+// them (16 bytes a lane), transposing reads hand them out as a sum's tiles stand.  With a load of two bytes a lane and row, or a store,
+// the memory unit was what a chunk waited for (a request takes it 40 to 80 cycles whatever its size).
 template <typename T>
-struct Rows64 {
-    using Raw = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
-    Raw x[4][4];
-    // own: the lane's offset, that of its column in row 4 g
-    __device__ __forceinline__ void load(const Buffer &b, uint32_t own, uint32_t stride_bytes)
+struct Slab {
+    static constexpr int WORDS = 128;
+    static_assert(sizeof(T) == 2);
+    uint4 *img;      // the wave's
+    uint32_t first;  // the wave's first column, in bytes
+    // (a clobber of memory, unlike Buffer::to_lds: what was read from here before has to have been read)
+    __device__ __forceinline__ void request(const Buffer &b, uint32_t stride_bytes, int lane) const
+    {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_at(img)), at = (uint32_t)(lane / 2) * stride_bytes + first + lane % 2 * 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * 1024), "v"(at + i * 32 * stride_bytes), "s"(b.words)
+                         : "memory", "m0");
+    }
+    __device__ __forceinline__ void read(f32x4_t (&x)[4], int lane) const
     {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t at = own + (16 * (i / 4) + i % 4) * stride_bytes;
-            if constexpr (sizeof(T) == 4)
-                x[i / 4][i % 4] = b.load4(at);
-            else
-                x[i / 4][i % 4] = b.load2(at);
+        for (int rt = 0; rt < 4; ++rt) {
+            const uint2 w = transposed_four(reinterpret_cast<const uint2 *>(img) + (16 * rt + 4 * (lane / 16) + lane % 16 / 4) * 4 + lane % 4);
+            const float2 lo = unpack_pair<T>(w.x), hi = unpack_pair<T>(w.y);
+            x[rt] = f32x4_t{lo.x, lo.y, hi.x, hi.y};
         }
     }
-    __device__ __forceinline__ float value(int rt, int r) const { return to_f32(__builtin_bit_cast(T, x[rt][r])); }
-};
-// The same rows of a result
-template <typename T>
-__device__ __forceinline__ void put_rows(const Buffer &b, uint32_t own, uint32_t stride_bytes, float scale, const f32x4_t (&x)[4])
-{
+    __device__ __forceinline__ void put(const Buffer &b, uint32_t stride_bytes, float scale, const f32x4_t (&x)[4], int lane) const
+    {
+        const int m = lane % 16, g = lane / 16;
+        uint2 *to = reinterpret_cast<uint2 *>(img);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t at = own + (16 * (i / 4) + i % 4) * stride_bytes;
-        if constexpr (sizeof(T) == 4)
-            b.store4(at, __float_as_uint(scale * x[i / 4][i % 4]));
-        else
-            b.store2(at, from_f32<T>(scale * x[i / 4][i % 4]).bits);
+        for (int rt = 0; rt < 4; ++rt) {   // column m, rows 4 g ..
+            const f32x4_t y = scale * x[rt];
+            to[rt * 64 + m * 4 + g] = make_uint2(pack_pair<T>(y[0], y[1]), pack_pair<T>(y[2], y[3]));
+        }
+        const uint32_t at = m * stride_bytes + first + 8 * g;
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt)     // row m, columns 4 g ..
+            b.store8(at + 16 * rt * stride_bytes, transposed_four(to + rt * 64 + (4 * g + m / 4) * 4 + m % 4));
     }
-}
+};
+
+// The wave's 16 columns of a chunk's 64 rows of a token array, as a sum's tiles stand: of 16-bit arrays through a slab, of fp32 ones by a
+// load for each row 16 rt + 4 g + r, which is on its way a chunk ahead.
+template <typename T>
+struct Columns {
+    static constexpr bool SLAB = sizeof(T) == 2;
+    uint32_t x[SLAB ? 1 : 16];
+    __device__ __forceinline__ void request(const Buffer &b, uint4 *slab, uint32_t first, uint32_t stride_bytes, int lane)
+    {
+        if constexpr (SLAB) {
+            Slab<T>{slab, first}.request(b, stride_bytes, lane);
+        } else {
+            const uint32_t own = anew(4 * (lane / 16) * stride_bytes + first + lane % 16 * 4);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                x[i] = b.load4(own + (16 * (i / 4) + i % 4) * stride_bytes);
+        }
+    }
+    __device__ __forceinline__ void read(const uint4 *slab, f32x4_t (&y)[4], int lane) const
+    {
+        if constexpr (SLAB)
+            Slab<T>{const_cast<uint4 *>(slab), 0}.read(y, lane);
+        else
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                y[i / 4][i % 4] = __uint_as_float(x[i]);
+    }
+    static __device__ __forceinline__ void put(const Buffer &b, uint4 *slab, uint32_t first, uint32_t stride_bytes, float scale, const f32x4_t (&y)[4], int lane)
+    {
+        if constexpr (SLAB) {
+            Slab<T>{slab, first}.put(b, stride_bytes, scale, y, lane);
+        } else {
+            const uint32_t own = anew(4 * (lane / 16) * stride_bytes + first + lane % 16 * 4);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                b.store4(own + (16 * (i / 4) + i % 4) * stride_bytes, __float_as_uint(scale * y[i / 4][i % 4]));
+        }
+    }
+};
 
 // Four values down a column from each of two blocks; the lane's 8 bytes are the first or second half of the words at p and q
 __device__ __forceinline__ uint4 transposed_pair(const uint4 *p, const uint4 *q, int half)
 {
-    typedef short v4s __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) v4s *Lds;
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(reinterpret_cast<const uint2 *>(p) + half));
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(reinterpret_cast<const uint2 *>(q) + half));
-    const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+    const uint2 l = transposed_four(reinterpret_cast<const uint2 *>(p) + half), h = transposed_four(reinterpret_cast<const uint2 *>(q) + half);
     return make_uint4(l.x, l.y, h.x, h.y);
 }
 // A 64 x 64 matrix's piece in LDS, tile row it, 32-column step s, lane (row m; group g: columns 4g .. and 16+4g .. of the step): its
@@ -459,8 +515,7 @@ struct TokenTile {
         for (int j = 0; j < NP; ++j)
             a[j] = img[((j * 4 + rt) * STEPS + ks) * 64 + lane];
     }
-    // the transpose: rows are the state's rows of tile mt, summed over tokens 32 s .. (ds_read_b64_tr_b16: 16 lanes read four
-    // rows of 16, four columns a lane, and get a column of four each)
+    // the transpose: rows are the state's rows of tile mt, summed over tokens 32 s ..
     static __device__ __forceinline__ void columns(const uint4 *img, int mt, int s, int lane, uint4 (&a)[NP])
     {
         const int at = (lane % 4) * 16 + 4 * (lane / 16) + lane % 16 / 4;

@@ -32,6 +32,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     using Gates = Words<SCAN_GATES / 4, NWV>;
     using Mats = Words<2 * SCAN_MAT, NWV>;
     __shared__ uint4 kimgs[BUF][Tok::WORDS], qimgs[BUF][Tok::WORDS], matss[BUF][2 * SCAN_MAT], gatess[BUF][SCAN_GATES / 4];
+    __shared__ uint4 slabs[NWV][sizeof(TIn) == 2 ? 128 : 1], oslabs[NWV][sizeof(TOut) == 2 ? 128 : 1];   // (values in, their gradients out; the outputs' in)
     const ScanArgs &a = ga.f;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
@@ -69,15 +70,16 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     const TIn *vp = static_cast<const TIn *>(a.v) + span.first * a.v_stride + hv * D;
     TIn *dvp = static_cast<TIn *>(ga.dv) + span.first * a.v_stride + hv * D;
     const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
-    const uint32_t vown = 4 * g * vst + col * sizeof(TIn), oown = 4 * g * ost + col * sizeof(TOut), eown = (4 * g * D + col) * 4;
+    const uint32_t first = 16 * (part * NWV + wave);   // the wave's column
+    uint4 *slab = slabs[wave], *oslab = oslabs[wave];
 
     const uint32_t kat = lds_at(kimgs[0]), qat = lds_at(qimgs[0]), mat = lds_at(matss[0]), gat = lds_at(gatess[0]);
     Tok knext, qnext;   // (without DMA)
     Mats mnext;
     Gates gnext;
-    Rows64<TOut> onext;
-    Rows64<float> znext;
-    Rows64<TIn> vnext;
+    Columns<TOut> onext;
+    Columns<float> znext;
+    Columns<TIn> vnext;
     auto request = [&](auto step, int c, int buf) {   // (in parts: kvb_scan_kernel)
         constexpr int PART = step();
         const int n = min(SC, span.len - c * SC);
@@ -99,9 +101,9 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     };
     auto request_rows = [&](int c) {
         const int n = min(SC, span.len - c * SC);
-        onext.load(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), anew(oown), ost);
-        znext.load(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), anew(eown), 4 * D);
-        vnext.load(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), anew(vown), vst);
+        onext.request(head_rows<TOut, D>(op + (int64_t)c * SC * a.Hv * D, (int64_t)a.Hv * D, n), oslab, first * sizeof(TOut), ost, lane);
+        znext.request(head_rows<float, D>(a.z + (own_chunk + (size_t)c * a.Hv) * SC * D, D, SC), nullptr, first * 4, 4 * D, lane);
+        vnext.request(head_rows<TIn, D>(vp + (int64_t)c * SC * a.v_stride, a.v_stride, n), slab, first * sizeof(TIn), vst, lane);
     };
     if (chunks > 0) {
         static_for<KS>([&](auto step) { request(step, chunks - 1, 0); });
@@ -110,28 +112,28 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     f32x4_t X[4] = {}, dn[4] = {};   // from a chunk's end on dV and D
     auto put = [&](int c) {
         const bool none = c >= chunks;
-        put_rows<TIn>(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, none ? 0 : min(SC, span.len - c * SC)), anew(vown), vst, 1.0f, X);
-        put_rows<float>(head_rows<float, D>(ga.dd + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, none ? 0 : SC), anew(eown), 4 * D, 1.0f, dn);
+        Columns<TIn>::put(head_rows<TIn, D>(dvp + (int64_t)c * SC * a.v_stride, a.v_stride, none ? 0 : min(SC, span.len - c * SC)), slab, first * sizeof(TIn), vst,
+                          1.0f, X, lane);
+        Columns<float>::put(head_rows<float, D>(ga.dd + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, none ? 0 : SC), nullptr, first * 4, 4 * D, 1.0f, dn, lane);
     };
     for (int c = chunks - 1, buf = 0; c >= 0; --c, buf = DMA ? buf ^ 1 : 0) {
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = matss[buf];
         const float4 *gate = reinterpret_cast<const float4 *>(gatess[buf]);
-        if constexpr (DMA) {
+        if constexpr (DMA || Columns<TIn>::SLAB)
             lds_loads_done();
-        } else {
+        if constexpr (!DMA) {
             knext.store(kimgs[0], wave, lane);
             qnext.store(qimgs[0], wave, lane);
             mnext.store(matss[0], wave, lane);
             gnext.store(gatess[0], wave, lane);
         }
-        f32x4_t dO[4], E[4], kd[4] = {};
+        f32x4_t dO[4], E[4], Z[4], kd[4] = {};
+        onext.read(oslab, dO, lane);
+        vnext.read(slab, E, lane);
+        znext.read(nullptr, Z, lane);
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                dO[rt][r] = onext.value(rt, r);
-                E[rt][r] = vnext.value(rt, r) + znext.value(rt, r);
-            }
+            E[rt] += Z[rt];
         settled(dO);
         settled(E);
         lds_barrier();
@@ -262,6 +264,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
         if constexpr (!DMA)
             lds_barrier();
     }
+    lds_loads_done();   // (what was asked for once more: it must not land in the slab below, or in a later workgroup's LDS)
     if (chunks > 0)
         put(0);
     if (ga.dstate0)
@@ -672,11 +675,12 @@ void launch_scan_grad_sized(const GradArgs &a, hipStream_t stream)
     const int64_t chunks = scan_chunks(a.f.n_tokens, a.f.B);
     if (a.f.n_tokens > 0)
         launch_part(kvb_scan_prep_kernel<TIn, D, true>, true, false, chunks * a.f.Hv, 256, stream, a.f);
-    scan_split<TIn, D>(a.f, [&]<int NWV>(int64_t blocks) {
-        if (a.f.n_tokens > 0)
+    if (a.f.n_tokens > 0)
+        scan_split<TIn, D>(a.f, [&]<int NWV>(int64_t blocks) {
             launch_part(kvb_scan_kernel<TIn, float, D, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
-        launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, blocks, 64 * NWV, stream, a);
-    });
+        });
+    constexpr int NWV = D == 32 ? 2 : 4;   // (eight waves' slabs would not fit beside the images)
+    launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, (int64_t)a.f.B * a.f.Hv * (D / (16 * NWV)), 64 * NWV, stream, a);
     if (a.f.n_tokens > 0)
         launch_part(kvb_scan_grad_kernel<TIn, TOut, D>, false, true, chunks * a.f.Hk, 2 * D, stream, a);
 }

@@ -199,6 +199,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     constexpr int WORDS = SCAN_GATES / 4 + (STATES ? 1 : 2) * SCAN_MAT, PREP = STATES ? GRAD_PREP : SCAN_PREP;
     using Prep = Words<WORDS, NWV>;
     __shared__ uint4 kimgs[BUF][Tok::WORDS], qimgs[BUF][STATES ? 1 : Tok::WORDS], preps[BUF][WORDS];
+    __shared__ uint4 slabs[NWV][sizeof(TIn) == 2 || sizeof(TOut) == 2 ? 128 : 1];   // (values in, outputs out)
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
     const int b = unit / a.Hv, hv = unit - b * a.Hv, hk = hv / a.r;
@@ -223,12 +224,13 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     const float *prep = a.prep + ((size_t)first_chunk(span, b) * a.Hv + hv) * PREP;
     const size_t prep_step = (size_t)a.Hv * PREP;
     const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), vst = a.v_stride * sizeof(TIn), ost = a.Hv * D * sizeof(TOut);
-    const uint32_t vown = 4 * g * vst + col * sizeof(TIn), oown = 4 * g * ost + col * sizeof(TOut);
+    const uint32_t first = 16 * (part * NWV + wave);   // the wave's column
+    uint4 *slab = slabs[wave];
 
     const uint32_t kat = lds_at(kimgs[0]), qat = lds_at(qimgs[0]), pat = lds_at(preps[0]);
     Tok knext, qnext;   // (without DMA)
     Prep pnext;
-    Rows64<TIn> vnext;
+    Columns<TIn> vnext;
     int next = min(SC, span.len);   // tokens of the chunk to be asked for, which kp .. prep point to
     // What that needs, asked for in KS parts, one for each step of the products with the state: at once, the requests would
     // wait for each other at the memory unit and the wave with them.
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
             pnext.load(image, wave, lane);
         }
         if constexpr (PART == KS - 1)
-            vnext.load(head_rows<TIn, D>(vp, a.v_stride, next), anew(vown), vst);
+            vnext.request(head_rows<TIn, D>(vp, a.v_stride, next), slab, first * sizeof(TIn), vst, lane);
     };
     Pieces<FULL> sp[KS];   // of the state
 #pragma unroll
@@ -257,11 +259,11 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     const size_t own_chunk = (size_t)first_chunk(span, b) * a.Hv + hv;
     auto put = [&](int c) {   // (STATES: O holds Z)
         if constexpr (STATES) {
-            put_rows<float>(head_rows<float, D>(a.z + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, c < 0 ? 0 : SC), (4 * g * D + col) * 4, 4 * D, 1.0f, O);
+            Columns<float>::put(head_rows<float, D>(a.z + (own_chunk + (int64_t)c * a.Hv) * SC * D, D, c < 0 ? 0 : SC), nullptr, first * 4, 4 * D, 1.0f, O, lane);
             return;
         }
         TOut *p = static_cast<TOut *>(a.out) + ((int64_t)(span.first + c * SC) * a.Hv + hv) * D;
-        put_rows<TOut>(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), anew(oown), ost, a.scale, O);
+        Columns<TOut>::put(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), slab, first * sizeof(TOut), ost, a.scale, O, lane);
     };
     if (chunks > 0)
         static_for<KS>([&](auto step) { request(step, 0); });
@@ -269,20 +271,16 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         const int buf = DMA ? c & 1 : 0;
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = preps[buf] + SCAN_GATES / 4;
         const float4 *gate = reinterpret_cast<const float4 *>(preps[buf]);
-        if constexpr (DMA) {
+        if constexpr (DMA || Columns<TIn>::SLAB)
             lds_loads_done();
-        } else {
+        if constexpr (!DMA) {
             knext.store(kimgs[0], wave, lane);
             if constexpr (!STATES)
                 qnext.store(qimgs[0], wave, lane);
             pnext.store(preps[0], wave, lane);
         }
         f32x4_t E[4], y[4] = {};
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                E[rt][r] = vnext.value(rt, r);
+        vnext.read(slab, E, lane);
         settled(E);
         lds_barrier();
         if (c + 1 < chunks) {   // (the last chunk is asked for once more behind it)
@@ -439,6 +437,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         if constexpr (!DMA)
             lds_barrier();
     }
+    lds_loads_done();   // (what was asked for once more: it must not land in the slab below, or in a later workgroup's LDS)
     if (chunks > 0)
         put(chunks - 1);
     if (a.state1)
