@@ -584,10 +584,30 @@ __device__ __forceinline__ void load_pair(const uint4 *img, int i, int lane, uin
 template <typename TIn>
 constexpr int scan_bound(int waves) { return PIECES<TIn> == 1 ? 512 : 64 * waves; }
 
-// How a head's columns are split over workgroups, 16 a wave: f<waves of a workgroup>(workgroups).
-#ifndef WIDE_FROM
-#define WIDE_FROM 256
-#endif
+constexpr int SCAN_CUS = 256;   // compute units of the card
+
+// Up to how many tokens a sequence, on average, kvb_scan goes token by token: 0.3 to 0.8 us a token against a chunk's fixed work.
+// us, token by token against chunks, bf16, 32 v-heads of 128: 16 sequences of 1 token 14 / 38, of 4 18 / 38, of 8 23 / 38, of 16 33 / 41; one
+// sequence of 1 4 / 12, of 8 10 / 12, of 16 16 / 13.  4 and not 8, for the tokens may all be one sequence's, one after the other.
+constexpr int TOKEN_MAX = 4;
+
+// Whether a workgroup works out M and P of its chunks itself, in one launch instead of two: for about a chunk a sequence, and workgroups
+// that each find a free compute unit (both halves of a head's columns do that work).  us, alone against two launches, bf16, d = 128: 1
+// sequence of 37 tokens, 32 v-heads 13.9 / 16.4; 8 of 64, 8 v-heads 15.5 / 19.3; 1 of 128, 32 v-heads 25.8 / 21.6; 32 of 64 (2048 workgroups)
+// 122 / 87; 4 of 60, 8 v-heads, fp32, d = 64 14.7 / 18.0.  fp32 at d = 128 has no room for it in LDS, d = 32 too few waves.
+template <typename TIn, int D>
+constexpr bool CAN_ALONE = D >= 64 && sizeof(TIn) * D < 512;
+template <int D>
+bool scan_alone(const ScanArgs &a)
+{
+    return a.n_tokens <= (int64_t)SC * a.B && (int64_t)a.B * a.Hv * (D / 64) <= SCAN_CUS;
+}
+
+// How a head's columns are split over workgroups, 16 a wave: f<waves of a workgroup>(workgroups).  LDS has room for one workgroup a
+// compute unit.  While there are units for all workgroups of four waves, those are faster (more units at work); from there on those of eight (a
+// unit does more at a time, and M and P are read once a head).  us, eight against four, 512 tokens, bf16, d = 128: 64 v-heads in all 66 / 53,
+// 128 79 / 68, 192 95 / 113, 256 110 / 126, 512 215 / 240.  With more pieces the images of eight waves' work leave no room for a second
+// buffer's registers, and four it is.
 template <typename TIn, int D, typename F>
 void scan_split(const ScanArgs &a, F &&f)
 {
@@ -597,7 +617,7 @@ void scan_split(const ScanArgs &a, F &&f)
     } else if constexpr (D == 64 || PIECES<TIn> > 1) {
         f.template operator()<4>(heads * (D / 64));
     } else {
-        if (heads >= WIDE_FROM)
+        if (2 * heads > SCAN_CUS)
             f.template operator()<8>(heads);
         else
             f.template operator()<4>(heads * 2);

@@ -677,7 +677,7 @@ void launch_scan_grad_sized(const GradArgs &a, hipStream_t stream)
         launch_part(kvb_scan_prep_kernel<TIn, D, true>, true, false, chunks * a.f.Hv, 256, stream, a.f);
     if (a.f.n_tokens > 0)
         scan_split<TIn, D>(a.f, [&]<int NWV>(int64_t blocks) {
-            launch_part(kvb_scan_kernel<TIn, float, D, NWV, true>, false, false, blocks, 64 * NWV, stream, a.f);
+            launch_part(kvb_scan_kernel<TIn, float, D, NWV, true, false>, false, false, blocks, 64 * NWV, stream, a.f);
         });
     constexpr int NWV = D == 32 ? 2 : 4;   // (eight waves' slabs would not fit beside the images)
     launch_part(kvb_scan_reverse_kernel<TIn, TOut, D, NWV>, a.f.n_tokens == 0, a.f.n_tokens == 0, (int64_t)a.f.B * a.f.Hv * (D / (16 * NWV)), 64 * NWV, stream, a);

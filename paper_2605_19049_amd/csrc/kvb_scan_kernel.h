@@ -2,7 +2,7 @@
 #ifndef KVB_SCAN_KERNEL_H
 #define KVB_SCAN_KERNEL_H
 
-#include "kvb_scan_device.h"
+#include "kvb_scan_token_kernel.h"
 
 namespace kvb_impl {
 
@@ -12,21 +12,23 @@ namespace kvb_impl {
 // registers are its second operand as they stand, if row 4 g + r is taken for what lane group g sums in its r-th step.
 // GRAD: M, M' and P' without its diagonal, which goes to the gates, instead of M and P.
 // c is summed in fp64, so that differences of it are good to fp32 whatever its size; a decay below exp(-1e5) counts as that (zero).
+struct PrepScratch {
+    static constexpr int LD = SC + 4;
+    float gs[SC * LD], ps[SC * LD], td[4 * 16 * 20], beta[SC];
+    double cs[SC];
+};
+// (of the n tokens from `first` on, by 256 threads; what comes out goes to gates and mats, in LDS or in memory)
 template <typename TIn, int D, bool GRAD>
-__global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
+__device__ __forceinline__ void prep_chunk(const ScanArgs &a, int first, int n, int hv, PrepScratch &lds, float *gates, uint4 *mats)
 {
-    constexpr int LD = SC + 4, MATS = GRAD ? 3 : 2, PREP = GRAD ? GRAD_PREP : SCAN_PREP;
-    __shared__ float gs[SC * LD], ps[SC * LD], td[4 * 16 * 20], beta[SC];
-    __shared__ double cs[SC];
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
-    const int w = blockIdx.x / a.Hv, hv = blockIdx.x - w * a.Hv, hk = hv / a.r;
-    const ChunkAt at = chunk_at(a.start, a.n_tokens, a.B, w);
-    if (at.n == 0)
-        return;
-    const size_t tok = (size_t)(at.first + min(lane, at.n - 1)) * a.Hv + hv;
+    constexpr int LD = PrepScratch::LD, MATS = GRAD ? 3 : 2;
+    float *gs = lds.gs, *ps = lds.ps, *td = lds.td, *beta = lds.beta;
+    double *cs = lds.cs;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16, hk = hv / a.r;
+    const size_t tok = (size_t)(first + min(lane, n - 1)) * a.Hv + hv;
     const float g1 = a.g[tok], b1 = a.beta[tok];
-    const Buffer k = head_rows<TIn, D>(static_cast<const TIn *>(a.k) + at.first * a.k_stride + hk * D, a.k_stride, at.n);
-    const Buffer q = head_rows<TIn, D>(static_cast<const TIn *>(a.q) + at.first * a.q_stride + hk * D, a.q_stride, at.n);
+    const Buffer k = head_rows<TIn, D>(static_cast<const TIn *>(a.k) + first * a.k_stride + hk * D, a.k_stride, n);
+    const Buffer q = head_rows<TIn, D>(static_cast<const TIn *>(a.q) + first * a.q_stride + hk * D, a.q_stride, n);
     const uint32_t kst = a.k_stride * sizeof(TIn), qst = a.q_stride * sizeof(TIn), col = 8 * g * sizeof(TIn);
     f32x4_t kk[4] = {}, qk[4] = {};
 #pragma unroll
@@ -47,21 +49,19 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
             mma(qk[nt], qa, b);
         }
     }
-    float *prep = a.prep + ((size_t)w * a.Hv + hv) * PREP;
-    const double c = sum_below(lane < at.n ? log2_gate(g1) : 0.0);
+    const double c = sum_below(lane < n ? log2_gate(g1) : 0.0);
     if (wave == 0) {
         const double last = __shfl(c, 63);
-        float *gates = prep;
-        const float bt = lane < at.n ? b1 : 0.0f;
+        const float bt = lane < n ? b1 : 0.0f;
         gates[lane] = decay(c);
-        gates[SC + lane] = lane < at.n ? decay(last - c) : 0.0f;
+        gates[SC + lane] = lane < n ? decay(last - c) : 0.0f;
         gates[2 * SC + lane] = bt;
         if (!GRAD)
             gates[3 * SC + lane] = 0.0f;
         cs[lane] = c;
         beta[lane] = bt;
     }
-    __syncthreads();
+    lds_barrier();
     float *gt = td + wave * 320;   // the transpose of the wave's diagonal block of G
 #pragma unroll
     for (int nt = 0; nt < 4; ++nt) {
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
                 gr[r] = i > j ? d * kk[nt][r] : 0.0f;
                 pr[r] = (GRAD ? i > j : i >= j) ? d * qk[nt][r] : 0.0f;
                 if (GRAD && i == j)
-                    prep[3 * SC + i] = qk[nt][r];
+                    gates[3 * SC + i] = qk[nt][r];
             }
             if (nt == wave)
                 *reinterpret_cast<float4 *>(gt + m * 20 + 4 * g) = make_float4(gr[0], gr[1], gr[2], gr[3]);
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
             gt[(4 * g + r) * 20 + m] = (4 * g + r == m ? 1.0f : 0.0f) + diag[r] * bm;
         }
     }
-    __syncthreads();
+    lds_barrier();
     f32x4_t mm[4], ym[4];   // block column `wave` of M, and beta M
 #pragma unroll
     for (int I = 0; I < 4; ++I) {
@@ -150,13 +150,13 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
             ym[I][r] = mm[I][r] * br[r];
         }
     }
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int I = 0; I < 4; ++I)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             gs[(16 * I + 4 * g + r) * LD + 16 * wave + m] = mm[I][r];
-    __syncthreads();
+    lds_barrier();
     for (int u = tid; u < MATS * SCAN_UNITS; u += 256) {
         const int of = u / SCAN_UNITS, t = (u - of * SCAN_UNITS) / 64;
         const float *from = (of == MATS - 1 ? ps : gs);
@@ -175,31 +175,47 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
         }
         uint4 p[FULL];
         cut8(x, p);
-        uint4 *to = reinterpret_cast<uint4 *>(prep + SCAN_GATES) + of * SCAN_MAT + u - of * SCAN_UNITS;
+        uint4 *to = mats + of * SCAN_MAT + u - of * SCAN_UNITS;
 #pragma unroll
         for (int j = 0; j < FULL; ++j)
             to[j * SCAN_UNITS] = p[j];
     }
 }
 
+template <typename TIn, int D, bool GRAD>
+__global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
+{
+    __shared__ PrepScratch lds;
+    const int w = blockIdx.x / a.Hv, hv = blockIdx.x - w * a.Hv;
+    const ChunkAt at = chunk_at(a.start, a.n_tokens, a.B, w);
+    if (at.n == 0)
+        return;
+    float *prep = a.prep + ((size_t)w * a.Hv + hv) * (GRAD ? GRAD_PREP : SCAN_PREP);
+    prep_chunk<TIn, D, GRAD>(a, at.first, at.n, hv, lds, prep, reinterpret_cast<uint4 *>(prep + SCAN_GATES));
+}
+
 // The state from chunk to chunk: a workgroup has NWV waves of 16 columns each of one (sequence, v-head).
 // A wave keeps its columns of the state in its sums' registers for the whole sequence; the chunk's
 // K S and Q S, E and the state's update follow from each other within the wave.  What the next chunk needs from memory is
 // requested a chunk ahead.
+// ALONE: M and P are not there yet, the workgroup works them out itself chunk by chunk: for few chunks, one launch instead of two.
 // STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
 // than the decays, which a difference of E and V would lose).
-template <typename TIn, typename TOut, int D, int NWV, bool STATES>
-__global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const ScanArgs a)
+template <typename TIn, typename TOut, int D, int NWV, bool STATES, bool ALONE>
+__global__ __launch_bounds__(ALONE ? 256 : scan_bound<TIn>(NWV)) void kvb_scan_kernel(const ScanArgs a)
 {
     constexpr int KT = D / 16, KS = D / 32, SPLIT = D / (16 * NWV);
     using Tok = TokenTile<TIn, D, NWV>;
     constexpr int NP = Tok::NP;
     constexpr bool DMA = NP == 1;   // keys and queries are operands as they come: all images go to LDS without passing registers, into
-    constexpr int BUF = DMA ? 2 : 1;     // one buffer while the other is in use
+    constexpr int BUF = DMA && !ALONE ? 2 : 1;   // one buffer while the other is in use
+    static_assert(!ALONE || (NWV == 4 && !STATES));
     constexpr int WORDS = SCAN_GATES / 4 + (STATES ? 1 : 2) * SCAN_MAT, PREP = STATES ? GRAD_PREP : SCAN_PREP;
     using Prep = Words<WORDS, NWV>;
     __shared__ uint4 kimgs[BUF][Tok::WORDS], qimgs[BUF][STATES ? 1 : Tok::WORDS], preps[BUF][WORDS];
     __shared__ uint4 slabs[NWV][sizeof(TIn) == 2 || sizeof(TOut) == 2 ? 128 : 1];   // (values in, outputs out)
+    struct Nothing {};
+    __shared__ std::conditional_t<ALONE, PrepScratch, Nothing> scratch;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
     const int b = unit / a.Hv, hv = unit - b * a.Hv, hk = hv / a.r;
@@ -235,18 +251,20 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
     // What that needs, asked for in KS parts, one for each step of the products with the state: at once, the requests would
     // wait for each other at the memory unit and the wave with them.
     auto request = [&](auto step, int buf) {
-        constexpr int PART = step();
+        constexpr int PART = step(), KS = ALONE ? 1 : D / 32;
         const Buffer kb = head_rows<TIn, D>(kp, a.k_stride, next), qb = head_rows<TIn, D>(qp, a.q_stride, next), image(prep, 16 * WORDS);
         if constexpr (DMA) {
             Tok::template to_lds<PART, KS>(kb, kst, kat + buf * 16 * Tok::WORDS, wave, lane);
             if constexpr (!STATES)
                 Tok::template to_lds<PART, KS>(qb, qst, qat + buf * 16 * Tok::WORDS, wave, lane);
-            Prep::template to_lds<PART, KS>(image, pat + buf * 16 * WORDS, wave, lane);
+            if constexpr (!ALONE)
+                Prep::template to_lds<PART, KS>(image, pat + buf * 16 * WORDS, wave, lane);
         } else if constexpr (PART == 0) {
             knext.load(kb, kst, wave, lane);
             if constexpr (!STATES)
                 qnext.load(qb, qst, wave, lane);
-            pnext.load(image, wave, lane);
+            if constexpr (!ALONE)
+                pnext.load(image, wave, lane);
         }
         if constexpr (PART == KS - 1)
             vnext.request(head_rows<TIn, D>(vp, a.v_stride, next), slab, first * sizeof(TIn), vst, lane);
@@ -265,10 +283,15 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
         TOut *p = static_cast<TOut *>(a.out) + ((int64_t)(span.first + c * SC) * a.Hv + hv) * D;
         Columns<TOut>::put(head_rows<TOut, D>(p, (int64_t)a.Hv * D, c < 0 ? 0 : min(SC, span.len - c * SC)), slab, first * sizeof(TOut), ost, a.scale, O, lane);
     };
-    if (chunks > 0)
+    if (!ALONE && chunks > 0)
         static_for<KS>([&](auto step) { request(step, 0); });
     for (int c = 0; c < chunks; ++c) {
-        const int buf = DMA ? c & 1 : 0;
+        const int buf = BUF == 2 ? c & 1 : 0;
+        if constexpr (ALONE) {
+            lds_barrier();   // (the chunk before has been read)
+            request(std::integral_constant<int, 0>{}, 0);
+            prep_chunk<TIn, D, false>(a, span.first + c * SC, next, hv, scratch, reinterpret_cast<float *>(preps[0]), preps[0] + SCAN_GATES / 4);
+        }
         const uint4 *kimg = kimgs[buf], *qimg = qimgs[buf], *mats = preps[buf] + SCAN_GATES / 4;
         const float4 *gate = reinterpret_cast<const float4 *>(preps[buf]);
         if constexpr (DMA || Columns<TIn>::SLAB)
@@ -277,7 +300,8 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
             knext.store(kimgs[0], wave, lane);
             if constexpr (!STATES)
                 qnext.store(qimgs[0], wave, lane);
-            pnext.store(preps[0], wave, lane);
+            if constexpr (!ALONE)
+                pnext.store(preps[0], wave, lane);
         }
         f32x4_t E[4], y[4] = {};
         vnext.read(slab, E, lane);
@@ -336,7 +360,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                                   bt[h] = as_f32x4(gate[32 + 4 * h + g]);
                               }
                           }
-                          if constexpr (rt == 2)
+                          if constexpr (rt == 2 && !ALONE)
                               request(std::integral_constant<int, ks>{}, buf ^ 1);
                       });
         // O = Q S; Y = V - gamma y, the pieces of beta Y
@@ -434,7 +458,7 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
                       });
         if constexpr (KT == 2)
             static_for<4>([&](auto j) { sp[0].word(j(), S[0], S[1]); });
-        if constexpr (!DMA)
+        if constexpr (!DMA && !ALONE)
             lds_barrier();
     }
     lds_loads_done();   // (what was asked for once more: it must not land in the slab below, or in a later workgroup's LDS)
@@ -451,10 +475,19 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_kernel(const Sc
 template <typename TIn, typename TOut, int D>
 void launch_scan_sized(const ScanArgs &a, hipStream_t stream)
 {
-    if (a.n_tokens > 0)
-        launch_part(kvb_scan_prep_kernel<TIn, D, false>, true, false, scan_chunks(a.n_tokens, a.B) * a.Hv, 256, stream, a);
+    if (a.n_tokens <= TOKEN_MAX * (int64_t)a.B) {
+        launch_part(kvb_scan_token_kernel<TIn, TOut, D>, true, true, (int64_t)a.B * a.Hv * (D / 32), 64, stream, a);
+        return;
+    }
+    if constexpr (CAN_ALONE<TIn, D>) {
+        if (scan_alone<D>(a)) {
+            launch_part(kvb_scan_kernel<TIn, TOut, D, 4, false, true>, true, true, (int64_t)a.B * a.Hv * (D / 64), 256, stream, a);
+            return;
+        }
+    }
+    launch_part(kvb_scan_prep_kernel<TIn, D, false>, true, false, scan_chunks(a.n_tokens, a.B) * a.Hv, 256, stream, a);
     scan_split<TIn, D>(a, [&]<int NWV>(int64_t blocks) {
-        launch_part(kvb_scan_kernel<TIn, TOut, D, NWV, false>, a.n_tokens == 0, true, blocks, 64 * NWV, stream, a);
+        launch_part(kvb_scan_kernel<TIn, TOut, D, NWV, false, false>, false, true, blocks, 64 * NWV, stream, a);
     });
 }
 template <typename TIn, typename TOut>
