@@ -604,23 +604,27 @@ bool scan_alone(const ScanArgs &a)
 }
 
 // How a head's columns are split over workgroups, 16 a wave: f<waves of a workgroup>(workgroups).  LDS has room for one workgroup a
-// compute unit.  While there are units for all workgroups of four waves, those are faster (more units at work); from there on those of eight (a
-// unit does more at a time, and M and P are read once a head).  us, eight against four, 512 tokens, bf16, d = 128: 64 v-heads in all 66 / 53,
-// 128 79 / 68, 192 95 / 113, 256 110 / 126, 512 215 / 240.  With more pieces the images of eight waves' work leave no room for a second
-// buffer's registers, and four it is.
+// compute unit, so while there are units for all, fewer waves are faster: they share LDS with fewer others.  Beyond that eight: a
+// unit does more at a time, and M and P are read once a head.
+// us, bf16, d = 128, 32 v-heads, two waves against four: 1 sequence of 8191 tokens 523 / 558, of 512 43.7 / 46.6, 4 of 512 (two
+// rounds of workgroups) 93.6 / 67.1; eight against four: 2 of 512 66 / 53, 4 79 / 68, 6 95 / 113, 8 110 / 126, 16 215 / 240.
+// More than one piece passes through registers, and more of them with fewer waves: two against four, fp16, 1 of 2000 234 / 230, fp32, 1
+// of 500 86 / 81; eight waves' images and registers do not fit.
 template <typename TIn, int D, typename F>
 void scan_split(const ScanArgs &a, F &&f)
 {
     const int64_t heads = (int64_t)a.B * a.Hv;
     if constexpr (D == 32) {
         f.template operator()<2>(heads);
-    } else if constexpr (D == 64 || PIECES<TIn> > 1) {
-        f.template operator()<4>(heads * (D / 64));
+    } else if constexpr (PIECES<TIn> > 1) {
+        f.template operator()<4>(D / 64 * heads);
     } else {
-        if (2 * heads > SCAN_CUS)
+        if (D / 32 * heads <= SCAN_CUS)
+            f.template operator()<2>(D / 32 * heads);
+        else if (D == 64 || D / 64 * heads <= SCAN_CUS)
+            f.template operator()<4>(D / 64 * heads);
+        else if constexpr (D == 128)
             f.template operator()<8>(heads);
-        else
-            f.template operator()<4>(heads * 2);
     }
 }
 
