@@ -27,12 +27,16 @@ struct AcceptArgs {
     int32_t B, T, V, segments, segment;
 };
 
-// Segments of a row, each a workgroup.
+// Segments of a row, each a workgroup; 1: the whole of a request by one workgroup, in one launch instead of two.  A row is split where one
+// workgroup would read it for longer than a launch takes and the requests alone do not fill the card.  us, split against whole rows, 4 drafts, fp32:
+// 1 request of 32000 tokens 11.8 / 9.1, of 40000 11.0 / 10.0, of 65537 12.0 / 12.9, of 150001 12.6 / 20.3; 150001 tokens, 16 requests 14.3 / 21.3, 64
+// 21.9 / 23.8, 128 32.6 / 27.6; 16 of 1000000 34 / 105.  Segments of at least 8192 (16384: 32 of 150001 18.3, against 16.2), about 1024 in all.
 inline int accept_segments(int B, int V)
 {
-    const int most = V / 8192;
-    const int want = 1024 / (B < 1 ? 1 : B);
-    return most < 2 || want < 2 ? 1 : want < most ? want : most;
+    if (V < 32768 || B > 64)
+        return 1;
+    const int most = V / 8192, want = 1024 / (B < 1 ? 1 : B);
+    return want < most ? want : most;
 }
 inline int accept_segment(int V, int segments) { return ((V + segments - 1) / segments + 2047) / 2048 * 2048; }
 
