@@ -290,7 +290,7 @@ typedef struct kvb_seqs {
  * kvb_scan -- the recurrence over whole sequences of any length, the way a prompt that no record
  * buffer holds enters a state (and the forward pass of training).  From state0, for each token in order,
  *      e_t = v_t - alpha_t k_t S,  S <- alpha_t S + beta_t k_t^T e_t,  o_t = scale q_t S       (Eq. 11-12)
- * in chunks of 64 tokens with all arithmetic to fp32 (16-bit inputs are exact).
+ * in chunks of 64 tokens (a few tokens: one by one) with all arithmetic to fp32 (16-bit inputs are exact).
  *   q, k    device [n_tokens, Hk, dk] in_dtype     v  device [n_tokens, Hv, dv] in_dtype
  *   g, beta device [n_tokens, Hv] fp32
  *   state0  device [n_slots, Hv, dk, dv] fp32, or NULL: zero
@@ -319,8 +319,8 @@ int kvb_scan(const kvb_shape *shape, const kvb_seqs *seqs,
  *   dq, dk, dv  device, written: in_dtype, strides of q, k and v.  q and k of a qk-head get the sum over its v-heads
  *   dg, dbeta   device [n_tokens, Hv] fp32, written; dg is the gradient of the log decay
  *   dstate0  device [n_slots, Hv, dk, dv] fp32, written, or NULL: not wanted.  May be dstate1
- *   work     device, kvb_scan_backward_work(shape, seqs) bytes, 16-byte aligned: at d = 128 some 230 KB for each 64 tokens
- *            of a v-head, the two states at each chunk's start above all
+ *   work     device, kvb_scan_backward_work(shape, seqs) bytes, 16-byte aligned: at d = 128 some 257 KB for each 64 tokens
+ *            of a v-head, the state and its gradient at each chunk's start above all (kvb_scan: 37 KB)
  * Rows of skipped sequences are not written.  The same inputs give the same bits.  16-bit gradients are rounded once from sums to
  * within 2^-16 of their terms (dq: 2^-24), all else is held to fp32.
  */

@@ -28,12 +28,13 @@ struct AcceptArgs {
 };
 
 // Segments of a row, each a workgroup; 1: the whole of a request by one workgroup, in one launch instead of two.  A row is split where one
-// workgroup would read it for longer than a launch takes and the requests alone do not fill the card.  us, split against whole rows, 4 drafts, fp32:
-// 1 request of 32000 tokens 11.8 / 9.1, of 40000 11.0 / 10.0, of 65537 12.0 / 12.9, of 150001 12.6 / 20.3; 150001 tokens, 16 requests 14.3 / 21.3, 64
-// 21.9 / 23.8, 128 32.6 / 27.6; 16 of 1000000 34 / 105.  Segments of at least 8192 (16384: 32 of 150001 18.3, against 16.2), about 1024 in all.
+// workgroup would read it for longer than a launch takes and the requests alone do not fill the card.  us, split against whole rows, 4 drafts,
+// fp32, nothing in the caches: 1 request of 32000 tokens 11.1 / 8.9, of 40000 10.7 / 10.5; 64 requests of 32000 15.5 / 11.0, of 65537 16.2 / 17.9, of
+// 150001 22.5 / 31.8; 128 of 65537 21.5 / 18.5, of 150001 35.7 / 38.5; 256 of 150001, bf16, 48.5 / 41.3.  Segments of at least 8192 (16384: 32
+// of 150001 18.3, against 16.2), about 1024 in all.
 inline int accept_segments(int B, int V)
 {
-    if (V < 32768 || B > 64)
+    if (V < 32768 || B > (V < 131072 ? 64 : 128))
         return 1;
     const int most = V / 8192, want = 1024 / (B < 1 ? 1 : B);
     return want < most ? want : most;

@@ -7,6 +7,9 @@
 //   kvb_verify_kernel.h  kvb_verify_mfma_kernel; instantiated by kvb_verify_bf16.hip, _f16.hip, _f32.hip
 //   kvb_flush.hip        kvb_flush_mfma_kernel, kvb_flush_rows_kernel, kvb_compact_kernel
 //   kvb_direct.hip       kvb_direct_mfma_kernel, kvb_direct_rows_kernel
+//   kvb_scan_device.h    whole sequences: kvb_scan_kernel.h (kvb_scan_prep_kernel, kvb_scan_kernel), kvb_scan_token_kernel.h,
+//                        kvb_scan_grad_kernel.h (kvb_scan_reverse_kernel, kvb_scan_grad_kernel); instantiated by kvb_scan_*.hip
+//   kvb_accept.hip       kvb_accept_row_kernel, kvb_accept_sum_kernel, kvb_accept_find_kernel
 //   kvb_api.hip          argument checks, the extern "C" entry points, the kernel timer
 //
 // Element types (Sec. 4.1: 16-bit vectors and records beside a fp32 state): TIn is the type of

@@ -8,8 +8,9 @@
 // (1 + G beta)^-1 = 1 + M beta with a strictly lower triangular M that does not depend on the state or on V, so
 //   kvb_scan_prep_kernel   works out M and P of all chunks side by side,
 //   kvb_scan_kernel        passes the state from chunk to chunk; the columns of the state do not mix, so
-//                          a wave takes 16 or 32 of them and is on its own but for the keys, queries, M and P, which the
-//                          waves of a workgroup share in LDS.
+//                          a wave takes 16 of them and is on its own but for the keys, queries, M and P, which the
+//                          waves of a workgroup share in LDS,
+//   kvb_scan_token_kernel  does without chunks where there are only a few tokens a sequence.
 //
 // Precision.  All products are taken on the bf16 matrix instruction with fp32 sums, at 16 times the rate of the fp32 one.  A fp32
 // factor is cut into three bf16 pieces (8 bits each: the pieces' sum is the value), a bf16 input is one piece and exact, a

@@ -11,6 +11,10 @@ namespace kvb_impl {
 // blocks below its own,  M_IJ = -(1 + M_II beta) (G_IJ + sum_K G_IK beta M_KJ),  on the fp32 matrix instruction: the sums'
 // registers are its second operand as they stand, if row 4 g + r is taken for what lane group g sums in its r-th step.
 // GRAD: M, M' and P' without its diagonal, which goes to the gates, instead of M and P.
+// Bounded by latency: some 30 dependent steps (products, the diagonal block's 15 columns, the blocks below) with four LDS round trips between, 8 us
+// for a chunk alone, and by its 37 KB of output where there are many.  Three workgroups a compute unit cover each other: 4096 units
+// (8191 tokens, 32 v-heads, d = 128) 82 us, 20 ns each.  Working M and P out once for all columns of a head, beside the chain over the
+// chunks and not in it, is what the split is for: 64 x 64 triangles cost a wave as much as its share of a chunk.
 // c is summed in fp64, so that differences of it are good to fp32 whatever its size; a decay below exp(-1e5) counts as that (zero).
 struct PrepScratch {
     static constexpr int LD = SC + 4;
@@ -196,8 +200,12 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 
 // The state from chunk to chunk: a workgroup has NWV waves of 16 columns each of one (sequence, v-head).
 // A wave keeps its columns of the state in its sums' registers for the whole sequence; the chunk's
-// K S and Q S, E and the state's update follow from each other within the wave.  What the next chunk needs from memory is
-// requested a chunk ahead.
+// K S and Q S, E and the state's update follow from each other within the wave, and the sums' registers are the next product's second operand
+// as they stand.  What the next chunk needs from memory is requested a chunk ahead.
+// Bounded by the chain of a chunk's products in a wave: 3.6 us a chunk, of which the matrix instructions are busy 1.3 (three pieces of the state
+// against one of the keys), cutting into pieces takes 0.6, requests and stores 0.9, the rest are waits for LDS and for sums.  Few sequences
+// leave most of the card idle: one of 8191 tokens, 32 v-heads, d = 128 470 us on 128 compute units, 128 chunks one after the other (55 Tflop/s
+// of the recurrence); 24 ragged ones of 1500 340 us on all of them (166 Tflop/s, 1.6 TB/s).
 // ALONE: M and P are not there yet, the workgroup works them out itself chunk by chunk: for few chunks, one launch instead of two.
 // STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
 // than the decays, which a difference of E and V would lose).

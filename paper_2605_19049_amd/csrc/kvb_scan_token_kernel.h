@@ -3,7 +3,8 @@
 // Everything is fp32 and on the vector units.  A call reads and writes the states and little else (4 d^2 bytes each way for each
 // v-head, against 6 d bytes of a bf16 token), so what counts is that all of a state is on its way before anything waits: a wave
 // has 32 columns, 4 of them and d / 8 rows a lane, asks for them in d / 8 loads of 16 bytes (128 bytes in a row from 8 lanes) and
-// needs no other wave.  A token then costs one pass over the registers for y and S'q and three additions across 8 lanes.
+// needs no other wave.  Measured: 16 single tokens of 32 v-heads of 128, 67.6 MB, 14.1 us or 4.8 TB/s (a copy of 1 GiB: 5.2 TB/s); 1 token
+// 3.9 us, which is launch and latency.  A token then costs one pass over the registers for y and S'q and three additions across 8 lanes.
 #ifndef KVB_SCAN_TOKEN_KERNEL_H
 #define KVB_SCAN_TOKEN_KERNEL_H
 
