@@ -77,6 +77,21 @@ __device__ __forceinline__ int state_row(const int32_t *slot, int n_slots, int b
     return s >= 0 && s < n_slots ? s : -1;
 }
 
+// Workgroup w of those that `parts` each of `units` need, which read the same keys and queries: consecutive workgroups go to the eight XCDs in
+// turn, so the parts of a unit are dealt eight apart and meet in one L2.  The units behind the last whole eight are dealt as they come.
+// us, against parts that follow each other, bf16, d = 128: kvb_scan_reverse_kernel, 4 sequences of 2048 tokens 234 / 241, kvb_scan_kernel, one of 8191 462 / 470.
+struct Dealt {
+    int unit, part;
+};
+__device__ __forceinline__ Dealt dealt(int w, int units, int parts)
+{
+    const int whole = units / 8 * 8, rest = w - whole * parts;
+    if (rest >= 0)
+        return Dealt{whole + rest / parts, rest % parts};
+    const int eight = w / (8 * parts), in = w - eight * 8 * parts;
+    return Dealt{8 * eight + in % 8, in / 8};
+}
+
 struct ChunkAt {
     int b, first, n;   // n = 0: nothing there
 };

@@ -22,8 +22,8 @@
 namespace kvb_impl {
 
 // From the last chunk to the first: dS in the sums' registers, as the state in kvb_scan_kernel.  Bounded by the chain of a chunk's products, like that,
-// and by what it leaves for the next kernel (dS and D, 96 KB a chunk and head at d = 128): 4 sequences of 2048 tokens, 32 v-heads, bf16 240 us, 7.5 us a
-// chunk, 0.7 GB, 2.9 TB/s.  States ahead of and gradients behind each chunk are stored because the chunks' other gradients are then
+// and by what it leaves for the next kernel (dS and D, 96 KB a chunk and head at d = 128): 4 sequences of 2048 tokens, 32 v-heads, bf16 234 us, 7.3 us a
+// chunk, 0.85 GB read and 0.5 written, 5.7 TB/s, some of it from the last-level cache.  States ahead of and gradients behind each chunk are stored because the chunks' other gradients are then
 // independent; working them out again would put two more chains in front of kvb_scan_grad_kernel.
 template <typename TIn, typename TOut, int D, int NWV>
 __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(const GradArgs ga)
@@ -39,8 +39,8 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
     __shared__ uint4 slabs[NWV][sizeof(TIn) == 2 ? 128 : 1], oslabs[NWV][sizeof(TOut) == 2 ? 128 : 1];   // (values in, their gradients out; the outputs' in)
     const ScanArgs &a = ga.f;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
-    const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
-    const int b = unit / a.Hv, hv = unit - b * a.Hv, hk = hv / a.r;
+    const Dealt at = dealt(blockIdx.x, a.B * a.Hk, a.r * SPLIT);
+    const int b = at.unit / a.Hk, hk = at.unit - b * a.Hk, hv = hk * a.r + at.part / SPLIT, part = at.part % SPLIT;
     const int row = state_row(a.slot, a.n_slots, b);
     if (row < 0)
         return;
@@ -279,8 +279,8 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
 // transposes: dQ' = S0 dO' and so on have the state's rows as first operand, which each wave reads from memory once, and
 // the tokens' rows (dO, E, dV) as second, from LDS.  The two 64 x 64 matrices are worked out a tile column a
 // wave, transposed; their sums' registers, two tiles together, are a second operand for W K, and read back transposed one for W' Q.
-// Bounded by latency, one workgroup of four waves a compute unit (some 500 registers a wave: all of dQ, dK and the products in flight; 61 % of a wave's
-// life is waiting): the example above 375 us, 0.85 GB read, 2.3 TB/s.  A qk-head a workgroup, not a v-head, makes dQ and dK sums in a fixed order
+// Bounded by memory and its latency, one workgroup of four waves a compute unit (some 500 registers a wave: all of dQ, dK and the products in flight;
+// 42 % of a wave's life is waiting for loads): the example above 376 us, 1.35 GB read, 3.8 TB/s.  A qk-head a workgroup, not a v-head, makes dQ and dK sums in a fixed order
 // without atomics or another pass.
 // Products that only dK depends on keep 2^-16 of a term for 16-bit dK; dQ is needed to fp32 for dg.
 template <typename TIn, typename TOut, int D>

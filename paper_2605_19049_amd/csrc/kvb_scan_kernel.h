@@ -202,9 +202,9 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 // A wave keeps its columns of the state in its sums' registers for the whole sequence; the chunk's
 // K S and Q S, E and the state's update follow from each other within the wave, and the sums' registers are the next product's second operand
 // as they stand.  What the next chunk needs from memory is requested a chunk ahead.
-// Bounded by the chain of a chunk's products in a wave: 3.6 us a chunk, of which the matrix instructions are busy 1.3 (three pieces of the state
+// Bounded by the chain of a chunk's products in a wave: 3.6 us a chunk, of which the matrix instructions are busy 1.5 (three pieces of the state
 // against one of the keys), cutting into pieces takes 0.6, requests and stores 0.9, the rest are waits for LDS and for sums.  Few sequences
-// leave most of the card idle: one of 8191 tokens, 32 v-heads, d = 128 470 us on 128 compute units, 128 chunks one after the other (55 Tflop/s
+// leave most of the card idle: one of 8191 tokens, 32 v-heads, d = 128 462 us on 128 compute units, 128 chunks one after the other (55 Tflop/s
 // of the recurrence); 24 ragged ones of 1500 340 us on all of them (166 Tflop/s, 1.6 TB/s).
 // ALONE: M and P are not there yet, the workgroup works them out itself chunk by chunk: for few chunks, one launch instead of two.
 // STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
@@ -225,8 +225,8 @@ __global__ __launch_bounds__(ALONE ? 256 : scan_bound<TIn>(NWV)) void kvb_scan_k
     struct Nothing {};
     __shared__ std::conditional_t<ALONE, PrepScratch, Nothing> scratch;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
-    const int unit = blockIdx.x / SPLIT, part = blockIdx.x % SPLIT;
-    const int b = unit / a.Hv, hv = unit - b * a.Hv, hk = hv / a.r;
+    const Dealt at = dealt(blockIdx.x, a.B * a.Hk, a.r * SPLIT);
+    const int b = at.unit / a.Hk, hk = at.unit - b * a.Hk, hv = hk * a.r + at.part / SPLIT, part = at.part % SPLIT;
     const int row = state_row(a.slot, a.n_slots, b);
     if (row < 0)
         return;
