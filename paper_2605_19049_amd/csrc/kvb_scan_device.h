@@ -79,7 +79,8 @@ __device__ __forceinline__ int state_row(const int32_t *slot, int n_slots, int b
 
 // Workgroup w of those that `parts` each of `units` need, which read the same keys and queries: consecutive workgroups go to the eight XCDs in
 // turn, so the parts of a unit are dealt eight apart and meet in one L2.  The units behind the last whole eight are dealt as they come.
-// us, against parts that follow each other, bf16, d = 128: kvb_scan_reverse_kernel, 4 sequences of 2048 tokens 234 / 241, kvb_scan_kernel, one of 8191 462 / 470.
+// us, against parts that follow each other, bf16, d = 128: kvb_scan_reverse_kernel, 4 sequences of 2048 tokens 234 / 241, kvb_scan_kernel, one of 8191 462 / 470
+// (0.29 GB read through the fabric, 1.29).
 struct Dealt {
     int unit, part;
 };

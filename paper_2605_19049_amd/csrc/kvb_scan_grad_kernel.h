@@ -23,7 +23,7 @@ namespace kvb_impl {
 
 // From the last chunk to the first: dS in the sums' registers, as the state in kvb_scan_kernel.  Bounded by the chain of a chunk's products, like that,
 // and by what it leaves for the next kernel (dS and D, 96 KB a chunk and head at d = 128): 4 sequences of 2048 tokens, 32 v-heads, bf16 234 us, 7.3 us a
-// chunk, 0.85 GB read and 0.5 written, 5.7 TB/s, some of it from the last-level cache.  States ahead of and gradients behind each chunk are stored because the chunks' other gradients are then
+// chunk, 0.54 GB read and 0.49 written, 4.4 TB/s.  States ahead of and gradients behind each chunk are stored because the chunks' other gradients are then
 // independent; working them out again would put two more chains in front of kvb_scan_grad_kernel.
 template <typename TIn, typename TOut, int D, int NWV>
 __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(const GradArgs ga)
@@ -280,7 +280,8 @@ __global__ __launch_bounds__(scan_bound<TIn>(NWV)) void kvb_scan_reverse_kernel(
 // the tokens' rows (dO, E, dV) as second, from LDS.  The two 64 x 64 matrices are worked out a tile column a
 // wave, transposed; their sums' registers, two tiles together, are a second operand for W K, and read back transposed one for W' Q.
 // Bounded by memory and its latency, one workgroup of four waves a compute unit (some 500 registers a wave: all of dQ, dK and the products in flight;
-// 42 % of a wave's life is waiting for loads): the example above 376 us, 1.35 GB read, 3.8 TB/s.  A qk-head a workgroup, not a v-head, makes dQ and dK sums in a fixed order
+// 39 % of a wave's life is waiting for loads): the example above 358 us, 1.24 GB read, 3.7 TB/s (keys and queries asked for anew for each
+// v-head 376 us, 1.35 GB).  A qk-head a workgroup, not a v-head, makes dQ and dK sums in a fixed order
 // without atomics or another pass.
 // Products that only dK depends on keep 2^-16 of a term for 16-bit dK; dQ is needed to fp32 for dg.
 template <typename TIn, typename TOut, int D>
@@ -294,11 +295,15 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
     constexpr bool APART = D < 128;
     constexpr int BESIDE = ONE > 2 * NP * ROWS ? ONE : 2 * NP * ROWS;
     constexpr int UNROLL = NP == FULL ? 1 : KS;   // (registers)
-    __shared__ uint4 lds[APART ? BESIDE + (FULL + LK) * W : ONE > TWO ? ONE : TWO];
+    constexpr int SHARED = APART ? BESIDE + (FULL + LK) * W : ONE > TWO ? ONE : TWO;
+    // bf16: what the next v-head's start needs from memory is asked for while this one's products with matrices run, its states a step
+    // ahead (with more pieces there are no registers for it), and keys and queries stay in LDS for all v-heads (nor room for that).
+    constexpr bool AHEAD = NP == 1 && NO == 1;
+    __shared__ uint4 lds[SHARED + (AHEAD ? 2 * ROWS : 0)];
     __shared__ float sums[5][4][SC], square[4];   // the tokens' dO'.E, Z.dV and Q.dQ', E.D' and E.(rest K dS1), and <dS1, S0>, by waves
     __shared__ double cs[SC];
     uint4 *oimg = lds, *eimg = oimg + NO * ROWS, *vimg = eimg + FULL * ROWS;
-    uint4 *w1 = lds + (APART ? BESIDE : 0), *w2 = w1 + FULL * W, *kimg = APART ? lds : w2 + LK * W, *qimg = kimg + NP * ROWS;
+    uint4 *w1 = lds + (APART ? BESIDE : 0), *w2 = w1 + FULL * W, *kimg = AHEAD ? lds + SHARED : APART ? lds : w2 + LK * W, *qimg = kimg + NP * ROWS;
     const ScanArgs &a = ga.f;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, m = lane % 16, g = lane / 16;
     const int w = blockIdx.x / a.Hk, hk = blockIdx.x - w * a.Hk;
@@ -311,9 +316,6 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
     Tok kt, qt;
     f32x4_t dq[2][4] = {}, dk[2][4] = {};
     const int mine = 32 * wave + 8 * g;   // the lane's first column: of the rows it stages and of what it stores
-    // What the next v-head's start needs from memory is asked for while this one's products with matrices run (bf16: with more
-    // pieces there are no registers for it), and its states a step ahead (fp32: when they are needed).
-    constexpr bool AHEAD = NP == 1 && NO == 1;
     Raw8<TIn> v[4];
     Raw8<TOut> o[4];
     Raw8<float> z[4], d[4], sraw[2][2], draw[2][2];
@@ -352,8 +354,13 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
             draw[to][t] = load_raw8<float>(dsb, from);
         }
     };
-    if constexpr (AHEAD)
+    if constexpr (AHEAD) {
+        kt.load(kb, kst, wave, lane);
+        qt.load(qb, qst, wave, lane);
         load_head(0);
+        kt.store(kimg, wave, lane);
+        qt.store(qimg, wave, lane);
+    }
     for (int h = 0; h < a.r; ++h) {
         const int hv = hk * a.r + h;
         const size_t unit = (size_t)w * a.Hv + hv;
@@ -465,10 +472,6 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
             sq += __shfl_xor(sq, s);
         if (lane == 0)
             square[wave] = sq;
-        if constexpr (AHEAD) {
-            kt.load(kb, kst, wave, lane);
-            qt.load(qb, qst, wave, lane);
-        }
         auto put_matrices = [&](int it, const f32x4_t (&y1)[4], const f32x4_t (&y2)[4]) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -547,9 +550,9 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
         if constexpr (!AHEAD) {
             kt.load(kb, kst, wave, lane);
             qt.load(qb, qst, wave, lane);
+            kt.store(kimg, wave, lane);
+            qt.store(qimg, wave, lane);
         }
-        kt.store(kimg, wave, lane);
-        qt.store(qimg, wave, lane);
         const float beta_now[4] = {beta[0], beta[1], beta[2], beta[3]};
         if constexpr (AHEAD)
             load_head(min(h + 1, a.r - 1));
@@ -618,8 +621,16 @@ __global__ __launch_bounds__(2 * D, 1) void kvb_scan_grad_kernel(const GradArgs 
 #pragma unroll
         for (int nt = 0; nt < 4; ++nt) {
             float x[8], y[8], dot = 0.0f, oe = 0.0f;
-            unpack8(load_raw8<TIn>(qb, (16 * nt + m) * qst + mine * (uint32_t)sizeof(TIn)), x);
-            unpack8(load_raw8<TIn>(kb, (16 * nt + m) * kst + mine * (uint32_t)sizeof(TIn)), y);
+            if constexpr (AHEAD) {   // (their images as first operands: 8 columns of a token a lane)
+                uint4 fq[1], fk[1];
+                Tok::rows(qimg, nt, wave, lane, fq);
+                Tok::rows(kimg, nt, wave, lane, fk);
+                unpack8(Raw8<TIn>{fq[0]}, x);
+                unpack8(Raw8<TIn>{fk[0]}, y);
+            } else {
+                unpack8(load_raw8<TIn>(qb, (16 * nt + m) * qst + mine * (uint32_t)sizeof(TIn)), x);
+                unpack8(load_raw8<TIn>(kb, (16 * nt + m) * kst + mine * (uint32_t)sizeof(TIn)), y);
+            }
 #pragma unroll
             for (int v = 0; v < NWV; ++v)
                 oe += sums[0][v][16 * nt + m];

@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 // as they stand.  What the next chunk needs from memory is requested a chunk ahead.
 // Bounded by the chain of a chunk's products in a wave: 3.6 us a chunk, of which the matrix instructions are busy 1.5 (three pieces of the state
 // against one of the keys), cutting into pieces takes 0.6, requests and stores 0.9, the rest are waits for LDS and for sums.  Few sequences
-// leave most of the card idle: one of 8191 tokens, 32 v-heads, d = 128 462 us on 128 compute units, 128 chunks one after the other (55 Tflop/s
+// leave most of the card idle: one of 8191 tokens, 32 v-heads, d = 128 455 us on 128 compute units, 128 chunks one after the other (55 Tflop/s
 // of the recurrence); 24 ragged ones of 1500 340 us on all of them (166 Tflop/s, 1.6 TB/s).
 // ALONE: M and P are not there yet, the workgroup works them out itself chunk by chunk: for few chunks, one launch instead of two.
 // STATES: for the gradients, no outputs; the state ahead of each chunk and Z = E - V go to the workspace (E - V is no larger
