@@ -355,7 +355,8 @@ typedef struct kvb_vocab {
  *   path     device int32 [B, T]: the accepted drafts, oldest first, then -1: kvb_compact's path
  *   accepted device int32 [B]: how many: kvb_compact's path_len, kvb_flush's accepted
  *   token    device int32 [B]: the token that follows the last accepted draft
- *   work     device, kvb_accept_work(vocab) bytes, 8-byte aligned; what it holds means nothing before and after the call
+ *   work     device, kvb_accept_work(vocab) bytes, 8-byte aligned; what it holds means nothing before and after the call.
+ *            kvb_accept_work grows with B and V: what it gives for the largest batch serves smaller ones
  * The walk starts at row 0 with r = the row and Z = 1 and looks at the drafts in order; draft i is tested if its parent is where
  * the walk stands.  It is accepted if u_i q_i(x_i) Z < r(x_i); then the walk stands at it, r is its row and Z = 1.
  * Otherwise r becomes max(r - Z q_i, 0) and Z its sum; for chosen drafts r(x_i) becomes 0 and Z loses what it was.  The token is

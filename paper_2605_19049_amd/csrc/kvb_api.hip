@@ -225,10 +225,7 @@ extern "C" {
 int64_t kvb_accept_work(const kvb_vocab *vocab)
 {
     const int rc = check_vocab(vocab);
-    if (rc != KVB_OK)
-        return rc;
-    const int segments = accept_segments(vocab->B, vocab->V);
-    return (int64_t)vocab->B * (8 * segments + (segments > 1 ? 16 : 0));
+    return rc != KVB_OK ? rc : accept_work_bytes(vocab->B, vocab->V);
 }
 
 int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *parent, const int32_t *tokens, const void *target,
