@@ -1,0 +1,84 @@
+"""Tensors that do not lie as a scan's kvb_seqs says are refused by the binding (no GPU: calls of no sequences, which launch nothing)."""
+import pytest
+import torch
+
+from paper_2605_19049_amd import kvb
+
+N, Hk, Hv, D = 10, 2, 4, 64
+SH = kvb.shape(0, Hk, Hv, D, D, 1, kvb.F32)
+NAMES = ("q", "k", "v", "g", "beta", "state0", "dout", "dstate1", "dq", "dk", "dv", "dg", "dbeta", "dstate0")
+
+
+def projection(n=N):
+    """q, k and v as parts of the rows of one projection."""
+    return [x.view(n, -1, D) for x in torch.zeros(n, (2 * Hk + Hv) * D).split([Hk * D, Hk * D, Hv * D], dim=1)]
+
+
+def packed(n=N):
+    return [torch.zeros(n, h, D) for h in (Hk, Hk, Hv)]
+
+
+def arrays(rows, grads, n=N):
+    a = dict(zip("qkv", rows))
+    a.update(zip(("dq", "dk", "dv"), grads))
+    a.update({x: torch.zeros(n, Hv) for x in ("g", "beta", "dg", "dbeta")})
+    a.update({x: torch.zeros(1, Hv, D, D) for x in ("state0", "dstate1", "dstate0")})
+    a["dout"] = torch.zeros(n, Hv, D)
+    return a
+
+
+def backward(a, sq, bound):
+    args = [SH, sq] + [a[x] for x in NAMES] + [torch.zeros(64)]
+    if bound:
+        return kvb.bind("kvb_scan_backward", *args, 0)()
+    return kvb.kvb_scan_backward(*args, stream=0)
+
+
+def forward(a, sq, bound):
+    args = [SH, sq] + [a[x] for x in NAMES[:6]] + [a["state0"], a.get("out", a["dout"]), torch.zeros(64)]
+    if bound:
+        return kvb.bind("kvb_scan", *args, 0)()
+    return kvb.kvb_scan(*args, stream=0)
+
+
+def seqs(rows, n=N):
+    return kvb.seqs(torch.zeros(1, dtype=torch.int32), n, 1, **dict(zip("qkv", rows)))
+
+
+@pytest.mark.parametrize("bound", [False, True])
+def test_gradients_lie_as_their_inputs_do(bound):
+    q, k, v = projection()
+    sq = seqs((q, k, v))
+    assert sq.q_stride == (2 * Hk + Hv) * D
+    backward(arrays((q, k, v), projection()), sq, bound)
+    for i in range(3):   # (empty_like of a part of a row is packed: rows of the projection apart, its end would be written behind)
+        grads = projection()
+        grads[i] = torch.empty_like((q, k, v)[i])
+        with pytest.raises(ValueError):
+            backward(arrays((q, k, v), grads), sq, bound)
+    backward(arrays(packed(), packed()), seqs(packed()), bound)
+    backward(arrays(packed(), packed()), seqs([]), bound)
+    with pytest.raises(ValueError):
+        backward(arrays(packed(), projection()), seqs(packed()), bound)
+
+
+@pytest.mark.parametrize("bound", [False, True])
+@pytest.mark.parametrize("call", [forward, backward])
+def test_inputs_lie_as_their_sequences_say(call, bound):
+    for rows, said in ((projection(), packed()), (packed(), projection()), (projection(), [])):
+        with pytest.raises(ValueError):
+            call(arrays(rows, said or packed()), seqs(said), bound)
+    call(arrays(projection(), projection()), seqs(projection()), bound)
+    with pytest.raises(ValueError):   # heads that do not follow each other
+        call(arrays([x.transpose(0, 1).contiguous().transpose(0, 1) for x in packed()], packed()), seqs(packed()), bound)
+
+
+@pytest.mark.parametrize("bound", [False, True])
+def test_rows_without_heads_and_addresses(bound):
+    flat = [x.view(N, -1) for x in packed()]
+    backward(arrays(flat, flat), seqs([]), bound)
+    parts = [x.flatten(1) if x.is_contiguous() else x.as_strided((N, x.shape[1] * D), (x.stride(0), 1)) for x in projection()]
+    backward(arrays(parts, parts), seqs(projection()), bound)
+    with pytest.raises(ValueError):
+        backward(arrays(parts, flat), seqs(projection()), bound)
+    backward({x: 4096 for x in NAMES}, seqs(projection()), bound)
