@@ -242,11 +242,12 @@ def kvb_direct(sh, st, slot, lens, Lmax, q, k, v, g, beta, out, stream=None, che
 
 def _token_stride(x, what):
     """Elements from one token's row to the next of a [n_tokens, heads, d] tensor whose tokens are contiguous, 0 for up to one token."""
-    if x is None or x.shape[0] < 2:
+    if x is None or x.shape[0] == 0:
         return 0
-    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or x.stride(0) < x.shape[1] * x.shape[2]:
+    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or \
+            (x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2]):
         raise ValueError("%s of shape %s and stride %s: [n_tokens, heads, d] with contiguous tokens is wanted" % (what, tuple(x.shape), tuple(x.stride())))
-    return x.stride(0)
+    return x.stride(0) if x.shape[0] > 1 else 0
 
 
 def seqs(start, n_tokens, n_slots, slot=None, q=None, k=None, v=None):

@@ -82,3 +82,16 @@ def test_rows_without_heads_and_addresses(bound):
     with pytest.raises(ValueError):
         backward(arrays(parts, flat), seqs(projection()), bound)
     backward({x: 4096 for x in NAMES}, seqs(projection()), bound)
+
+
+@pytest.mark.parametrize("n", [1, 2])
+def test_heads_of_a_single_token_follow_each_other(n):
+    """A part of each head's row: heads 3 d apart, which no stride of a kvb_seqs says."""
+    x = torch.zeros(n, Hk, 3 * D)[:, :, :D]
+    for bad in (x, torch.zeros(n, Hk, 2 * D)[:, :, ::2], torch.zeros(n, Hk, 1).expand(n, Hk, D), torch.zeros(D, Hk, n).permute(2, 1, 0)):
+        with pytest.raises(ValueError):
+            kvb.seqs(0, n, 1, q=bad)
+        with pytest.raises(ValueError):
+            forward(arrays([bad] + packed(n)[1:], packed(n), n), seqs([], n), False)
+    assert kvb.seqs(0, n, 1, q=torch.zeros(n, 1, 3 * D)[:, :, :D]).q_stride == (0 if n == 1 else 3 * D)   # (one head: rows apart)
+    assert kvb.seqs(0, 0, 1, q=torch.zeros(0, Hk, D)).q_stride == 0
