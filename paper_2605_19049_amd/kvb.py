@@ -255,12 +255,19 @@ def seqs(start, n_tokens, n_slots, slot=None, q=None, k=None, v=None):
     return KvbSeqs(_ptr(start), _ptr(slot), _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v"), n_tokens, n_slots)
 
 
-def _check_rows(fn_name, args):
-    """ValueError where a tensor of a scan's token rows does not lie as the kvb_seqs says: the kernels would read or write other memory.
-    args: the C arguments.  Addresses are taken as they are."""
+_SCAN = ("q", "k", "v", "g", "beta", "state0", "state1", "out")
+_BACKWARD = _SCAN[:6] + ("dout", "dstate1", "dq", "dk", "dv", "dg", "dbeta", "dstate0")
+
+
+def _check_layouts(fn_name, args):
+    """ValueError where a tensor of a scan does not lie as the kvb_seqs says (q, k, v and their gradients) or packed (the others): the
+    kernels would read or write other memory.  args: the C arguments.  Addresses are taken as they are."""
     if fn_name not in ("kvb_scan", "kvb_scan_backward"):
         return
     sq, q, k, v = args[1:5]
+    for what, x in zip(_SCAN if fn_name == "kvb_scan" else _BACKWARD, args[2:]):
+        if what not in ("q", "k", "v", "dq", "dk", "dv") and hasattr(x, "stride") and not x.is_contiguous():
+            raise ValueError("%s of shape %s and stride %s is not contiguous" % (what, tuple(x.shape), tuple(x.stride())))
     rows = [("q", q, sq.q_stride), ("k", k, sq.k_stride), ("v", v, sq.v_stride)]
     if fn_name == "kvb_scan_backward":
         rows += [("d" + what, x, stride) for (what, _, stride), x in zip(rows, args[10:13])]
@@ -283,7 +290,7 @@ def scan_work(sh, sq):
 
 
 def kvb_scan(sh, sq, q, k, v, g, beta, state0, state1, out, work, stream=None, check=True):
-    _check_rows("kvb_scan", (sh, sq, q, k, v))
+    _check_layouts("kvb_scan", (sh, sq, q, k, v, g, beta, state0, state1, out))
     rc = lib().kvb_scan(ctypes.byref(sh), ctypes.byref(sq), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state0),
                         _ptr(state1), _ptr(out), _ptr(work), _stream(stream))
     return _check(rc, "kvb_scan", check)
@@ -295,8 +302,8 @@ def scan_backward_work(sh, sq):
 
 
 def kvb_scan_backward(sh, sq, q, k, v, g, beta, state0, dout, dstate1, dq, dk, dv, dg, dbeta, dstate0, work, stream=None, check=True):
-    """dq, dk, dv lie as q, k, v do (the strides in sq); ValueError for a tensor that does not."""
-    _check_rows("kvb_scan_backward", (sh, sq, q, k, v, g, beta, state0, dout, dstate1, dq, dk, dv))
+    """dq, dk, dv lie as q, k, v do (the strides in sq), the other arrays packed; ValueError for a tensor that does not."""
+    _check_layouts("kvb_scan_backward", (sh, sq, q, k, v, g, beta, state0, dout, dstate1, dq, dk, dv, dg, dbeta, dstate0))
     rc = lib().kvb_scan_backward(ctypes.byref(sh), ctypes.byref(sq), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state0), _ptr(dout),
                                  _ptr(dstate1), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dg), _ptr(dbeta), _ptr(dstate0), _ptr(work), _stream(stream))
     return _check(rc, "kvb_scan_backward", check)
@@ -323,7 +330,7 @@ def bind(fn_name, *args):
     same pointers (for serving loops, where per-call marshalling would rival a 20 us
     kernel).  `args` are exactly the C arguments; tensors, structs and ints are converted
     once.  The caller keeps the tensors and structs alive."""
-    _check_rows(fn_name, args)
+    _check_layouts(fn_name, args)
     fn = getattr(lib(), fn_name)
     conv = []
     for a, t in zip(args, fn.argtypes):

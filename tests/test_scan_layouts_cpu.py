@@ -95,3 +95,24 @@ def test_heads_of_a_single_token_follow_each_other(n):
             forward(arrays([bad] + packed(n)[1:], packed(n), n), seqs([], n), False)
     assert kvb.seqs(0, n, 1, q=torch.zeros(n, 1, 3 * D)[:, :, :D]).q_stride == (0 if n == 1 else 3 * D)   # (one head: rows apart)
     assert kvb.seqs(0, 0, 1, q=torch.zeros(0, Hk, D)).q_stride == 0
+
+
+@pytest.mark.parametrize("bound", [False, True])
+def test_what_has_no_stride_is_packed(bound):
+    """Gates as columns of a projection's rows, transposed or broadcast gradients: there is no stride that could say so."""
+    q, k, v = packed()
+    wide = torch.zeros(N, 2 * Hv + 3)
+    for name, bad in (("g", wide[:, :Hv]), ("beta", wide[:, Hv:2 * Hv]), ("state0", torch.zeros(1, Hv, D, 2 * D)[..., :D])):
+        for call in (forward, backward):
+            with pytest.raises(ValueError):
+                call({**arrays((q, k, v), packed()), name: bad}, seqs((q, k, v)), bound)
+    for name, bad in (("dout", torch.zeros(1, 1, D).expand(N, Hv, D)), ("dg", wide[:, :Hv]), ("dbeta", torch.zeros(Hv, N).t()),
+                      ("dstate1", torch.zeros(1, Hv, D, D).transpose(2, 3)), ("dstate0", torch.zeros(1, Hv, D, D).transpose(2, 3))):
+        with pytest.raises(ValueError):
+            backward({**arrays((q, k, v), packed()), name: bad}, seqs((q, k, v)), bound)
+    with pytest.raises(ValueError):
+        forward({**arrays((q, k, v), packed()), "out": torch.zeros(Hv, N, D).transpose(0, 1)}, seqs((q, k, v)), bound)
+    a = arrays((q, k, v), packed())
+    a.update(g=torch.zeros(2 * N, Hv)[N:], state0=None, dstate1=None, dstate0=None)   # (contiguous; not there)
+    backward(a, seqs((q, k, v)), bound)
+    forward(a, seqs((q, k, v)), bound)
