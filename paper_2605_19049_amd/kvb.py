@@ -255,29 +255,53 @@ def seqs(start, n_tokens, n_slots, slot=None, q=None, k=None, v=None):
     return KvbSeqs(_ptr(start), _ptr(slot), _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v"), n_tokens, n_slots)
 
 
+def _check_packed(what, x):
+    if hasattr(x, "stride") and not x.is_contiguous():
+        raise ValueError("%s of shape %s and stride %s is not contiguous" % (what, tuple(x.shape), tuple(x.stride())))
+
+
 _SCAN = ("q", "k", "v", "g", "beta", "state0", "state1", "out")
 _BACKWARD = _SCAN[:6] + ("dout", "dstate1", "dq", "dk", "dv", "dg", "dbeta", "dstate0")
+_ACCEPT = ("n_drafts", "parent", "tokens", "target", "draft", "u", "s", "path", "accepted", "token")
+
+
+def _check_scan(names, sq, args):
+    """Tensors of a scan lie as the kvb_seqs says (q, k, v and their gradients) or packed (the others)."""
+    strides = {"q": sq.q_stride, "k": sq.k_stride, "v": sq.v_stride}
+    for what, x in zip(names, args):
+        if what[-1] not in strides:
+            _check_packed(what, x)
+        elif hasattr(x, "stride") and x.dim() in (2, 3):
+            x, said = x if x.dim() == 3 else x[:, None], strides[what[-1]]
+            stride = _token_stride(x, what)
+            if stride and stride != (said or x.shape[1] * x.shape[2]):
+                raise ValueError("%s has %d elements from token to token, the sequences say %s" % (what, stride, said or "packed"))
+
+
+def _check_accept(vo, args):
+    """Rows of probabilities lie one stride of the kvb_vocab after the other, the other arrays packed."""
+    row = vo.stride or vo.V
+    for what, x in zip(_ACCEPT, args):
+        if what not in ("target", "draft"):
+            _check_packed(what, x)
+        elif hasattr(x, "stride") and x.numel():
+            step = 1
+            for i in reversed(range(x.dim())):
+                if x.shape[i] > 1 and x.stride(i) != step:
+                    raise ValueError("%s of shape %s and stride %s: rows of %d elements, one after the other, are wanted" %
+                                     (what, tuple(x.shape), tuple(x.stride()), row))
+                step = row if i == x.dim() - 1 and x.dim() > 1 else step * x.shape[i]
 
 
 def _check_layouts(fn_name, args):
-    """ValueError where a tensor of a scan does not lie as the kvb_seqs says (q, k, v and their gradients) or packed (the others): the
-    kernels would read or write other memory.  args: the C arguments.  Addresses are taken as they are."""
-    if fn_name not in ("kvb_scan", "kvb_scan_backward"):
-        return
-    sq, q, k, v = args[1:5]
-    for what, x in zip(_SCAN if fn_name == "kvb_scan" else _BACKWARD, args[2:]):
-        if what not in ("q", "k", "v", "dq", "dk", "dv") and hasattr(x, "stride") and not x.is_contiguous():
-            raise ValueError("%s of shape %s and stride %s is not contiguous" % (what, tuple(x.shape), tuple(x.stride())))
-    rows = [("q", q, sq.q_stride), ("k", k, sq.k_stride), ("v", v, sq.v_stride)]
-    if fn_name == "kvb_scan_backward":
-        rows += [("d" + what, x, stride) for (what, _, stride), x in zip(rows, args[10:13])]
-    for what, x, said in rows:
-        if not hasattr(x, "stride") or x.dim() not in (2, 3):
-            continue
-        x = x if x.dim() == 3 else x[:, None]
-        stride = _token_stride(x, what)
-        if stride and stride != (said or x.shape[1] * x.shape[2]):
-            raise ValueError("%s has %d elements from token to token, the sequences say %s" % (what, stride, said or "packed"))
+    """ValueError where a tensor does not lie as the call takes it: the kernels would read or write other memory.  args: the C
+    arguments.  Addresses are taken as they are."""
+    if fn_name == "kvb_scan":
+        _check_scan(_SCAN, args[1], args[2:])
+    elif fn_name == "kvb_scan_backward":
+        _check_scan(_BACKWARD, args[1], args[2:])
+    elif fn_name == "kvb_accept":
+        _check_accept(args[0], args[1:])
 
 
 def _work(nbytes, where):
@@ -320,6 +344,7 @@ def accept_work(vo):
 
 
 def kvb_accept(vo, n_drafts, parent, tokens, target, draft, u, s, path, accepted, token, work, stream=None, check=True):
+    _check_layouts("kvb_accept", (vo, n_drafts, parent, tokens, target, draft, u, s, path, accepted, token))
     rc = lib().kvb_accept(ctypes.byref(vo), _ptr(n_drafts), _ptr(parent), _ptr(tokens), _ptr(target), _ptr(draft), _ptr(u),
                           _ptr(s), _ptr(path), _ptr(accepted), _ptr(token), _ptr(work), _stream(stream))
     return _check(rc, "kvb_accept", check)
