@@ -244,10 +244,10 @@ def _token_stride(x, what):
     """Elements from one token's row to the next of a [n_tokens, heads, d] tensor whose tokens are contiguous, 0 for up to one token."""
     if x is None or x.shape[0] == 0:
         return 0
-    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or \
-            (x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2]):
-        raise ValueError("%s of shape %s and stride %s: [n_tokens, heads, d] with contiguous tokens is wanted" % (what, tuple(x.shape), tuple(x.stride())))
-    return x.stride(0) if x.shape[0] > 1 else 0
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or stride[2] != 1 or (shape[1] > 1 and stride[1] != shape[2]) or (shape[0] > 1 and stride[0] < shape[1] * shape[2]):
+        raise ValueError("%s of shape %s and stride %s: [n_tokens, heads, d] with contiguous tokens is wanted" % (what, tuple(shape), stride))
+    return stride[0] if shape[0] > 1 else 0
 
 
 def seqs(start, n_tokens, n_slots, slot=None, q=None, k=None, v=None):
@@ -256,7 +256,7 @@ def seqs(start, n_tokens, n_slots, slot=None, q=None, k=None, v=None):
 
 
 def _check_packed(what, x):
-    if hasattr(x, "stride") and not x.is_contiguous():
+    if not (x is None or isinstance(x, int) or x.is_contiguous()):
         raise ValueError("%s of shape %s and stride %s is not contiguous" % (what, tuple(x.shape), tuple(x.stride())))
 
 
@@ -269,10 +269,11 @@ def _check_scan(names, sq, args):
     """Tensors of a scan lie as the kvb_seqs says (q, k, v and their gradients) or packed (the others)."""
     strides = {"q": sq.q_stride, "k": sq.k_stride, "v": sq.v_stride}
     for what, x in zip(names, args):
-        if what[-1] not in strides:
+        said = strides.get(what[-1])
+        if said is None or (said == 0 and not isinstance(x, int) and x is not None and x.is_contiguous()):
             _check_packed(what, x)
-        elif hasattr(x, "stride") and x.dim() in (2, 3):
-            x, said = x if x.dim() == 3 else x[:, None], strides[what[-1]]
+        elif not (x is None or isinstance(x, int)) and x.dim() in (2, 3):
+            x = x if x.dim() == 3 else x[:, None]
             stride = _token_stride(x, what)
             if stride and stride != (said or x.shape[1] * x.shape[2]):
                 raise ValueError("%s has %d elements from token to token, the sequences say %s" % (what, stride, said or "packed"))
@@ -284,7 +285,7 @@ def _check_accept(vo, args):
     for what, x in zip(_ACCEPT, args):
         if what not in ("target", "draft"):
             _check_packed(what, x)
-        elif hasattr(x, "stride") and x.numel():
+        elif not (x is None or isinstance(x, int)) and x.numel():
             step = 1
             for i in reversed(range(x.dim())):
                 if x.shape[i] > 1 and x.stride(i) != step:
