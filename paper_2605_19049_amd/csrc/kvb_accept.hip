@@ -222,7 +222,7 @@ __device__ Walk walk(const AcceptArgs &a, int b, Probs<T> &rows, float *mass_at,
     const int x = rows.tokens[i0], up = TREE && a.parent ? a.parent[(int64_t)b * a.T + i0] : i0 - 1;
     const float u = a.u[(int64_t)b * a.T + i0];
     const int parent = up < -1 || up >= i0 ? -1 : up, known = x >= 0 && x < a.V, xs = known ? x : 0;
-    const float p = to_f32(target[(parent + 1) * a.stride + xs]);
+    const float pt = to_f32(target[(parent + 1) * a.stride + xs]), p = pt == pt ? pt : 0.0f;   // (no number: nothing, and what is left loses nothing)
     const float q = rows.q ? to_f32(rows.q[m0 * a.stride + xs]) : 1.0f;   // of token i in row m
 
     Walk w{-1, 0, 0};
