@@ -361,9 +361,10 @@ typedef struct kvb_vocab {
  * the walk stands.  It is accepted if u_i q_i(x_i) Z < r(x_i); then the walk stands at it, r is its row and Z = 1.
  * Otherwise r becomes max(r - Z q_i, 0) and Z its sum; for chosen drafts r(x_i) becomes 0 and Z loses what it was.  The token is
  * drawn from r (from the row itself if nothing is left of r, -1 if that has nothing either): weights are r cut off to 0..1
- * in whole multiples of 2^-48, rounded down, and the token is the first whose running sum exceeds floor(s W), W their sum.
- * Each operation is one rounding in fp32, sums are exact: the results do not depend on the launch.  A probability of the target that
- * is not a number counts as 0, one of a draft as infinity: a draft whose own is none is not accepted (as 0 it always would be).
+ * in whole multiples of 2^-48, rounded down, and the token is the first whose running sum exceeds floor(s W) in fp64, W their sum.
+ * Each operation is one rounding in fp32, sums are exact: the results do not depend on the launch.  (Rows that sum to more than 32 are
+ * no probabilities; they get one of their tokens, but which of those next to s W may depend on it.)  A probability of the target
+ * that is not a number counts as 0, one of a draft as infinity: a draft whose own is none is not accepted (as 0 it always would be).
  */
 int64_t kvb_accept_work(const kvb_vocab *vocab);
 int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *parent, const int32_t *tokens,

@@ -2,8 +2,8 @@
 //
 // The walk down the drafts needs single probabilities.  What has to be read as a whole is one row of the target (and the draft's row
 // that was rejected there): the token that follows is drawn from what is left of it.  Weights are whole multiples of 2^-48, held as fp64
-// integers, so sums are exact in any order (up to 32 times what a row of probabilities sums to) and the token does not depend on how
-// the row was split.  All comparisons are in fp32, each operation rounded by itself (no contraction): p and q of 16 bits are exact.
+// integers, so sums of up to 32 are exact in any order (probabilities sum to 1) and the token does not depend on how
+// the row was split; rows that sum to more get one of their tokens.  All comparisons are in fp32, each operation rounded by itself (no contraction): p and q of 16 bits are exact.
 //   few, long rows     kvb_accept_sum_kernel walks and sums a row's segments side by side, kvb_accept_find_kernel looks for the token
 //   otherwise          kvb_accept_row_kernel does both, a workgroup a request
 //   trees with draft probabilities: after a rejection the next sibling is tested against the sum of what is left, a whole row;
@@ -142,7 +142,24 @@ __device__ double sum_row(const Probs<T> &rows, const Walk &w, int lo, int hi, d
     return total;
 }
 
-// The first token of lo .. hi-1 whose running sum exceeds aim (which is below the range's sum), hi - lo some hundreds: a few neighbours
+// The first of n ranges, with sums at(0) .. at(n - 1) of which one at least is not zero, whose running sum exceeds aim; aim becomes what is
+// left of it there.  Rows that sum to more than 32 have rounded sums, and an aim between two of them may pass the last one: then the last
+// range with anything in it, and so on inside, so that a token is found all the same.
+template <typename At>
+__device__ __forceinline__ int pick(int n, double &aim, At &&at)
+{
+    int last = 0;
+    for (int v = 0; v < n; ++v) {
+        const double s = at(v);
+        if (aim < s)
+            return v;
+        aim -= s;
+        last = s > 0.0 ? v : last;
+    }
+    aim = __builtin_huge_val();
+    return last;
+}
+// The first token of lo .. hi-1 whose running sum exceeds aim (as in pick), hi - lo some hundreds: a few neighbours
 // a thread.  The thread that has it writes it.
 template <bool TREE, int WAVES, typename T>
 __device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, double *part, int32_t *to)
@@ -167,26 +184,30 @@ __device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, dou
     if (lane == 63)
         part[wave] = upto;
     __syncthreads();
-    for (int v = 0; v < wave; ++v)
-        upto += part[v];
-    double run = upto - own;
-    if (run <= aim && aim < upto)
+    if (wave != pick(WAVES, aim, [&](int v) { return part[v]; }))
+        return;
+    const uint64_t some = __ballot(own > 0.0), past = __ballot(own > 0.0 && aim < upto);
+    if (lane == (past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some | 1))) {
+        double run = upto - own;
+        int token = from;
         for (int j = from; j < end; ++j) {
-            run += at(j);
-            if (aim < run) {
-                *to = j;
-                break;
+            const double x = at(j);
+            if (x > 0.0) {
+                token = j;
+                run += x;
+                if (aim < run)
+                    break;
             }
         }
+        *to = token;
+    }
 }
 // The same for a range of any length whose waves' sums are in `part`: on to the wave's range that has it, until that is short.
 template <bool TREE, int WAVES, typename T>
 __device__ void find_long(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, double *part, int32_t *to)
 {
     for (;;) {
-        int v = 0;
-        for (; v + 1 < WAVES && part[v] <= aim; ++v)
-            aim -= part[v];
+        const int v = pick(WAVES, aim, [&](int i) { return part[i]; });
         const int from = bound_of(lo, hi, v, WAVES), end = bound_of(lo, hi, v + 1, WAVES);
         lo = from;
         hi = end;
@@ -358,9 +379,7 @@ __global__ __launch_bounds__(1024) void kvb_accept_find_kernel(const AcceptArgs 
         return;
     }
     double aim = aim_of(a.s[b], total);
-    int s = 0;
-    for (; s + 1 < a.segments && sums[s] <= aim; ++s)
-        aim -= sums[s];
+    const int s = pick(a.segments, aim, [&](int i) { return sums[i]; });
     const int lo = min(a.V, s * a.segment), hi = min(a.V, (s + 1) * a.segment);
     sum_row<TREE, 16>(rows, w, lo, hi, part);
     find_long<TREE, 16>(rows, w, lo, hi, aim, part, a.token + b);

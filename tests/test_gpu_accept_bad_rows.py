@@ -1,4 +1,4 @@
-"""kvb_accept on rows that are no probabilities: what is not a number."""
+"""kvb_accept on rows that are no probabilities: what is not a number, and rows that sum to more than fp64 adds up exactly."""
 import numpy as np
 import pytest
 import torch
@@ -62,3 +62,14 @@ def test_a_drawn_draft_whose_probability_is_not_a_number(V):
 def test_a_target_row_of_nothing_but_nan():
     for V in (64, 40000):
         assert run(np.full((2, V), NAN), None, [0], [0.0], 0.5) == ([-1], 0, -1)
+
+
+@pytest.mark.parametrize("V, at", [(600, 0), (600, 290), (40000, 0), (40000, 20000), (70000, 65400)])
+def test_a_row_that_sums_to_more_than_fp64_holds_exactly(V, at):
+    """100 ones, 100 values of 2^-48, 100 ones: with s = 1/2 the running sums that lie on either side of the aim differ by less than
+    their rounding.  A token of the row comes out all the same, one of those next to the aim."""
+    target = np.zeros((2, V), np.float32)
+    target[0, at:at + 300] = 1.0
+    target[0, at + 100:at + 200] = 2.0 ** -48
+    path, accepted, token = run(target, None, [V - 1], [0.5], 0.5)
+    assert path == [-1] and accepted == 0 and at + 99 <= token <= at + 200
