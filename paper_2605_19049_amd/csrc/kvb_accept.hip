@@ -142,12 +142,20 @@ __device__ double sum_row(const Probs<T> &rows, const Walk &w, int lo, int hi, d
     return total;
 }
 
+// Sums of weights up to here are exact.  Only rows that are no probabilities reach it, and then an aim may fall between two sums of the
+// same tokens that were rounded differently: the search takes care of that (where told so; 0.5 us otherwise).
+constexpr double EXACT_SUM = 0x1p53;
 // The first of n ranges, with sums at(0) .. at(n - 1) of which one at least is not zero, whose running sum exceeds aim; aim becomes what is
-// left of it there.  Rows that sum to more than 32 have rounded sums, and an aim between two of them may pass the last one: then the last
-// range with anything in it, and so on inside, so that a token is found all the same.
+// left of it there.  rounded: an aim that passes the last one gets the last range with anything in it, and so on inside.
 template <typename At>
-__device__ __forceinline__ int pick(int n, double &aim, At &&at)
+__device__ __forceinline__ int pick(int n, double &aim, bool rounded, At &&at)
 {
+    if (!rounded) {
+        int v = 0;
+        for (; v + 1 < n && at(v) <= aim; ++v)
+            aim -= at(v);
+        return v;
+    }
     int last = 0;
     for (int v = 0; v < n; ++v) {
         const double s = at(v);
@@ -162,7 +170,7 @@ __device__ __forceinline__ int pick(int n, double &aim, At &&at)
 // The first token of lo .. hi-1 whose running sum exceeds aim (as in pick), hi - lo some hundreds: a few neighbours
 // a thread.  The thread that has it writes it.
 template <bool TREE, int WAVES, typename T>
-__device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, double *part, int32_t *to)
+__device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, bool rounded, double *part, int32_t *to)
 {
     const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, each = (hi - lo + 64 * WAVES - 1) / (64 * WAVES);
     const int from = min(hi, lo + (int)threadIdx.x * each), end = min(hi, from + each);
@@ -184,30 +192,42 @@ __device__ void find_in(const Probs<T> &rows, const Walk &w, int lo, int hi, dou
     if (lane == 63)
         part[wave] = upto;
     __syncthreads();
-    if (wave != pick(WAVES, aim, [&](int v) { return part[v]; }))
-        return;
-    const uint64_t some = __ballot(own > 0.0), past = __ballot(own > 0.0 && aim < upto);
-    if (lane == (past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some | 1))) {
+    if (rounded) {
+        if (wave != pick(WAVES, aim, true, [&](int v) { return part[v]; }))
+            return;
+        const uint64_t some = __ballot(own > 0.0), past = __ballot(own > 0.0 && aim < upto);
+        if (lane != (past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some | 1)))
+            return;
         double run = upto - own;
-        int token = from;
         for (int j = from; j < end; ++j) {
             const double x = at(j);
             if (x > 0.0) {
-                token = j;
+                *to = j;
                 run += x;
                 if (aim < run)
                     break;
             }
         }
-        *to = token;
+        return;
     }
+    for (int v = 0; v < wave; ++v)
+        upto += part[v];
+    double run = upto - own;
+    if (run <= aim && aim < upto)
+        for (int j = from; j < end; ++j) {
+            run += at(j);
+            if (aim < run) {
+                *to = j;
+                break;
+            }
+        }
 }
 // The same for a range of any length whose waves' sums are in `part`: on to the wave's range that has it, until that is short.
 template <bool TREE, int WAVES, typename T>
-__device__ void find_long(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, double *part, int32_t *to)
+__device__ void find_long(const Probs<T> &rows, const Walk &w, int lo, int hi, double aim, bool rounded, double *part, int32_t *to)
 {
     for (;;) {
-        const int v = pick(WAVES, aim, [&](int i) { return part[i]; });
+        const int v = pick(WAVES, aim, rounded, [&](int i) { return part[i]; });
         const int from = bound_of(lo, hi, v, WAVES), end = bound_of(lo, hi, v + 1, WAVES);
         lo = from;
         hi = end;
@@ -215,7 +235,7 @@ __device__ void find_long(const Probs<T> &rows, const Walk &w, int lo, int hi, d
             break;
         sum_row<TREE, WAVES>(rows, w, lo, hi, part);
     }
-    find_in<TREE, WAVES>(rows, w, lo, hi, aim, part, to);
+    find_in<TREE, WAVES>(rows, w, lo, hi, aim, rounded, part, to);
 }
 
 // floor(s total), below total
@@ -325,7 +345,7 @@ __device__ void find_row(const AcceptArgs &a, int b, const Probs<T> &rows, Walk 
             a.token[b] = -1;
         return;
     }
-    find_long<TREE, WAVES>(rows, w, 0, a.V, aim_of(a.s[b], total), part, a.token + b);
+    find_long<TREE, WAVES>(rows, w, 0, a.V, aim_of(a.s[b], total), total >= EXACT_SUM, part, a.token + b);
 }
 
 }  // namespace
@@ -379,10 +399,11 @@ __global__ __launch_bounds__(1024) void kvb_accept_find_kernel(const AcceptArgs 
         return;
     }
     double aim = aim_of(a.s[b], total);
-    const int s = pick(a.segments, aim, [&](int i) { return sums[i]; });
+    const bool rounded = total >= EXACT_SUM;
+    const int s = pick(a.segments, aim, rounded, [&](int i) { return sums[i]; });
     const int lo = min(a.V, s * a.segment), hi = min(a.V, (s + 1) * a.segment);
     sum_row<TREE, 16>(rows, w, lo, hi, part);
-    find_long<TREE, 16>(rows, w, lo, hi, aim, part, a.token + b);
+    find_long<TREE, 16>(rows, w, lo, hi, aim, rounded, part, a.token + b);
 }
 
 namespace {
