@@ -302,6 +302,8 @@ typedef struct kvb_seqs {
  *           before and after the call.  kvb_scan_work depends on B, Hv and n_tokens alone, grows with
  *           them, and returns one of the error codes for what the call would refuse.
  * Head sizes and types as elsewhere: dk == dv in {32, 64, 128}, fp32, bf16 or fp16.
+ * Whether tokens go one by one or in chunks is decided by their average number a sequence (up to 4: one by one): a long sequence among
+ * many that are empty or short is better given a call of its own.
  * A value that is not finite may make NaN of any output of its head in the 64-token chunk that holds it (counted from the
  * sequence's start) and behind it; log decays down to -infinity are fine.
  */

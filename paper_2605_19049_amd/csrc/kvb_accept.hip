@@ -7,7 +7,8 @@
 //   few, long rows     kvb_accept_sum_kernel walks and sums a row's segments side by side, kvb_accept_find_kernel looks for the token
 //   otherwise          kvb_accept_row_kernel does both, a workgroup a request
 //   trees with draft probabilities: after a rejection the next sibling is tested against the sum of what is left, a whole row;
-//                      a workgroup a request
+//                      a workgroup a request, which reads the target's row and those of all drafts rejected there once more for each sum.
+//                      8 siblings, fp32, 150001 tokens: 1 request 81 us with 1.4 of them rejected, 245 with 6.2; 64 requests 430 and 473
 // Bounded by reading the rows where there are many: 128 requests of 150001 tokens, 4 drafts, fp32, 146 MB, 35.6 us or 4.1 TB/s; few are bounded by
 // the chain launch, walk (two loads), sum, search: 1 request of 32000 tokens 9 us.  Rows are read twice, to sum and to find, the second time
 // only the part of a row that holds the token: which weight the random number falls on is known only after the sum.

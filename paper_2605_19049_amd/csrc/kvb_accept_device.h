@@ -28,10 +28,13 @@ struct AcceptArgs {
 };
 
 // Segments of a row, each a workgroup; 1: the whole of a request by one workgroup, in one launch instead of two.  A row is split where one
-// workgroup would read it for longer than a launch takes and the requests alone do not fill the card.  us, split against whole rows, 4 drafts,
-// fp32, nothing in the caches: 1 request of 32000 tokens 11.1 / 8.9, of 40000 10.7 / 10.5; 64 requests of 32000 15.5 / 11.0, of 65537 16.2 / 17.9, of
-// 150001 22.5 / 31.8; 128 of 65537 21.5 / 18.5, of 150001 35.7 / 38.5; 256 of 150001, bf16, 48.5 / 41.3.  Segments of at least 8192 (16384: 32
-// of 150001 18.3, against 16.2), about 1024 in all.
+// workgroup would take longer for it than a launch does and the requests alone do not fill the card.  That goes by tokens, not bytes: what a
+// workgroup takes is the work and latency for each, 150001 tokens of bf16 38 us and of fp32 37.  us, split against whole rows, 4 drawn drafts, nothing in
+// the caches, fp32: 1 request of 32768 tokens 11.7 / 9.8, of 40000 10.7 / 10.5, of 65537 13.4 / 14.1, of 150001 14.2 / 22.0; 64 of 32768 15.3 / 13.5, of
+// 65537 18.6 / 20.8, of 150001 26.2 / 37.3; 96 of 65537 21.2 / 21.8, of 100003 25.5 / 28.4; 128 of 65537 24.8 / 22.8, of 100003 30.7 / 29.6, of 150001 38.5 / 41.5;
+// 160 of 150001 47.1 / 44.3.  bf16: 64 of 65537 19.9 / 21.8; 128 of 65537 21.9 / 22.6, of 150001 32.3 / 40.5; 160 of 150001 37.7 / 41.0; 200 42.1 / 42.6; 256
+// 51.5 / 43.6.  So the bounds are those of fp32, and on the low side for 16 bits; around 32768 tokens a split costs up to 2 us.  Segments of at
+// least 8192 (16384: 32 of 150001 18.3, against 16.2), about 1024 in all.
 inline int accept_split_most(int V) { return V < 32768 ? 0 : V < 131072 ? 64 : 128; }   // requests up to which rows are split; grows with V
 inline int accept_segments(int B, int V)
 {

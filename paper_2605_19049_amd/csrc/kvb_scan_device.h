@@ -605,13 +605,16 @@ constexpr int SCAN_CUS = 256;   // compute units of the card
 
 // Up to how many tokens a sequence, on average, kvb_scan goes token by token: 0.3 to 0.8 us a token against a chunk's fixed work.
 // us, token by token against chunks, bf16, 32 v-heads of 128: 16 sequences of 1 token 14 / 38, of 4 18 / 38, of 8 23 / 38, of 16 33 / 41; one
-// sequence of 1 4 / 12, of 8 10 / 12, of 16 16 / 13.  4 and not 8, for the tokens may all be one sequence's, one after the other.
+// sequence of 1 4 / 12, of 8 10 / 12, of 16 16 / 13.  4 and not 8, for the tokens may all be one sequence's, one after the other: the host knows
+// the average alone.  A long sequence among many that are empty or short then takes about 1 us a token: 128 slots of which one has 512 tokens 505 us,
+// with 513 of them, by chunks, 145 (the one alone 43; the empty ones' states are copied); 512 slots, one of 2048, 2034 (alone 134); 63 single tokens and one sequence of 190 197, of 194 141.
 constexpr int TOKEN_MAX = 4;
 
 // Whether a workgroup works out M and P of its chunks itself, in one launch instead of two: for about a chunk a sequence, and workgroups
 // that each find a free compute unit (both halves of a head's columns do that work).  us, alone against two launches, bf16, d = 128: 1
 // sequence of 37 tokens, 32 v-heads 13.9 / 16.4; 8 of 64, 8 v-heads 15.5 / 19.3; 1 of 128, 32 v-heads 25.8 / 21.6; 32 of 64 (2048 workgroups)
-// 122 / 87; 4 of 60, 8 v-heads, fp32, d = 64 14.7 / 18.0.  fp32 at d = 128 has no room for it in LDS, d = 32 too few waves.
+// 122 / 87; 4 of 60, 8 v-heads, fp32, d = 64 14.7 / 18.0.  This, too, goes by the average: 8 sequences of 8 v-heads with all tokens in one of 512 88 us,
+// of 513 45.  fp32 at d = 128 has no room for it in LDS, d = 32 too few waves.
 template <typename TIn, int D>
 constexpr bool CAN_ALONE = D >= 64 && sizeof(TIn) * D < 512;
 template <int D>

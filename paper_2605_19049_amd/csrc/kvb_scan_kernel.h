@@ -203,7 +203,8 @@ __global__ __launch_bounds__(256, 3) void kvb_scan_prep_kernel(const ScanArgs a)
 // K S and Q S, E and the state's update follow from each other within the wave, and the sums' registers are the next product's second operand
 // as they stand.  What the next chunk needs from memory is requested a chunk ahead.
 // Bounded by the chain of a chunk's products in a wave: 3.6 us a chunk, of which the matrix instructions are busy 1.5 (three pieces of the state
-// against one of the keys), cutting into pieces takes 0.6, requests and stores 0.9, the rest are waits for LDS and for sums.  Few sequences
+// against one of the keys), cutting into pieces takes 0.6, requests and stores 0.9, the rest are waits for LDS (37 % of the cycles it is in use go to
+// bank conflicts) and for sums.  Few sequences
 // leave most of the card idle: one of 8191 tokens, 32 v-heads, d = 128 455 us on 128 compute units, 128 chunks one after the other (55 Tflop/s
 // of the recurrence); 24 ragged ones of 1500 340 us on all of them (166 Tflop/s, 1.6 TB/s).
 // ALONE: M and P are not there yet, the workgroup works them out itself chunk by chunk: for few chunks, one launch instead of two.
