@@ -374,6 +374,161 @@ int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *p
                int32_t *path, int32_t *accepted, int32_t *token, void *work, void *stream);
 
 /*
+ * Around the recurrence: what makes a layer's q, k, v, g and beta from the rows of its projection (kvb_conv and its forms), the norms ahead of a
+ * block and behind the recurrence (kvb_norm), and the norm of all gradients together (kvb_grad_norm, kvb_clip).
+ */
+#define KVB_CONV_UNIT 1   /* kvb_taps.flags: q and k are divided by sqrt(sum of squares over the head + eps) */
+
+typedef struct kvb_taps {
+    const void  *weight;     /* device [C, width] in_dtype, C = (2 Hk + Hv) dk channels: q's, k's, v's, head by head.  The last    */
+                             /* tap is the token's own                                                                           */
+    const void  *bias;       /* device [C] in_dtype, or NULL: none                                                               */
+    const float *A_log;      /* device [Hv] fp32, for the gates                                                                  */
+    const float *dt_bias;    /* device [Hv] fp32, for the gates                                                                  */
+    int64_t      x_stride;   /* elements from one token's row of x to the next: at least C, in bytes a multiple of 16, at most 2^26;
+                                0: packed.  So that x may be part of the rows of one projection                                  */
+    int64_t      a_stride;   /* the same of a and b: at least Hv, at most 2^26; 0: packed                                        */
+    int64_t      b_stride;
+    int32_t      width;      /* 2, 3 or 4 taps                                                                                   */
+    int32_t      flags;      /* KVB_CONV_UNIT                                                                                    */
+    float        eps;        /* above 0 with KVB_CONV_UNIT                                                                       */
+} kvb_taps;
+
+/*
+ * kvb_conv -- whole sequences (kvb_seqs, ragged and packed).  With E the width - 1 rows of the sequence's state followed by its inputs,
+ *      z_t = bias + sum_i weight_i E_{t+i}      y = z / (1 + exp(-z))      q, k, v = y, q and k of length one (KVB_CONV_UNIT)
+ *      g = -exp(A_log) log(1 + exp(a + dt_bias))      beta = 1 / (1 + exp(-b))
+ *   shape   B, Hk, Hv, dk == dv in {32, 64, 128}, in_dtype; the rest is not looked at
+ *   x       device [n_tokens, C] in_dtype         a, b  device [n_tokens, Hv] in_dtype; both NULL: no gates are wanted, g and beta are NULL too
+ *   state0  device [n_slots, width - 1, C] in_dtype, the last inputs, oldest first; NULL: zero
+ *   state1  the same, written: the state behind the last token (an empty sequence's is its state0); NULL: not wanted.  May be state0
+ *   q, k, v device, written: [n_tokens, Hk or Hv, dk] in_dtype, strides of seqs
+ *   g, beta device, written: [n_tokens, Hv] fp32
+ * All arithmetic is fp32, results are rounded once.  What is written must not overlap x, a and b.
+ * Rows of skipped sequences (slot outside 0..n_slots-1) are not written.
+ */
+int kvb_conv(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs, const void *x, const void *a, const void *b,
+             const void *state0, void *state1, void *q, void *k, void *v, float *g, float *beta, void *stream);
+
+/*
+ * kvb_conv_decode -- kvb_conv for one token of each request, as kvb_decode wants them.  slot device int32 [B] (not NULL, none twice), rows of n_slots
+ * states; x [B, C], a, b [B, Hv]; q, k, v, g, beta packed; state0 and state1 as above (state1 may be state0).
+ */
+int kvb_conv_decode(const kvb_shape *shape, const kvb_taps *taps, const int32_t *slot, int32_t n_slots, const void *x, const void *a, const void *b,
+                    const void *state0, void *state1, void *q, void *k, void *v, float *g, float *beta, void *stream);
+
+/*
+ * kvb_conv_verify -- the same for T drafts of each request, as kvb_verify and kvb_verify_tree want them: draft i's taps reach back over its ancestors
+ * and then the state.  The state is left alone.
+ *   T       1..KVB_MAX_DRAFTS       x device [B, T, C], a, b [B, T, Hv] (the strides from draft to draft, requests follow each other); q .. beta packed
+ *   parent  device int32 [B, T] as kvb_verify_tree's, or NULL: a chain.  An entry outside -1 .. i-1 is taken as -1
+ */
+int kvb_conv_verify(const kvb_shape *shape, const kvb_taps *taps, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent,
+                    const void *x, const void *a, const void *b, const void *state, void *q, void *k, void *v, float *g, float *beta, void *stream);
+
+/*
+ * kvb_conv_commit -- the accepted drafts of a preceding kvb_conv_verify enter the state: state1 becomes the last width - 1 rows of state0 and theirs.
+ *   path     device int32 [B, T], kvb_accept's or kvb_compact's: the accepted drafts, oldest first; NULL: drafts 0, 1, .. of a chain
+ *   accepted device int32 [B]: how many, 0..T
+ *   x        as kvb_conv_verify was given it
+ *   state0, state1  as above, state1 not NULL.  May be the same
+ * A path that is not increasing within 0..T-1 or a number outside 0..T commits nothing: state1 becomes state0 (kvb_compact reports these).
+ */
+int kvb_conv_commit(const kvb_shape *shape, const kvb_taps *taps, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *path,
+                    const int32_t *accepted, const void *x, const void *state0, void *state1, void *stream);
+
+/*
+ * kvb_conv_backward -- the gradients of kvb_conv, from those of its outputs and last states.
+ *   x .. state0     as kvb_conv was given them (a and b NULL: no gates; dg, dbeta, da, db, dA_log and ddt_bias are NULL too.  Without any
+ *                   tokens dA_log and ddt_bias alone count, which become 0)
+ *   dq, dk, dv      device in_dtype, strides of q, k and v in seqs         dg, dbeta  device [n_tokens, Hv] fp32
+ *   dstate1         device [n_slots, width - 1, C] in_dtype, or NULL: zero
+ *   dx, da, db      device, written: in_dtype, strides of x, a and b
+ *   dweight, dbias  device [C, width], [C] fp32, written; dbias is NULL if and only if there is no bias
+ *   dA_log, ddt_bias  device [Hv] fp32, written
+ *   dstate0         device [n_slots, width - 1, C] in_dtype, written, or NULL: not wanted.  Not dstate1
+ *   work            device, kvb_conv_backward_work(shape, taps, seqs) bytes, 16-byte aligned; what it holds means nothing before and after the call.
+ *                   It grows with B and n_tokens
+ * What is written must not overlap what is read.  Rows of skipped sequences are neither written nor counted in the sums.  The same inputs give the
+ * same bits.
+ */
+int64_t kvb_conv_backward_work(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs);
+int kvb_conv_backward(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs, const void *x, const void *a, const void *b,
+                      const void *state0, const void *dq, const void *dk, const void *dv, const float *dg, const float *dbeta, const void *dstate1,
+                      void *dx, void *da, void *db, float *dweight, float *dbias, float *dA_log, float *ddt_bias, void *dstate0, void *work,
+                      void *stream);
+
+#define KVB_MAX_WIDTH 16384 /* longest row of kvb_norm */
+
+typedef struct kvb_rows {
+    int64_t x_stride;     /* elements from one token's rows of x to the next, of gate: at least heads * width, in bytes a multiple of 16,  */
+    int64_t gate_stride;  /* at most 2^26; 0: packed.  A token's heads follow each other                                                  */
+    int32_t n_tokens;
+    int32_t heads;        /* rows of a token, each with a norm of its own                                                                 */
+    int32_t width;        /* elements of a row: a multiple of 8, 8..KVB_MAX_WIDTH                                                         */
+    int32_t dtype;        /* of gate, weight and out: KVB_F32, KVB_BF16 or KVB_F16                                                        */
+    int32_t x_dtype;      /* of x, res and sum: KVB_F32 or dtype                                                                          */
+    float   eps;          /* above 0                                                                                                      */
+    float   scale;        /* of x where there is a residual, 1 where there is none                                                        */
+} kvb_rows;
+
+/*
+ * kvb_norm -- the root mean square norm of rows, with the residual ahead of it and the gate behind it:
+ *      s = res + scale x, rounded to x_dtype (x itself without a residual)      out = s / sqrt(mean s^2 + eps) weight gate / (1 + exp(-gate))
+ * Behind the recurrence: x its outputs (fp32 or 16 bits), heads = Hv, width = dv, gate from the layer's projection.  Ahead of a block: heads = 1, x what
+ * the block before put out, res the stream that it is added to.
+ *   x       device [n_tokens, heads, width] x_dtype         res   the same, packed, or NULL: none
+ *   gate    device [n_tokens, heads, width] dtype, or NULL: none       weight  device [width] dtype
+ *   sum     device, written: s, packed, or NULL: not wanted.  Without a residual NULL.  May be res, or x where that lies packed
+ *   out     device, written: [n_tokens, heads, width] dtype, packed.  May be x (of the same type) or gate where they lie packed
+ * All arithmetic is fp32; squares above the range of fp32 make a row 0.
+ */
+int kvb_norm(const kvb_rows *rows, const void *x, const void *res, const void *gate, const void *weight, void *sum, void *out, void *stream);
+
+/*
+ * kvb_norm_backward -- the gradients of kvb_norm.
+ *   x        what the norm was taken of: kvb_norm's sum where there was a residual, else its x; x_stride is this array's
+ *   gate, weight  as kvb_norm was given them          dout  device [n_tokens, heads, width] dtype, packed
+ *   dsum     device x_dtype, packed: the gradient of sum from what else it went to; NULL: zero
+ *   dx       device, written: x_dtype, lies as x does; scale times the gradient of s
+ *   dres     device, written: x_dtype, packed: the gradient of s; NULL: not wanted.  May be dsum
+ *   dgate    device, written: dtype, lies as gate does; NULL if and only if there is no gate
+ *   dweight  device [width] fp32, written
+ *   work     device, kvb_norm_backward_work(rows) bytes, 16-byte aligned; means nothing before and after the call.  It grows with n_tokens
+ * The same inputs give the same bits.
+ */
+int64_t kvb_norm_backward_work(const kvb_rows *rows);
+int kvb_norm_backward(const kvb_rows *rows, const void *x, const void *gate, const void *weight, const void *dout, const void *dsum, void *dx,
+                      void *dres, void *dgate, float *dweight, void *work, void *stream);
+
+#define KVB_LIST_BLOCK 16384
+
+typedef struct kvb_list {       /* some tensors; all arrays are on the device                                        */
+    void *const   *data;        /* [n] addresses, each aligned to its elements                                       */
+    const int64_t *size;        /* [n] elements, 0 is fine                                                           */
+    const int32_t *type;        /* [n] KVB_F32, KVB_BF16 or KVB_F16                                                  */
+    const int32_t *first;       /* [n+1] running sum of ceil(size / KVB_LIST_BLOCK), from 0                          */
+    int32_t        n;
+    int32_t        blocks;      /* first[n]                                                                          */
+} kvb_list;
+
+/*
+ * kvb_grad_norm -- norm = the root of the sum of squares of all elements (summed in fp64).
+ *   norm  device fp32 [1], written       work  device, kvb_grad_norm_work(list) bytes, 8-byte aligned; means nothing before and after the call
+ */
+int64_t kvb_grad_norm_work(const kvb_list *list);
+int kvb_grad_norm(const kvb_list *list, float *norm, void *work, void *stream);
+
+/*
+ * kvb_clip -- every element times min(1, largest / (norm + 1e-6)), in fp32, rounded once.
+ *   to       tensors of the same sizes and types (only data is looked at), or NULL: in place.  None may overlap another's source
+ *   norm     device fp32 [1]: kvb_grad_norm's, or what ranks that hold a part each have made of theirs
+ *   largest  at least 0
+ * Where nothing is to be cut, nothing is written in place.  A norm that is infinite makes every finite element 0, one that is not a number all NaN.
+ */
+int kvb_clip(const kvb_list *list, const kvb_list *to, const float *norm, float largest, void *stream);
+
+/*
  * Kernel timer (measurement aid, no part of the method).  A timer owns two HIP events.
  * kvb_timer_arm makes the NEXT kernel that the calling thread launches through this
  * library record its own begin and end timestamps into them; kvb_timer_read waits for that

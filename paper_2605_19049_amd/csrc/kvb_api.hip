@@ -1,6 +1,9 @@
 // Host side of the library: argument checks (all before the first HIP call), the extern "C" entry
 // points of include/kvb.h, the kernel timer.
 #include "kvb_accept_device.h"
+#include "kvb_layer_device.h"
+
+#include <cmath>
 
 namespace kvb_impl {
 
@@ -218,9 +221,339 @@ int check_vocab(const kvb_vocab *vo)
     return KVB_OK;
 }
 
+int64_t conv_channels(const kvb_shape *sh) { return (int64_t)(2 * (int64_t)sh->Hk + sh->Hv) * sh->dk; }
+
+// The shape (as far as it matters) and the taps of a convolution, without its tokens.
+int check_taps(const kvb_shape *sh, const kvb_taps *ta)
+{
+    if (!sh || !ta || sh->B < 0 || sh->Hk <= 0 || sh->Hv <= 0 || sh->Hv % sh->Hk != 0 || sh->dk <= 0 || sh->dv <= 0)
+        return KVB_EINVAL;
+    if (sh->in_dtype != KVB_F32 && sh->in_dtype != KVB_BF16 && sh->in_dtype != KVB_F16)
+        return KVB_EUNSUPPORTED;
+    if (sh->dk != sh->dv || (sh->dk != 32 && sh->dk != 64 && sh->dk != 128))
+        return KVB_EUNSUPPORTED;
+    const int64_t C = conv_channels(sh), size = sh->in_dtype == KVB_F32 ? 4 : 2;
+    if (C * 4 > 1 << 26)
+        return KVB_EINVAL;
+    if (!ta->weight || !aligned(ta->weight, 16) || !aligned(ta->bias, 16) || !aligned(ta->A_log, 4) || !aligned(ta->dt_bias, 4))
+        return KVB_EINVAL;
+    if (ta->x_stride != 0 && (ta->x_stride < C || ta->x_stride > 1 << 26 || ta->x_stride * size > 1 << 26 || ta->x_stride * size % 16 != 0))
+        return KVB_EINVAL;
+    for (const int64_t s : {ta->a_stride, ta->b_stride})
+        if (s != 0 && (s < sh->Hv || s > 1 << 26))
+            return KVB_EINVAL;
+    if (ta->width < 1 || (ta->flags & ~KVB_CONV_UNIT) != 0 || !std::isfinite(ta->eps) || ((ta->flags & KVB_CONV_UNIT) && !(ta->eps > 0.0f)))
+        return KVB_EINVAL;
+    return ta->width >= 2 && ta->width <= 4 ? KVB_OK : KVB_EUNSUPPORTED;
+}
+// Workgroups of four waves, one for each unit
+bool conv_units_fit(const kvb_shape *sh, int64_t tokens) { return tokens <= INT32_MAX / (conv_groups((int)conv_channels(sh)) + 1); }
+
+// The inputs of a convolution's tokens, and whether there are gates
+int check_conv_inputs(const kvb_shape *sh, const kvb_taps *ta, bool tokens, const void *x, const void *a, const void *b, const void *state0)
+{
+    const size_t size = sh->in_dtype == KVB_F32 ? 4 : 2;
+    if (!aligned(x, 16) || !aligned(a, size) || !aligned(b, size) || !aligned(state0, 16) || (tokens && !x) || !a != !b)
+        return KVB_EINVAL;
+    return a && (!ta->A_log || !ta->dt_bias) ? KVB_EINVAL : KVB_OK;
+}
+int check_conv_outputs(bool tokens, bool gates, const void *q, const void *k, const void *v, const float *g, const float *beta)
+{
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(g, 4) || !aligned(beta, 4) || (tokens && (!q || !k || !v)))
+        return KVB_EINVAL;
+    return tokens && (gates != (g != nullptr) || gates != (beta != nullptr)) ? KVB_EINVAL : KVB_OK;
+}
+
+ConvArgs conv_args(const kvb_shape *sh, const kvb_taps *ta, const void *x, const void *a, const void *b, const void *state0)
+{
+    ConvArgs r{};
+    const int64_t C = conv_channels(sh);
+    r.x = x, r.a = a, r.b = b, r.weight = ta->weight, r.bias = ta->bias, r.A_log = ta->A_log, r.dt_bias = ta->dt_bias, r.state0 = state0;
+    r.x_stride = ta->x_stride ? ta->x_stride : C, r.a_stride = ta->a_stride ? ta->a_stride : sh->Hv, r.b_stride = ta->b_stride ? ta->b_stride : sh->Hv;
+    r.q_stride = r.k_stride = (int64_t)sh->Hk * sh->dk, r.v_stride = (int64_t)sh->Hv * sh->dv;
+    r.B = sh->B, r.T = 1, r.Hk = sh->Hk, r.Hv = sh->Hv, r.d = sh->dk, r.C = (int)C, r.gates = a != nullptr, r.unit = ta->flags & KVB_CONV_UNIT, r.eps = ta->eps;
+    return r;
+}
+void conv_seqs(ConvArgs &r, const kvb_seqs *sq)
+{
+    r.start = sq->start, r.slot = sq->slot, r.n_slots = sq->n_slots, r.n_tokens = sq->n_tokens;
+    r.q_stride = sq->q_stride ? sq->q_stride : r.q_stride, r.k_stride = sq->k_stride ? sq->k_stride : r.k_stride, r.v_stride = sq->v_stride ? sq->v_stride : r.v_stride;
+}
+int check_conv_seqs(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
+{
+    int rc = check_taps(sh, ta);
+    if (rc != KVB_OK)
+        return rc;
+    kvb_shape own = *sh;   // (types of outputs mean nothing here)
+    own.out_dtype = KVB_F32;
+    rc = check_seqs(&own, sq);
+    if (rc != KVB_OK)
+        return rc;
+    return conv_units_fit(sh, pieces_of(sq->n_tokens, sh->B, CONV_LEAST_LG)) ? KVB_OK : KVB_EINVAL;
+}
+// T tokens of each of B requests
+int conv_tokens_common(const kvb_shape *sh, const kvb_taps *ta, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent, const void *x,
+                       const void *a, const void *b, const void *state0, void *state1, void *q, void *k, void *v, float *g, float *beta, void *stream)
+{
+    int rc = check_taps(sh, ta);
+    if (rc == KVB_OK)
+        rc = check_conv_inputs(sh, ta, sh->B > 0, x, a, b, state0);
+    if (rc == KVB_OK)
+        rc = check_conv_outputs(sh->B > 0, a != nullptr, q, k, v, g, beta);
+    if (rc != KVB_OK)
+        return rc;
+    if ((sh->B > 0 && !slot) || !aligned(slot, 4) || !aligned(parent, 4) || !aligned(state1, 16) || n_slots < 0 || T < 1 || T > KVB_MAX_DRAFTS)
+        return KVB_EINVAL;
+    if (!conv_units_fit(sh, (int64_t)sh->B * T))
+        return KVB_EINVAL;
+    if (sh->B == 0)
+        return KVB_OK;
+    ConvArgs r = conv_args(sh, ta, x, a, b, state0);
+    r.slot = slot, r.n_slots = n_slots, r.T = T, r.parent = parent, r.state1 = state1;
+    r.q = q, r.k = k, r.v = v, r.g = g, r.beta = beta;
+    g_launch_status = hipSuccess;
+    launch_conv_tokens(sh->in_dtype, ta->width, r, static_cast<hipStream_t>(stream));
+    return finish_launch();
+}
+
+int64_t conv_columns(const ConvArgs &r, int width) { return (int64_t)(width + (r.bias != nullptr)) * r.C + (r.gates ? 2 * r.Hv : 0); }
+
+// Workspace for the gates' columns too: what there is of them is not known here
+int64_t conv_grad_work_bytes(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
+{
+    const int64_t C = conv_channels(sh), columns = (ta->width + 1) * C + 2 * sh->Hv;
+    return 4 * columns * conv_most_parts(sq->n_tokens, sh->B);
+}
+
+int check_rows(const kvb_rows *ro)
+{
+    if (!ro || ro->n_tokens < 0 || ro->heads < 1 || ro->width < 8 || ro->width > KVB_MAX_WIDTH || ro->width % 8 != 0)
+        return KVB_EINVAL;
+    for (const int t : {ro->dtype, ro->x_dtype})
+        if (t != KVB_F32 && t != KVB_BF16 && t != KVB_F16)
+            return KVB_EUNSUPPORTED;
+    if (ro->x_dtype != KVB_F32 && ro->x_dtype != ro->dtype)
+        return KVB_EUNSUPPORTED;
+    if (!(ro->eps > 0.0f) || !std::isfinite(ro->eps) || !std::isfinite(ro->scale))
+        return KVB_EINVAL;
+    const int64_t w = (int64_t)ro->heads * ro->width, size[2] = {ro->x_dtype == KVB_F32 ? 4 : 2, ro->dtype == KVB_F32 ? 4 : 2}, stride[2] = {ro->x_stride, ro->gate_stride};
+    for (int i = 0; i < 2; ++i)
+        if (w * 4 > 1 << 26 || (stride[i] != 0 && (stride[i] < w || stride[i] > 1 << 26 || stride[i] * size[i] > 1 << 26 || stride[i] * size[i] % 16 != 0)))
+            return KVB_EINVAL;
+    return (int64_t)ro->n_tokens * ro->heads > INT32_MAX ? KVB_EINVAL : KVB_OK;
+}
+NormArgs norm_args(const kvb_rows *ro, const void *x, const void *res, const void *gate, const void *weight, void *sum, void *out)
+{
+    const int64_t w = (int64_t)ro->heads * ro->width;
+    return NormArgs{x, res, gate, weight, sum, out, ro->x_stride ? ro->x_stride : w, ro->gate_stride ? ro->gate_stride : w, (int64_t)ro->n_tokens * ro->heads,
+                    ro->heads, ro->width, ro->eps, ro->scale};
+}
+// (dispatch_types has the pairs the other way round: the narrower type first)
+template <typename F>
+int norm_types(const kvb_rows *ro, F &&f)
+{
+    return dispatch_types(ro->dtype, ro->x_dtype, [&]<typename T, typename TX>() { f.template operator()<TX, T>(); });
+}
+
+int check_list(const kvb_list *li)
+{
+    if (!li || li->n < 0 || li->blocks < 0 || (li->n == 0 && li->blocks > 0))
+        return KVB_EINVAL;
+    if (li->n > 0 && (!li->data || !li->size || !li->type || !li->first))
+        return KVB_EINVAL;
+    return aligned(li->data, 8) && aligned(li->size, 8) && aligned(li->type, 4) && aligned(li->first, 4) ? KVB_OK : KVB_EINVAL;
+}
+
 }  // namespace
 
 extern "C" {
+
+int kvb_conv(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs, const void *x, const void *a, const void *b, const void *state0,
+             void *state1, void *q, void *k, void *v, float *g, float *beta, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_conv_seqs(shape, taps, seqs);
+    if (rc == KVB_OK)
+        rc = check_conv_inputs(shape, taps, seqs->n_tokens > 0, x, a, b, state0);
+    if (rc == KVB_OK)
+        rc = check_conv_outputs(seqs->n_tokens > 0, a != nullptr, q, k, v, g, beta);
+    if (rc != KVB_OK)
+        return rc;
+    if (!seqs->start || !aligned(seqs->start, 4) || !aligned(seqs->slot, 4) || !aligned(state1, 16))
+        return KVB_EINVAL;
+    if (shape->B == 0)
+        return KVB_OK;
+    ConvArgs r = conv_args(shape, taps, x, a, b, state0);
+    conv_seqs(r, seqs);
+    r.state1 = state1, r.q = q, r.k = k, r.v = v, r.g = g, r.beta = beta;
+    g_launch_status = hipSuccess;
+    launch_conv(shape->in_dtype, taps->width, r, static_cast<hipStream_t>(stream));
+    return finish_launch();
+}
+
+int kvb_conv_decode(const kvb_shape *shape, const kvb_taps *taps, const int32_t *slot, int32_t n_slots, const void *x, const void *a, const void *b,
+                    const void *state0, void *state1, void *q, void *k, void *v, float *g, float *beta, void *stream)
+{
+    DisarmOnExit disarm;
+    return conv_tokens_common(shape, taps, slot, n_slots, 1, nullptr, x, a, b, state0, state1, q, k, v, g, beta, stream);
+}
+
+int kvb_conv_verify(const kvb_shape *shape, const kvb_taps *taps, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent, const void *x,
+                    const void *a, const void *b, const void *state, void *q, void *k, void *v, float *g, float *beta, void *stream)
+{
+    DisarmOnExit disarm;
+    return conv_tokens_common(shape, taps, slot, n_slots, T, parent, x, a, b, state, nullptr, q, k, v, g, beta, stream);
+}
+
+int kvb_conv_commit(const kvb_shape *shape, const kvb_taps *taps, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *path,
+                    const int32_t *accepted, const void *x, const void *state0, void *state1, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_taps(shape, taps);
+    if (rc == KVB_OK)
+        rc = check_conv_inputs(shape, taps, shape->B > 0, x, nullptr, nullptr, state0);
+    if (rc != KVB_OK)
+        return rc;
+    if ((shape->B > 0 && (!slot || !accepted || !state1)) || !aligned(slot, 4) || !aligned(path, 4) || !aligned(accepted, 4) || !aligned(state1, 16) || n_slots < 0 || T < 1 ||
+        T > KVB_MAX_DRAFTS || !conv_units_fit(shape, shape->B))
+        return KVB_EINVAL;
+    if (shape->B == 0)
+        return KVB_OK;
+    ConvArgs r = conv_args(shape, taps, x, nullptr, nullptr, state0);
+    r.slot = slot, r.n_slots = n_slots, r.T = T, r.path = path, r.accepted = accepted, r.state1 = state1;
+    g_launch_status = hipSuccess;
+    launch_conv_commit(shape->in_dtype, taps->width, r, static_cast<hipStream_t>(stream));
+    return finish_launch();
+}
+
+int64_t kvb_conv_backward_work(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs)
+{
+    const int rc = check_conv_seqs(shape, taps, seqs);
+    return rc != KVB_OK ? rc : conv_grad_work_bytes(shape, taps, seqs);
+}
+
+int kvb_conv_backward(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs, const void *x, const void *a, const void *b,
+                      const void *state0, const void *dq, const void *dk, const void *dv, const float *dg, const float *dbeta, const void *dstate1,
+                      void *dx, void *da, void *db, float *dweight, float *dbias, float *dA_log, float *ddt_bias, void *dstate0, void *work, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_conv_seqs(shape, taps, seqs);
+    const bool tokens = rc == KVB_OK && seqs->n_tokens > 0, gates = tokens ? a != nullptr : dA_log != nullptr;
+    if (rc == KVB_OK)
+        rc = check_conv_inputs(shape, taps, tokens, x, a, b, state0);
+    if (rc == KVB_OK)
+        rc = check_conv_outputs(tokens, gates, dq, dk, dv, dg, dbeta);
+    if (rc != KVB_OK)
+        return rc;
+    const size_t size = shape->in_dtype == KVB_F32 ? 4 : 2;
+    if (!seqs->start || !aligned(seqs->start, 4) || !aligned(seqs->slot, 4) || !aligned(dstate1, 16) || !aligned(dx, 16) || !aligned(da, size) || !aligned(db, size) ||
+        !aligned(dweight, 4) || !aligned(dbias, 4) || !aligned(dA_log, 4) || !aligned(ddt_bias, 4) || !aligned(dstate0, 16) || !aligned(work, 16))
+        return KVB_EINVAL;
+    if ((tokens && (!dx || gates != (da != nullptr) || gates != (db != nullptr))) || !dweight || !work || (dbias != nullptr) != (taps->bias != nullptr) ||
+        gates != (dA_log != nullptr) || gates != (ddt_bias != nullptr) || (dstate0 && dstate0 == dstate1))
+        return KVB_EINVAL;
+    ConvGradArgs r{};
+    r.f = conv_args(shape, taps, x, a, b, state0);
+    conv_seqs(r.f, seqs);
+    r.f.gates = gates;
+    r.dq = dq, r.dk = dk, r.dv = dv, r.dg = dg, r.dbeta = dbeta, r.dstate1 = dstate1, r.dx = dx, r.da = da, r.db = db, r.dstate0 = dstate0;
+    const ConvParts parts = conv_parts(seqs->n_tokens, shape->B, r.f.C);
+    r.part = static_cast<float *>(work), r.parts = parts.parts, r.each = parts.each, r.columns = (int)conv_columns(r.f, taps->width);
+    g_launch_status = hipSuccess;
+    hipStream_t hs = static_cast<hipStream_t>(stream);
+    if (shape->in_dtype == KVB_F32)
+        launch_conv_grad_typed<float>(taps->width, r, parts.lg, dweight, dbias, dA_log, ddt_bias, hs);
+    else if (shape->in_dtype == KVB_BF16)
+        launch_conv_grad_typed<bf16_t>(taps->width, r, parts.lg, dweight, dbias, dA_log, ddt_bias, hs);
+    else
+        launch_conv_grad_typed<f16_t>(taps->width, r, parts.lg, dweight, dbias, dA_log, ddt_bias, hs);
+    return finish_launch();
+}
+
+int kvb_norm(const kvb_rows *rows, const void *x, const void *res, const void *gate, const void *weight, void *sum, void *out, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_rows(rows);
+    if (rc != KVB_OK)
+        return rc;
+    if (!aligned(x, 16) || !aligned(res, 16) || !aligned(gate, 16) || !aligned(weight, 16) || !aligned(sum, 16) || !aligned(out, 16))
+        return KVB_EINVAL;
+    if (rows->n_tokens == 0)   // (arrays of no elements may be NULL)
+        return KVB_OK;
+    if (!x || !weight || !out || (!res && (sum || rows->scale != 1.0f)))
+        return KVB_EINVAL;
+    const NormArgs a = norm_args(rows, x, res, gate, weight, sum, out);
+    g_launch_status = hipSuccess;
+    rc = norm_types(rows, [&]<typename TX, typename T>() { launch_norm_typed<TX, T>(a, static_cast<hipStream_t>(stream)); });
+    if (rc != KVB_OK)
+        return rc;
+    return finish_launch();
+}
+
+int64_t kvb_norm_backward_work(const kvb_rows *rows)
+{
+    const int rc = check_rows(rows);
+    return rc != KVB_OK ? rc : 4 * (int64_t)rows->width * norm_most_parts((int64_t)rows->n_tokens * rows->heads, rows->width);
+}
+
+int kvb_norm_backward(const kvb_rows *rows, const void *x, const void *gate, const void *weight, const void *dout, const void *dsum, void *dx, void *dres,
+                      void *dgate, float *dweight, void *work, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_rows(rows);
+    if (rc != KVB_OK)
+        return rc;
+    if (!aligned(x, 16) || !aligned(gate, 16) || !aligned(weight, 16) || !aligned(dout, 16) || !aligned(dsum, 16) || !aligned(dx, 16) || !aligned(dres, 16) ||
+        !aligned(dgate, 16) || !aligned(dweight, 4) || !aligned(work, 16))
+        return KVB_EINVAL;
+    if (!dweight || (rows->n_tokens > 0 && !weight) || (gate != nullptr) != (dgate != nullptr) || (rows->n_tokens > 0 && (!x || !dout || !dx || !work)))
+        return KVB_EINVAL;
+    NormGradArgs a{norm_args(rows, x, nullptr, gate, weight, nullptr, nullptr), dout, dsum, dx, dres, dgate, static_cast<float *>(work), 0, rows->scale};
+    a.parts = norm_parts(a.f.rows, a.f.width);
+    g_launch_status = hipSuccess;
+    rc = norm_types(rows, [&]<typename TX, typename T>() { launch_norm_grad_typed<TX, T>(a, dweight, static_cast<hipStream_t>(stream)); });
+    if (rc != KVB_OK)
+        return rc;
+    return finish_launch();
+}
+
+int64_t kvb_grad_norm_work(const kvb_list *list)
+{
+    const int rc = check_list(list);
+    return rc != KVB_OK ? rc : 8 * (int64_t)list->blocks;
+}
+
+int kvb_grad_norm(const kvb_list *list, float *norm, void *work, void *stream)
+{
+    DisarmOnExit disarm;
+    const int rc = check_list(list);
+    if (rc != KVB_OK)
+        return rc;
+    if (!norm || !aligned(norm, 4) || !aligned(work, 8) || (list->blocks > 0 && !work))
+        return KVB_EINVAL;
+    g_launch_status = hipSuccess;
+    launch_grad_norm(ListArgs{list->data, nullptr, list->size, list->type, list->first, list->n, list->blocks}, norm, static_cast<double *>(work),
+                     static_cast<hipStream_t>(stream));
+    return finish_launch();
+}
+
+int kvb_clip(const kvb_list *list, const kvb_list *to, const float *norm, float largest, void *stream)
+{
+    DisarmOnExit disarm;
+    int rc = check_list(list);
+    if (rc == KVB_OK && to)
+        rc = check_list(to);
+    if (rc != KVB_OK)
+        return rc;
+    if (!norm || !aligned(norm, 4) || !(largest >= 0.0f) || (to && (to->n != list->n || to->blocks != list->blocks)))
+        return KVB_EINVAL;
+    if (list->blocks == 0)
+        return KVB_OK;
+    g_launch_status = hipSuccess;
+    launch_clip(ListArgs{list->data, to ? to->data : list->data, list->size, list->type, list->first, list->n, list->blocks}, norm, largest,
+                static_cast<hipStream_t>(stream));
+    return finish_launch();
+}
 
 int64_t kvb_accept_work(const kvb_vocab *vocab)
 {

@@ -1,0 +1,318 @@
+// kvb_conv, kvb_conv_decode, kvb_conv_verify, kvb_conv_commit: what makes a layer's queries, keys, values and gates from the rows of its
+// projection.  With E the state's rows followed by a sequence's inputs,
+//     z_t = bias + sum_i w_i E_{t+i},  y = z / (1 + exp(-z)),  q, k = y / sqrt(sum y^2 + eps) over a head,  v = y
+//     g = -exp(A_log) log(1 + exp(a + dt_bias)),  beta = 1 / (1 + exp(-b))
+// A lane has 8 channels, so that loads and stores are 16 bytes (16-bit types), a head is 4, 8 or 16 neighbouring lanes and its sum of squares
+// stays inside a row of 16.  A wave has 512 channels; the units behind the channels' are the gates'.
+#include "kvb_layer_device.h"
+
+namespace kvb_impl {
+
+namespace {
+
+// A lane's 8 channels: their weights, where their results go
+template <typename T, int W>
+struct Lane8 {
+    float w[W][8], bias[8];
+    T *to;               // the first token's
+    int64_t to_stride;
+    int lg;              // 2^lg lanes a head
+    bool unit;           // q or k, to be of length one
+    float eps;
+
+    __device__ __forceinline__ Lane8(const ConvArgs &a, int ch) : lg(a.d == 128 ? 4 : a.d == 64 ? 3 : 2), eps(a.eps)
+    {
+        const T *wp = static_cast<const T *>(a.weight) + (int64_t)ch * W;
+        Raw8<T> raw[W], rb{};
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            raw[i] = load_raw8(wp + 8 * i);
+        if (a.bias)
+            rb = load_raw8(static_cast<const T *>(a.bias) + ch);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {   // (8 channels of W taps each, one after the other)
+            float y[8];
+            unpack8(raw[i], y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                w[(8 * i + j) % W][(8 * i + j) / W] = y[j];
+        }
+        unpack8(rb, bias);
+        const int nq = a.Hk * a.d;
+        unit = a.unit && ch < 2 * nq;
+        to = ch < nq ? static_cast<T *>(a.q) + ch : ch < 2 * nq ? static_cast<T *>(a.k) + (ch - nq) : static_cast<T *>(a.v) + (ch - 2 * nq);
+        to_stride = ch < nq ? a.q_stride : ch < 2 * nq ? a.k_stride : a.v_stride;
+    }
+    // y from z, and of length one
+    __device__ __forceinline__ void finish(float (&z)[8]) const
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            z[j] *= sigmoid(z[j]);
+            sum = fmaf(z[j], z[j], sum);
+        }
+        sum = sum_to16(sum, lg);
+        const float r = unit ? __builtin_amdgcn_rsqf(sum + eps) : 1.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] *= r;
+    }
+};
+
+// Gates of the tokens t0 .. t1-1
+template <typename T>
+__device__ __forceinline__ void gates_of(const ConvArgs &a, int64_t t0, int n, int lane)
+{
+    const GateLanes l = gate_lanes(a.Hv, lane);
+    for (int h = l.head; h < a.Hv; h += l.heads) {
+        const float rate = -expf(a.A_log[h]), shift = a.dt_bias[h];
+#pragma unroll 4
+        for (int t = l.token; t < n; t += l.tokens) {
+            const float y = to_f32(static_cast<const T *>(a.a)[(t0 + t) * a.a_stride + h]) + shift;
+            const float b = to_f32(static_cast<const T *>(a.b)[(t0 + t) * a.b_stride + h]);
+            a.g[(t0 + t) * a.Hv + h] = rate * softplus(y);
+            a.beta[(t0 + t) * a.Hv + h] = 1.0f / (1.0f + expf(-b));
+        }
+    }
+}
+
+}  // namespace
+
+// Whole sequences: a wave takes 2^lg tokens of one of them, with the taps' inputs in registers.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int units, int lg)
+{
+    constexpr int U = 4;   // tokens at a time
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
+    const int unit = blockIdx.x * 4 + wave, each = groups + a.gates;
+    if (unit >= units)
+        return;
+    const int w = unit / each, group = unit - w * each;
+    const Piece p = piece_at(a.start, a.n_tokens, a.B, w, lg);
+    const int row = state_row(a.slot, a.n_slots, p.b);
+    if (!p.some || row < 0)
+        return;
+    if (group == groups) {
+        gates_of<T>(a, (int64_t)p.first + p.t0, p.t1 - p.t0, lane);
+        return;
+    }
+    const int ch = group * CONV_LANES + lane * 8;
+    if (ch >= a.C)
+        return;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)p.first * a.x_stride + ch;
+    const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch : nullptr;
+    auto input_at = [&](int e) {   // row e of E
+        if (e >= W - 1)
+            return load_raw8(x + (int64_t)(e - (W - 1)) * a.x_stride);
+        return s0 ? load_raw8(s0 + (int64_t)e * a.C) : Raw8<T>{};
+    };
+    if (p.t0 < p.t1) {
+        Raw8<T> raw[U], before[W - 1];
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            before[i] = input_at(p.t0 + i);
+        auto request = [&](int t) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                raw[u] = load_raw8(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
+        };
+        request(p.t0);
+        const Lane8<T, W> l(a, ch);
+        float e[W - 1 + U][8];
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            unpack8(before[i], e[i]);
+        for (int t = p.t0; t < p.t1; t += U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                unpack8(raw[u], e[W - 1 + u]);
+            if (t + U < p.t1)
+                request(t + U);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (t + u < p.t1) {
+                    float z[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        z[j] = l.bias[j];
+#pragma unroll
+                        for (int i = 0; i < W; ++i)
+                            z[j] = fmaf(l.w[i][j], e[u + i][j], z[j]);
+                    }
+                    l.finish(z);
+                    store8(l.to + ((int64_t)p.first + t + u) * l.to_stride, z);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    e[i][j] = e[U + i][j];
+        }
+    }
+    // The first piece's wave writes the last state: nobody else reads the first one's rows, which it may lie in.
+    if (p.t0 == 0 && a.state1) {
+        T *s1 = static_cast<T *>(a.state1) + (int64_t)row * (W - 1) * a.C + ch;
+        Raw8<T> last[W - 1];
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            last[i] = input_at(p.len + i);
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            store_raw8<false, true>(s1 + (int64_t)i * a.C, last[i]);
+    }
+}
+
+// T tokens of each request, a wave one of them: its taps' inputs are its ancestors and, behind the first of them, the state's rows.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, int units)
+{
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
+    const int unit = blockIdx.x * 4 + wave, each = groups + a.gates;
+    if (unit >= units)
+        return;
+    const int token = unit / each, group = unit - token * each, b = token / a.T, i0 = token - b * a.T;
+    const int row = state_row(a.slot, a.n_slots, b);
+    if (row < 0)
+        return;
+    if (group == groups) {
+        gates_of<T>(a, token, 1, lane);
+        return;
+    }
+    int up = -1;   // lane i: draft i's parent
+    if (a.parent) {
+        const int i = min(lane, a.T - 1), p = a.parent[(int64_t)b * a.T + i];
+        up = p < -1 || p >= i ? -1 : p;
+    } else {
+        up = lane - 1;
+    }
+    const int ch = group * CONV_LANES + lane * 8;
+    // places: a draft, or row W - 1 + place of the state
+    int place[W];
+    place[W - 1] = i0;
+#pragma unroll
+    for (int i = W - 2; i >= 0; --i)
+        place[i] = place[i + 1] >= 0 ? __builtin_amdgcn_readlane(up, place[i + 1]) : place[i + 1] - 1;
+    if (ch >= a.C)
+        return;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)b * a.T * a.x_stride + ch;
+    const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch : nullptr;
+    Raw8<T> raw[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if (place[i] >= 0)
+            raw[i] = load_raw8(x + (int64_t)place[i] * a.x_stride);
+        else
+            raw[i] = s0 ? load_raw8(s0 + (int64_t)(W - 1 + place[i]) * a.C) : Raw8<T>{};
+    }
+    const Lane8<T, W> l(a, ch);
+    float z[8], e[W][8];
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+        unpack8(raw[i], e[i]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        z[j] = l.bias[j];
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            z[j] = fmaf(l.w[i][j], e[i][j], z[j]);
+    }
+    l.finish(z);
+    store8(l.to + (int64_t)token * l.to_stride, z);
+    if (a.state1) {   // (single tokens)
+        T *s1 = static_cast<T *>(a.state1) + (int64_t)row * (W - 1) * a.C + ch;
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            store_raw8<false, true>(s1 + (int64_t)i * a.C, raw[i + 1]);
+    }
+}
+
+// The state behind the accepted drafts: the last W - 1 rows of the state and theirs.
+template <typename T, int W>
+__global__ __launch_bounds__(256) void kvb_conv_commit_kernel(const ConvArgs a, int units)
+{
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
+    const int unit = blockIdx.x * 4 + wave;
+    if (unit >= units)
+        return;
+    const int b = unit / groups, group = unit - b * groups;
+    const int row = state_row(a.slot, a.n_slots, b);
+    if (row < 0)
+        return;
+    int n = __builtin_amdgcn_readfirstlane(a.accepted[b]);
+    const int at = a.path ? a.path[(int64_t)b * a.T + min(lane, a.T - 1)] : lane, prev = __shfl_up(at, 1);
+    const bool good = lane >= n || (at >= 0 && at < a.T && (lane == 0 || at > prev));
+    n = n < 0 || n > a.T || !__all(good) ? 0 : n;
+    const int ch = group * CONV_LANES + lane * 8;
+    int from[W - 1];   // rows of E: the state's, then the accepted drafts'
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i)
+        from[i] = n + i < W - 1 ? -1 : __builtin_amdgcn_readlane(at, n + i - (W - 1));
+    if (ch >= a.C)
+        return;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)b * a.T * a.x_stride + ch;
+    const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch : nullptr;
+    T *s1 = static_cast<T *>(a.state1) + (int64_t)row * (W - 1) * a.C + ch;
+    Raw8<T> raw[W - 1];
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) {
+        if (from[i] >= 0)
+            raw[i] = load_raw8(x + (int64_t)from[i] * a.x_stride);
+        else
+            raw[i] = s0 ? load_raw8(s0 + (int64_t)(n + i) * a.C) : Raw8<T>{};
+    }
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i)
+        store_raw8<false, true>(s1 + (int64_t)i * a.C, raw[i]);
+}
+
+namespace {
+
+template <typename F>
+void with_width(int width, F &&f)
+{
+    if (width == 4)
+        f.template operator()<4>();
+    else if (width == 3)
+        f.template operator()<3>();
+    else
+        f.template operator()<2>();
+}
+template <typename F>
+void with_taps(int dtype, int width, F &&f)
+{
+    with_width(width, [&]<int W>() {
+        if (dtype == KVB_F32)
+            f.template operator()<float, W>();
+        else if (dtype == KVB_BF16)
+            f.template operator()<bf16_t, W>();
+        else
+            f.template operator()<f16_t, W>();
+    });
+}
+
+int conv_lg(int64_t n_tokens, int groups) { return n_tokens * groups >= 1 << 16 ? 5 : 3; }
+
+}  // namespace
+
+void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
+{
+    const int groups = conv_groups(a.C), lg = conv_lg(a.n_tokens, groups);
+    const int units = (int)(pieces_of(a.n_tokens, a.B, lg) * (groups + a.gates));
+    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units, lg); });
+}
+
+void launch_conv_tokens(int dtype, int width, const ConvArgs &a, hipStream_t stream)
+{
+    const int units = a.B * a.T * (conv_groups(a.C) + a.gates);
+    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_token_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units); });
+}
+
+void launch_conv_commit(int dtype, int width, const ConvArgs &a, hipStream_t stream)
+{
+    const int units = a.B * conv_groups(a.C);
+    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_commit_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units); });
+}
+
+}  // namespace kvb_impl

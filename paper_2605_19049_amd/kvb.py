@@ -18,9 +18,14 @@ STATUS_OVERFLOW = 1
 STATUS_BADPATH = 2
 STORE_STREAM, STORE_RESIDENT, STORE_FILL_APART = 1, 2, 4
 FILL_APART = 32   # words from one slot's fill to the next with STORE_FILL_APART
+CONV_UNIT = 1
+MAX_WIDTH = 16384
+LIST_BLOCK = 16384
 
 EXPORTS = ("kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact", "kvb_direct",
            "kvb_scan_work", "kvb_scan", "kvb_scan_backward_work", "kvb_scan_backward", "kvb_accept_work", "kvb_accept",
+           "kvb_conv", "kvb_conv_decode", "kvb_conv_verify", "kvb_conv_commit", "kvb_conv_backward_work", "kvb_conv_backward",
+           "kvb_norm", "kvb_norm_backward_work", "kvb_norm_backward", "kvb_grad_norm_work", "kvb_grad_norm", "kvb_clip",
            "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read", "kvb_timer_destroy",
            "kvb_strerror", "kvb_version")
 
@@ -49,6 +54,22 @@ class KvbSeqs(ctypes.Structure):
 class KvbVocab(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("stride", ctypes.c_int64)]
+
+
+class KvbTaps(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("A_log", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("a_stride", ctypes.c_int64), ("b_stride", ctypes.c_int64), ("width", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class KvbRows(ctypes.Structure):
+    _fields_ = [("x_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64), ("n_tokens", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("x_dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class KvbList(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("size", ctypes.c_void_p), ("type", ctypes.c_void_p), ("first", ctypes.c_void_p),
+                ("n", ctypes.c_int32), ("blocks", ctypes.c_int32)]
 
 
 class KvbError(RuntimeError):
@@ -94,7 +115,23 @@ def lib():
         L.kvb_accept_work.argtypes = [op]
         L.kvb_accept.argtypes = [op] + [vp] * 12
         L.kvb_accept_work.restype = ctypes.c_int64
-        for name in ("kvb_scan", "kvb_scan_backward", "kvb_accept", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
+        ap, rp, lp = ctypes.POINTER(KvbTaps), ctypes.POINTER(KvbRows), ctypes.POINTER(KvbList)
+        L.kvb_conv.argtypes = [sp, ap, qp] + [vp] * 11
+        L.kvb_conv_decode.argtypes = [sp, ap, vp, i32] + [vp] * 11
+        L.kvb_conv_verify.argtypes = [sp, ap, vp, i32, i32] + [vp] * 11
+        L.kvb_conv_commit.argtypes = [sp, ap, vp, i32, i32] + [vp] * 6
+        L.kvb_conv_backward_work.argtypes = [sp, ap, qp]
+        L.kvb_conv_backward.argtypes = [sp, ap, qp] + [vp] * 20
+        L.kvb_norm.argtypes = [rp] + [vp] * 7
+        L.kvb_norm_backward_work.argtypes = [rp]
+        L.kvb_norm_backward.argtypes = [rp] + [vp] * 11
+        L.kvb_grad_norm_work.argtypes = [lp]
+        L.kvb_grad_norm.argtypes = [lp] + [vp] * 3
+        L.kvb_clip.argtypes = [lp, lp, vp, ctypes.c_float, vp]
+        for name in ("kvb_conv_backward_work", "kvb_norm_backward_work", "kvb_grad_norm_work"):
+            getattr(L, name).restype = ctypes.c_int64
+        for name in ("kvb_conv", "kvb_conv_decode", "kvb_conv_verify", "kvb_conv_commit", "kvb_conv_backward", "kvb_norm", "kvb_norm_backward",
+                     "kvb_grad_norm", "kvb_clip", "kvb_scan", "kvb_scan_backward", "kvb_accept", "kvb_decode", "kvb_decode_flush", "kvb_flush", "kvb_verify", "kvb_verify_tree", "kvb_compact",
                      "kvb_direct", "kvb_version",
                      "kvb_timer_create", "kvb_timer_arm", "kvb_timer_read"):
             getattr(L, name).restype = ctypes.c_int
@@ -294,10 +331,78 @@ def _check_accept(vo, args):
                 step = row if i == x.dim() - 1 and x.dim() > 1 else step * x.shape[i]
 
 
+_CONV_OUT = ("q", "k", "v", "g", "beta")
+_CONV_NAMES = {
+    "kvb_conv": ("x", "a", "b", "state0", "state1") + _CONV_OUT,
+    "kvb_conv_decode": ("slot", None, "x", "a", "b", "state0", "state1") + _CONV_OUT,
+    "kvb_conv_verify": ("slot", None, None, "parent", "x", "a", "b", "state") + _CONV_OUT,
+    "kvb_conv_commit": ("slot", None, None, "path", "accepted", "x", "state0", "state1"),
+    "kvb_conv_backward": ("x", "a", "b", "state0", "dq", "dk", "dv", "dg", "dbeta", "dstate1", "dx", "da", "db", "dweight", "dbias", "dA_log", "ddt_bias", "dstate0")}
+_NORM = ("x", "res", "gate", "weight", "sum", "out")
+_NORM_BACKWARD = ("x", "gate", "weight", "dout", "dsum", "dx", "dres", "dgate", "dweight")
+
+
+def _check_token_rows(what, x, said, width):
+    """Rows of `width` contiguous elements, `said` from one token to the next (0: packed).  The tokens may have any number of leading axes."""
+    if x is None or isinstance(x, int) or x.numel() == 0:
+        return
+    step, left, strided = 1, width, False
+    for i in reversed(range(x.dim())):
+        if left > 1:   # inside a token
+            if x.shape[i] > 1 and x.stride(i) != step:
+                break
+            if left % x.shape[i]:
+                break
+            left //= x.shape[i]
+            step *= x.shape[i]
+            continue
+        if not strided:
+            step, strided = said or width, True
+        if x.shape[i] > 1 and x.stride(i) != step:
+            break
+        step *= x.shape[i]
+    else:
+        if left == 1:
+            return
+    raise ValueError("%s of shape %s and stride %s: tokens of %d contiguous elements are wanted, %d from one to the next" %
+                     (what, tuple(x.shape), tuple(x.stride()), width, said or width))
+
+
+def _check_conv(names, sh, ta, sq, args):
+    """Inputs, and the gradients of inputs, lie as the kvb_taps says, results as the kvb_seqs (None: packed) says, the others packed."""
+    C = (2 * sh.Hk + sh.Hv) * sh.dk
+    said = {"x": (ta.x_stride, C), "dx": (ta.x_stride, C)}
+    for n, stride in (("a", ta.a_stride), ("b", ta.b_stride)):
+        said[n] = said["d" + n] = (stride, sh.Hv)
+    for n, h in (("q", sh.Hk), ("k", sh.Hk), ("v", sh.Hv)):
+        said[n] = said["d" + n] = (getattr(sq, n + "_stride") if sq is not None else 0, h * sh.dk)
+    for what, x in zip(names, args):
+        if what in said:
+            _check_token_rows(what, x, *said[what])
+        elif what is not None:
+            _check_packed(what, x)
+
+
+def _check_norm(names, ro, args):
+    said = {"x": ro.x_stride, "dx": ro.x_stride, "gate": ro.gate_stride, "dgate": ro.gate_stride}
+    for what, x in zip(names, args):
+        if what in said:
+            _check_token_rows(what, x, said[what], ro.heads * ro.width)
+        else:
+            _check_packed(what, x)
+
+
 def _check_layouts(fn_name, args):
     """ValueError where a tensor does not lie as the call takes it: the kernels would read or write other memory.  args: the C
     arguments.  Addresses are taken as they are."""
-    if fn_name == "kvb_scan":
+    if fn_name in _CONV_NAMES:
+        seqs_too = fn_name in ("kvb_conv", "kvb_conv_backward")
+        _check_conv(_CONV_NAMES[fn_name], args[0], args[1], args[2] if seqs_too else None, args[3 if seqs_too else 2:])
+    elif fn_name == "kvb_norm":
+        _check_norm(_NORM, args[0], args[1:])
+    elif fn_name == "kvb_norm_backward":
+        _check_norm(_NORM_BACKWARD, args[0], args[1:])
+    elif fn_name == "kvb_scan":
         _check_scan(_SCAN, args[1], args[2:])
     elif fn_name == "kvb_scan_backward":
         _check_scan(_BACKWARD, args[1], args[2:])
@@ -351,6 +456,122 @@ def kvb_accept(vo, n_drafts, parent, tokens, target, draft, u, s, path, accepted
     return _check(rc, "kvb_accept", check)
 
 
+def taps(weight, width=4, bias=None, A_log=None, dt_bias=None, x=None, a=None, b=None, unit=True, eps=1e-6):
+    """A kvb_taps; x, a, b: the tensors [.., row] whose token strides it takes (None: packed)."""
+    def stride(t, what):
+        if t is None or t.numel() == 0:
+            return 0
+        tokens = [i for i in range(t.dim() - 1) if t.shape[i] > 1]
+        if (t.shape[-1] > 1 and t.stride(-1) != 1) or (tokens and t.stride(tokens[-1]) < t.shape[-1]):
+            raise ValueError("%s of shape %s and stride %s: contiguous rows are wanted" % (what, tuple(t.shape), tuple(t.stride())))
+        return t.stride(tokens[-1]) if tokens else 0
+    for what, t in (("weight", weight), ("bias", bias), ("A_log", A_log), ("dt_bias", dt_bias)):
+        _check_packed(what, t)
+    return KvbTaps(_ptr(weight), _ptr(bias), _ptr(A_log), _ptr(dt_bias), stride(x, "x"), stride(a, "a"), stride(b, "b"), width, CONV_UNIT if unit else 0, eps)
+
+
+def _call(fn_name, *args, stream=None, check=True):
+    """args: the C arguments, structs first, without the stream"""
+    _check_layouts(fn_name, args)
+    conv = [ctypes.byref(x) if isinstance(x, ctypes.Structure) else x if t in (ctypes.c_int32, ctypes.c_float) else _ptr(x)
+            for x, t in zip(args, getattr(lib(), fn_name).argtypes)]
+    return _check(getattr(lib(), fn_name)(*conv, _stream(stream)), fn_name, check)
+
+
+def kvb_conv(sh, ta, sq, x, a, b, state0, state1, q, k, v, g, beta, stream=None, check=True):
+    """x, a, b lie as the kvb_taps says, q, k, v as the kvb_seqs says, the other arrays packed; ValueError for a tensor that does not."""
+    return _call("kvb_conv", sh, ta, sq, x, a, b, state0, state1, q, k, v, g, beta, stream=stream, check=check)
+
+
+def kvb_conv_decode(sh, ta, slot, n_slots, x, a, b, state0, state1, q, k, v, g, beta, stream=None, check=True):
+    return _call("kvb_conv_decode", sh, ta, slot, n_slots, x, a, b, state0, state1, q, k, v, g, beta, stream=stream, check=check)
+
+
+def kvb_conv_verify(sh, ta, slot, n_slots, T, parent, x, a, b, state, q, k, v, g, beta, stream=None, check=True):
+    return _call("kvb_conv_verify", sh, ta, slot, n_slots, T, parent, x, a, b, state, q, k, v, g, beta, stream=stream, check=check)
+
+
+def kvb_conv_commit(sh, ta, slot, n_slots, T, path, accepted, x, state0, state1, stream=None, check=True):
+    return _call("kvb_conv_commit", sh, ta, slot, n_slots, T, path, accepted, x, state0, state1, stream=stream, check=check)
+
+
+def conv_backward_work(sh, ta, sq):
+    """Bytes of workspace that kvb_conv_backward needs."""
+    return _work(lib().kvb_conv_backward_work(ctypes.byref(sh), ctypes.byref(ta), ctypes.byref(sq)), "kvb_conv_backward_work")
+
+
+def kvb_conv_backward(sh, ta, sq, x, a, b, state0, dq, dk, dv, dg, dbeta, dstate1, dx, da, db, dweight, dbias, dA_log, ddt_bias, dstate0, work,
+                      stream=None, check=True):
+    """dx, da, db lie as x, a, b do (the strides in ta), dq, dk, dv as the kvb_seqs says, the other arrays packed; ValueError for a tensor that does not."""
+    return _call("kvb_conv_backward", sh, ta, sq, x, a, b, state0, dq, dk, dv, dg, dbeta, dstate1, dx, da, db, dweight, dbias, dA_log, ddt_bias,
+                      dstate0, work, stream=stream, check=check)
+
+
+def rows(n_tokens, heads, width, dtype, x_dtype=None, x=None, gate=None, eps=1e-6, scale=1.0):
+    """A kvb_rows; x, gate: the tensors [n_tokens, heads, width] (or [n_tokens, width]) whose token strides it takes (None: packed)."""
+    def stride(t, what):
+        return 0 if t is None else _token_stride(t if t.dim() == 3 else t.unflatten(-1, (heads, width)), what)
+    return KvbRows(stride(x, "x"), stride(gate, "gate"), n_tokens, heads, width, dtype, dtype if x_dtype is None else x_dtype, eps, scale)
+
+
+def kvb_norm(ro, x, res, gate, weight, sum, out, stream=None, check=True):
+    return _call("kvb_norm", ro, x, res, gate, weight, sum, out, stream=stream, check=check)
+
+
+def norm_backward_work(ro):
+    """Bytes of workspace that kvb_norm_backward needs."""
+    return _work(lib().kvb_norm_backward_work(ctypes.byref(ro)), "kvb_norm_backward_work")
+
+
+def kvb_norm_backward(ro, x, gate, weight, dout, dsum, dx, dres, dgate, dweight, work, stream=None, check=True):
+    """dx and dgate lie as x and gate do (the strides in ro), the other arrays packed; ValueError for a tensor that does not."""
+    return _call("kvb_norm_backward", ro, x, gate, weight, dout, dsum, dx, dres, dgate, dweight, work, stream=stream, check=check)
+
+
+class TensorList:
+    """The device arrays of a kvb_list over some tensors, made once (a copy to the device each); it keeps the tensors.  c() is the kvb_list."""
+
+    def __init__(self, tensors, device=None):
+        import torch
+        self.tensors = list(tensors)
+        codes = {torch_dtype(c): c for c in (F32, BF16, F16)}
+        for t in self.tensors:
+            if t.dtype not in codes:
+                raise ValueError("a tensor of %s: float32, bfloat16 and float16 are wanted" % t.dtype)
+            _check_packed("a tensor", t)
+        where = {t.device for t in self.tensors}
+        if len(where) > 1:
+            raise ValueError("tensors on several devices: %s" % sorted(map(str, where)))
+        device = where.pop() if where else device or "cuda"
+        self.sizes, self.types, first = [t.numel() for t in self.tensors], [codes[t.dtype] for t in self.tensors], [0]
+        for n in self.sizes:
+            first.append(first[-1] - (-n // LIST_BLOCK))
+        self.blocks = first[-1]
+        if self.blocks > 2 ** 31 - 1:
+            raise ValueError("too many elements")
+        self._data, self._size = (torch.tensor(x, dtype=torch.int64, device=device) for x in ([t.data_ptr() for t in self.tensors], self.sizes))
+        self._type, self._first = (torch.tensor(x, dtype=torch.int32, device=device) for x in (self.types, first))
+
+    def c(self):
+        some = bool(self.tensors)
+        return KvbList(*((_ptr(x) if some else None) for x in (self._data, self._size, self._type, self._first)), len(self.tensors), self.blocks)
+
+
+def grad_norm_work(li):
+    """Bytes of workspace that kvb_grad_norm needs."""
+    return _work(lib().kvb_grad_norm_work(ctypes.byref(li)), "kvb_grad_norm_work")
+
+
+def kvb_grad_norm(li, norm, work, stream=None, check=True):
+    """li: a kvb_list, TensorList(..).c()"""
+    return _call("kvb_grad_norm", li, norm, work, stream=stream, check=check)
+
+
+def kvb_clip(li, to, norm, largest, stream=None, check=True):
+    """to: a kvb_list of tensors of the same sizes and types, or None: in place"""
+    return _call("kvb_clip", li, to, norm, largest, stream=stream, check=check)
+
+
 def bind(fn_name, *args):
     """Pre-marshal one call: returns a zero-argument callable that re-issues it with the
     same pointers (for serving loops, where per-call marshalling would rival a 20 us
@@ -362,6 +583,8 @@ def bind(fn_name, *args):
     for a, t in zip(args, fn.argtypes):
         if isinstance(a, ctypes.Structure):
             conv.append(ctypes.byref(a))
+        elif a is None:
+            conv.append(None)
         elif t is ctypes.c_void_p:
             conv.append(ctypes.c_void_p(_ptr(a)))
         else:
