@@ -289,7 +289,7 @@ int check_conv_seqs(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
     rc = check_seqs(&own, sq);
     if (rc != KVB_OK)
         return rc;
-    return conv_units_fit(sh, pieces_of(sq->n_tokens, sh->B, CONV_LEAST_LG)) ? KVB_OK : KVB_EINVAL;
+    return conv_units_fit(sh, pieces_of(sq->n_tokens, sh->B, CONV_LEAST)) ? KVB_OK : KVB_EINVAL;
 }
 // T tokens of each of B requests
 int conv_tokens_common(const kvb_shape *sh, const kvb_taps *ta, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent, const void *x,
@@ -322,7 +322,7 @@ int64_t conv_columns(const ConvArgs &r, int width) { return (int64_t)(width + (r
 int64_t conv_grad_work_bytes(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
 {
     const int64_t C = conv_channels(sh), columns = (ta->width + 1) * C + 2 * sh->Hv;
-    return 4 * columns * conv_most_parts(sq->n_tokens, sh->B);
+    return 4 * columns * conv_most_parts(sq->n_tokens, sh->B, conv_groups((int)C));
 }
 
 int check_rows(const kvb_rows *ro)
@@ -457,16 +457,16 @@ int kvb_conv_backward(const kvb_shape *shape, const kvb_taps *taps, const kvb_se
     conv_seqs(r.f, seqs);
     r.f.gates = gates;
     r.dq = dq, r.dk = dk, r.dv = dv, r.dg = dg, r.dbeta = dbeta, r.dstate1 = dstate1, r.dx = dx, r.da = da, r.db = db, r.dstate0 = dstate0;
-    const ConvParts parts = conv_parts(seqs->n_tokens, shape->B, r.f.C);
+    const ConvParts parts = conv_parts(seqs->n_tokens, shape->B, conv_groups(r.f.C) + gates);
     r.part = static_cast<float *>(work), r.parts = parts.parts, r.each = parts.each, r.columns = (int)conv_columns(r.f, taps->width);
     g_launch_status = hipSuccess;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     if (shape->in_dtype == KVB_F32)
-        launch_conv_grad_typed<float>(taps->width, r, parts.lg, dweight, dbias, dA_log, ddt_bias, hs);
+        launch_conv_grad_typed<float>(taps->width, r, parts.most, dweight, dbias, dA_log, ddt_bias, hs);
     else if (shape->in_dtype == KVB_BF16)
-        launch_conv_grad_typed<bf16_t>(taps->width, r, parts.lg, dweight, dbias, dA_log, ddt_bias, hs);
+        launch_conv_grad_typed<bf16_t>(taps->width, r, parts.most, dweight, dbias, dA_log, ddt_bias, hs);
     else
-        launch_conv_grad_typed<f16_t>(taps->width, r, parts.lg, dweight, dbias, dA_log, ddt_bias, hs);
+        launch_conv_grad_typed<f16_t>(taps->width, r, parts.most, dweight, dbias, dA_log, ddt_bias, hs);
     return finish_launch();
 }
 
@@ -520,7 +520,7 @@ int kvb_norm_backward(const kvb_rows *rows, const void *x, const void *gate, con
 int64_t kvb_grad_norm_work(const kvb_list *list)
 {
     const int rc = check_list(list);
-    return rc != KVB_OK ? rc : 8 * (int64_t)list->blocks;
+    return rc != KVB_OK ? rc : 8 * (int64_t)list->blocks * list_split(list->blocks);
 }
 
 int kvb_grad_norm(const kvb_list *list, float *norm, void *work, void *stream)

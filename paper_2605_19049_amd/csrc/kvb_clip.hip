@@ -9,22 +9,36 @@ namespace kvb_impl {
 
 namespace {
 
-struct BlockOf {
-    int tensor;
+// A part of a block, as scalars
+struct Item {
+    const void *p;
+    void *to;
+    int type, n;    // n = 0: nothing there
     int64_t from;   // its first element
-    int n;          // 0: nothing there
 };
-__device__ __forceinline__ BlockOf block_of(const ListArgs &a, int block)
+__device__ __forceinline__ int of_lane(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
+__device__ __forceinline__ int64_t of_lane(int64_t x, int i)
 {
-    const int lane = threadIdx.x % 64;
-    int before = 0;   // tensors that end at or before this block
-    for (int i0 = 0; i0 < a.n; i0 += 64) {
-        const int i = min(i0 + lane, a.n - 1);
-        before += __popcll(__ballot(i0 + lane < a.n && a.first[i + 1] <= block));
-    }
-    const int i = __builtin_amdgcn_readfirstlane(min(before, a.n - 1));
-    const int64_t from = (int64_t)(block - a.first[i]) * KVB_LIST_BLOCK, left = a.size[i] - from;
-    return BlockOf{i, from, from < 0 || left <= 0 ? 0 : (int)min(left, (int64_t)KVB_LIST_BLOCK)};
+    return (int64_t)((uint64_t)(uint32_t)of_lane((int)(x >> 32), i) << 32 | (uint32_t)of_lane((int)x, i));
+}
+// Lane i asks for all that there is of tensor i, so that up to 64 tensors take one wait, not two.
+__device__ __forceinline__ Item item_of(const ListArgs &a, int unit, int split)
+{
+    const int lane = threadIdx.x % 64, block = unit / split, part = unit - block * split;
+    int i = 0;   // the last tensor that the lane looked at; tensors that end at or before this block
+    int before = 0;
+    for (int i0 = 0; i0 + 64 < a.n; i0 += 64)
+        before += __popcll(__ballot(a.first[i0 + lane + 1] <= block));
+    // (what is left of the last 64, or of those that the block is among)
+    const int base = before / 64 * 64;
+    i = min(base + lane, a.n - 1);
+    const int begin = a.first[i], end = a.first[i + 1], type = a.type[i];
+    const int64_t size = a.size[i], p = reinterpret_cast<int64_t>(a.data[i]), to = reinterpret_cast<int64_t>(a.to ? a.to[i] : nullptr);
+    const int at = min(base + (int)__popcll(__ballot(base + lane < a.n && end <= block)), a.n - 1) - base;
+    const int64_t from = (int64_t)(block - of_lane(begin, at)) * KVB_LIST_BLOCK + part * (KVB_LIST_BLOCK / split), left = of_lane(size, at) - from;
+    const bool there = block >= of_lane(begin, at) && left > 0;
+    return Item{reinterpret_cast<const void *>(of_lane(p, at)), reinterpret_cast<void *>(of_lane(to, at)), of_lane(type, at),
+                there ? (int)min(left, (int64_t)(KVB_LIST_BLOCK / split)) : 0, from};
 }
 
 __device__ __forceinline__ double squares(const float (&x)[8], double sum)
@@ -47,8 +61,21 @@ __device__ __forceinline__ double squares_of(const T *p, int n)
 {
     double sum = 0.0;
     const int ahead = ahead_of(p, n), vectors = (n - ahead) / 8, tail = ahead + 8 * vectors;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < vectors; i += 256) {
+    int i = threadIdx.x;
+    for (; i + 7 * 256 < vectors; i += 8 * 256) {   // (eight loads on their way at once)
+        Raw8<T> raw[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            raw[k] = load_raw8(p + ahead + 8 * (i + k * 256));
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float x[8];
+            unpack8(raw[k], x);
+            sum = squares(x, sum);
+        }
+    }
+#pragma unroll 2
+    for (; i < vectors; i += 256) {
         float x[8];
         unpack8(load_raw8(p + ahead + 8 * i), x);
         sum = squares(x, sum);
@@ -70,43 +97,55 @@ __device__ __forceinline__ double sum_wave(double x)
 }
 
 template <typename T>
+__device__ __forceinline__ void scale8(const Raw8<T> &raw, T *to, float c)
+{
+    float x[8];
+    unpack8(raw, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        x[j] *= c;
+    store8<true>(to, x);
+}
+template <typename T>
 __device__ __forceinline__ void scale_of(const T *p, T *to, int n, float c)
 {
     if (c == 1.0f && p == to)
         return;
     const bool alike = ((reinterpret_cast<uintptr_t>(p) ^ reinterpret_cast<uintptr_t>(to)) & 15) == 0;
     const int ahead = alike ? ahead_of(p, n) : 0, vectors = alike ? (n - ahead) / 8 : 0, tail = ahead + 8 * vectors;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < vectors; i += 256) {
-        float x[8];
-        unpack8(load_raw8(p + ahead + 8 * i), x);
+    int i = threadIdx.x;
+    for (; i + 7 * 256 < vectors; i += 8 * 256) {
+        Raw8<T> raw[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            x[j] *= c;
-        store8(to + ahead + 8 * i, x);
+        for (int k = 0; k < 8; ++k)
+            raw[k] = load_raw8(p + ahead + 8 * (i + k * 256));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            scale8(raw[k], to + ahead + 8 * (i + k * 256), c);
     }
+#pragma unroll 2
+    for (; i < vectors; i += 256)
+        scale8(load_raw8(p + ahead + 8 * i), to + ahead + 8 * i, c);
     if ((int)threadIdx.x < ahead)
         to[threadIdx.x] = from_f32<T>(to_f32(p[threadIdx.x]) * c);
-    for (int i = tail + threadIdx.x; i < n; i += 256)
+    for (i = tail + threadIdx.x; i < n; i += 256)
         to[i] = from_f32<T>(to_f32(p[i]) * c);
 }
 
 }  // namespace
 
-__global__ __launch_bounds__(256) void kvb_squares_kernel(const ListArgs a, double *sums)
+__global__ __launch_bounds__(256) void kvb_squares_kernel(const ListArgs a, int split, double *sums)
 {
     __shared__ double part[4];
-    const BlockOf b = block_of(a, blockIdx.x);
+    const Item b = item_of(a, blockIdx.x, split);
     double sum = 0.0;
     if (b.n > 0) {
-        const int type = a.type[b.tensor];
-        const void *p = a.data[b.tensor];
-        if (type == KVB_F32)
-            sum = squares_of(static_cast<const float *>(p) + b.from, b.n);
-        else if (type == KVB_BF16)
-            sum = squares_of(static_cast<const bf16_t *>(p) + b.from, b.n);
+        if (b.type == KVB_F32)
+            sum = squares_of(static_cast<const float *>(b.p) + b.from, b.n);
+        else if (b.type == KVB_BF16)
+            sum = squares_of(static_cast<const bf16_t *>(b.p) + b.from, b.n);
         else
-            sum = squares_of(static_cast<const f16_t *>(p) + b.from, b.n);
+            sum = squares_of(static_cast<const f16_t *>(b.p) + b.from, b.n);
     }
     sum = sum_wave(sum);
     if (threadIdx.x % 64 == 0)
@@ -134,33 +173,33 @@ __global__ __launch_bounds__(1024) void kvb_root_kernel(const double *sums, int 
     }
 }
 
-__global__ __launch_bounds__(256) void kvb_clip_kernel(const ListArgs a, const float *norm, float largest)
+__global__ __launch_bounds__(256) void kvb_clip_kernel(const ListArgs a, int split, const float *norm, float largest)
 {
-    const BlockOf b = block_of(a, blockIdx.x);
+    const float total = *norm;
+    const Item b = item_of(a, blockIdx.x, split);
     if (b.n <= 0)
         return;
     // (not fminf, which drops a norm that is not a number)
-    const float cut = largest / (*norm + 1e-6f), c = cut > 1.0f ? 1.0f : cut;
-    const int type = a.type[b.tensor];
-    const void *p = a.data[b.tensor];
-    void *to = a.to[b.tensor];
-    if (type == KVB_F32)
-        scale_of(static_cast<const float *>(p) + b.from, static_cast<float *>(to) + b.from, b.n, c);
-    else if (type == KVB_BF16)
-        scale_of(static_cast<const bf16_t *>(p) + b.from, static_cast<bf16_t *>(to) + b.from, b.n, c);
+    const float cut = largest / (total + 1e-6f), c = cut > 1.0f ? 1.0f : cut;
+    if (b.type == KVB_F32)
+        scale_of(static_cast<const float *>(b.p) + b.from, static_cast<float *>(b.to) + b.from, b.n, c);
+    else if (b.type == KVB_BF16)
+        scale_of(static_cast<const bf16_t *>(b.p) + b.from, static_cast<bf16_t *>(b.to) + b.from, b.n, c);
     else
-        scale_of(static_cast<const f16_t *>(p) + b.from, static_cast<f16_t *>(to) + b.from, b.n, c);
+        scale_of(static_cast<const f16_t *>(b.p) + b.from, static_cast<f16_t *>(b.to) + b.from, b.n, c);
 }
 
 void launch_grad_norm(const ListArgs &a, float *norm, double *work, hipStream_t stream)
 {
+    const int split = list_split(a.blocks);
     if (a.blocks > 0)
-        launch_part(kvb_squares_kernel, true, false, a.blocks, 256, stream, a, work);
-    launch_part(kvb_root_kernel, a.blocks == 0, true, 1, 1024, stream, (const double *)work, a.blocks, norm);
+        launch_part(kvb_squares_kernel, true, false, (int64_t)a.blocks * split, 256, stream, a, split, work);
+    launch_part(kvb_root_kernel, a.blocks == 0, true, 1, 1024, stream, (const double *)work, a.blocks * split, norm);
 }
 void launch_clip(const ListArgs &a, const float *norm, float largest, hipStream_t stream)
 {
-    launch_part(kvb_clip_kernel, true, true, a.blocks, 256, stream, a, norm, largest);
+    const int split = list_split(a.blocks);
+    launch_part(kvb_clip_kernel, true, true, (int64_t)a.blocks * split, 256, stream, a, split, norm, largest);
 }
 
 }  // namespace kvb_impl

@@ -79,9 +79,9 @@ __device__ __forceinline__ void gates_of(const ConvArgs &a, int64_t t0, int n, i
 
 }  // namespace
 
-// Whole sequences: a wave takes 2^lg tokens of one of them, with the taps' inputs in registers.
-template <typename T, int W>
-__global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int units, int lg)
+// Whole sequences: a wave takes up to `most` tokens of one of them, with the taps' inputs in registers.
+template <typename T, int W, bool STREAM>
+__global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int units, int most)
 {
     constexpr int U = 4;   // tokens at a time
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
     if (unit >= units)
         return;
     const int w = unit / each, group = unit - w * each;
-    const Piece p = piece_at(a.start, a.n_tokens, a.B, w, lg);
+    const Piece p = piece_at(a.start, a.n_tokens, a.B, w, most);
     const int row = state_row(a.slot, a.n_slots, p.b);
     if (!p.some || row < 0)
         return;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
         auto request = [&](int t) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                raw[u] = load_raw8(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
+                raw[u] = load_raw8_if<STREAM>(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
         };
         request(p.t0);
         const Lane8<T, W> l(a, ch);
@@ -228,6 +228,69 @@ __global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, i
     }
 }
 
+// The same, a wave all drafts of a request: every row is read once and handed from draft to draft in LDS, where a lane finds nothing but its own channels.
+template <typename T, int W>
+__global__ __launch_bounds__(64) void kvb_conv_drafts_kernel(const ConvArgs a)
+{
+    __shared__ Raw8<T> rows[W - 1 + KVB_MAX_DRAFTS][64];
+    const int lane = threadIdx.x, groups = conv_groups(a.C), each = groups + a.gates, b = blockIdx.x / each, group = blockIdx.x - b * each;
+    const int row = state_row(a.slot, a.n_slots, b);
+    if (row < 0)
+        return;
+    if (group == groups) {
+        gates_of<T>(a, (int64_t)b * a.T, a.T, lane);
+        return;
+    }
+    int up = lane - 1;   // lane i: draft i's parent
+    if (a.parent) {
+        const int i = min(lane, a.T - 1), p = a.parent[(int64_t)b * a.T + i];
+        up = p < -1 || p >= i ? -1 : p;
+    }
+    const int own_ch = group * CONV_LANES + lane * 8, ch = own_ch < a.C ? own_ch : 0;
+    const T *x = static_cast<const T *>(a.x) + (int64_t)b * a.T * a.x_stride + ch;
+    Raw8<T> state[W - 1] = {}, raw[KVB_MAX_DRAFTS];
+    if (a.state0) {
+        const T *s0 = static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch;
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            state[i] = load_raw8(s0 + (int64_t)i * a.C);
+    }
+#pragma unroll
+    for (int i = 0; i < KVB_MAX_DRAFTS; ++i)
+        if (i < a.T)
+            raw[i] = load_raw8(x + (int64_t)i * a.x_stride);
+    const Lane8<T, W> l(a, ch);
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i)
+        rows[i][lane] = state[i];
+#pragma unroll
+    for (int i = 0; i < KVB_MAX_DRAFTS; ++i)
+        if (i < a.T)
+            rows[W - 1 + i][lane] = raw[i];
+    for (int i = 0; i < a.T; ++i) {
+        float z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] = l.bias[j];
+        int place[W];   // a draft, or row W - 1 + place of the state
+        place[W - 1] = i;
+#pragma unroll
+        for (int k = W - 2; k >= 0; --k)
+            place[k] = place[k + 1] >= 0 ? __builtin_amdgcn_readlane(up, place[k + 1]) : place[k + 1] - 1;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            float e[8];
+            unpack8(rows[W - 1 + place[k]][lane], e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                z[j] = fmaf(l.w[k][j], e[j], z[j]);
+        }
+        l.finish(z);
+        if (own_ch < a.C)
+            store8(l.to + ((int64_t)b * a.T + i) * l.to_stride, z);
+    }
+}
+
 // The state behind the accepted drafts: the last W - 1 rows of the state and theirs.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void kvb_conv_commit_kernel(const ConvArgs a, int units)
@@ -292,20 +355,28 @@ void with_taps(int dtype, int width, F &&f)
     });
 }
 
-int conv_lg(int64_t n_tokens, int groups) { return n_tokens * groups >= 1 << 16 ? 5 : 3; }
-
 }  // namespace
 
 void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 {
-    const int groups = conv_groups(a.C), lg = conv_lg(a.n_tokens, groups);
-    const int units = (int)(pieces_of(a.n_tokens, a.B, lg) * (groups + a.gates));
-    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units, lg); });
+    const int each = conv_groups(a.C) + a.gates, most = conv_most(a.n_tokens, a.B, each), units = (int)(pieces_of(a.n_tokens, a.B, most) * each);
+    // x past the caches where it and what is made from it fill half of the last level: what reads the results next finds more of them there
+    const bool stream_x = (int64_t)a.n_tokens * a.C * (dtype == KVB_F32 ? 4 : 2) > 64 << 20;
+    with_taps(dtype, width, [&]<typename T, int W>() {
+        if (stream_x)
+            launch_part(kvb_conv_kernel<T, W, true>, true, true, (units + 3) / 4, 256, stream, a, units, most);
+        else
+            launch_part(kvb_conv_kernel<T, W, false>, true, true, (units + 3) / 4, 256, stream, a, units, most);
+    });
 }
 
 void launch_conv_tokens(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 {
-    const int units = a.B * a.T * (conv_groups(a.C) + a.gates);
+    const int each = conv_groups(a.C) + a.gates, units = a.B * a.T * each;
+    if (a.T > 1 && units >= 8192) {
+        with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_drafts_kernel<T, W>, true, true, a.B * each, 64, stream, a); });
+        return;
+    }
     with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_token_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units); });
 }
 

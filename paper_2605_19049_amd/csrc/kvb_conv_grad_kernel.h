@@ -33,15 +33,15 @@ __device__ __forceinline__ void gate_grads(const ConvGradArgs &g, int64_t t0, in
     }
 }
 
-template <typename T, int W>
-__global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g, int lg)
+template <typename T, int W, bool BIAS>
+__global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g, int most)
 {
-    constexpr int AHEAD = sizeof(T) == 2 ? 4 : 2;   // tokens asked for ahead
+    constexpr int AHEAD = 2;   // tokens asked for ahead
     constexpr int PLANE = CONV_LANES;
-    __shared__ float sums[4][(W + 1) * PLANE];
+    __shared__ float sums[4][(W + BIAS) * PLANE];
     const ConvArgs &a = g.f;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
-    const int each = groups + a.gates, part = blockIdx.x / each, group = blockIdx.x - part * each;
+    const int group = blockIdx.x / g.parts, part = blockIdx.x - group * g.parts;
     float *to = g.part + (int64_t)part * g.columns;
 
     if (group == groups) {
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
             const int h = h0 + l.head;
             float dA = 0.0f, ddt = 0.0f;
             for (int i = 0; i < g.each; ++i) {
-                const Piece p = piece_at(a.start, a.n_tokens, a.B, (part * 4 + wave) * g.each + i, lg);
+                const Piece p = piece_at(a.start, a.n_tokens, a.B, (part * 4 + wave) * g.each + i, most);
                 if (p.t0 < p.t1 && state_row(a.slot, a.n_slots, p.b) >= 0 && h < a.Hv)
                     gate_grads<T>(g, (int64_t)p.first + p.t0, p.t1 - p.t0, h, l, dA, ddt);
             }
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
                     for (int t = 0; t < l.tokens; ++t)
                         s += sums[v][64 * which + t * l.heads + head];
                 if (h0 + head < a.Hv)
-                    to[(int64_t)(W + (a.bias != nullptr)) * a.C + which * a.Hv + h0 + head] = s;
+                    to[(int64_t)(W + BIAS) * a.C + which * a.Hv + h0 + head] = s;
             }
             __syncthreads();
         }
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
     const int own_ch = group * CONV_LANES + lane * 8;
     const bool active = own_ch < a.C;
     const int ch = active ? own_ch : 0, nq = a.Hk * a.d, lgh = a.d == 128 ? 4 : a.d == 64 ? 3 : 2;
-    float w[W][8], bias[8], dw[W][8] = {}, dbias[8] = {};
+    float w[W][8], bias[8] = {}, dw[W][8] = {}, dbias[8] = {};
     {
         const T *wp = static_cast<const T *>(a.weight) + (int64_t)ch * W;
 #pragma unroll
@@ -85,17 +85,15 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
             for (int j = 0; j < 8; ++j)
                 w[(8 * i + j) % W][(8 * i + j) / W] = y[j];
         }
-        Raw8<T> rb{};
-        if (a.bias)
-            rb = load_raw8(static_cast<const T *>(a.bias) + ch);
-        unpack8(rb, bias);
+        if constexpr (BIAS)
+            unpack8(load_raw8(static_cast<const T *>(a.bias) + ch), bias);
     }
-    const bool unit = a.unit && ch < 2 * nq;
+    const bool unit = a.unit && ch < 2 * nq, any_unit = a.unit && group * CONV_LANES < 2 * nq;   // of the lane; of some lane of the wave
     const T *dn_first = ch < nq ? static_cast<const T *>(g.dq) + ch : ch < 2 * nq ? static_cast<const T *>(g.dk) + (ch - nq) : static_cast<const T *>(g.dv) + (ch - 2 * nq);
     const int64_t dn_stride = ch < nq ? a.q_stride : ch < 2 * nq ? a.k_stride : a.v_stride;
 
     for (int n = 0; n < g.each; ++n) {
-        const Piece p = piece_at(a.start, a.n_tokens, a.B, (part * 4 + wave) * g.each + n, lg);
+        const Piece p = piece_at(a.start, a.n_tokens, a.B, (part * 4 + wave) * g.each + n, most);
         const int row = state_row(a.slot, a.n_slots, p.b);
         if (!p.some || row < 0 || !active)
             continue;
@@ -147,21 +145,28 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
                             z[j] = fmaf(w[i][j], e[(u + 4 - (W - 1) + i) % 4][j], z[j]);
                         s[j] = sigmoid(z[j]);
                         z[j] *= s[j];   // y
-                        sq = fmaf(z[j], z[j], sq);
-                        dot = fmaf(z[j], d[j], dot);
                     }
-                    sq = sum_to16(sq, lgh);
-                    dot = sum_to16(dot, lgh);
-                    const float r = unit ? __builtin_amdgcn_rsqf(sq + a.eps) : 1.0f, c = unit ? r * r * r * dot : 0.0f;
+                    if (any_unit) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float dy = fmaf(r, d[j], -c * z[j]);
-                        dz[u][j] = dy * fmaf(z[j], 1.0f - s[j], s[j]);
+                        for (int j = 0; j < 8; ++j) {
+                            sq = fmaf(z[j], z[j], sq);
+                            dot = fmaf(z[j], d[j], dot);
+                        }
+                        sq = sum_to16(sq, lgh);
+                        dot = sum_to16(dot, lgh);
+                        const float r = unit ? __builtin_amdgcn_rsqf(sq + a.eps) : 1.0f, c = unit ? r * r * r * dot : 0.0f;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            d[j] = fmaf(r, d[j], -c * z[j]);   // dy
                     }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        dz[u][j] = d[j] * fmaf(z[j], 1.0f - s[j], s[j]);
                     if (t < p.t1)
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
-                            dbias[j] += dz[u][j];
+                            if constexpr (BIAS)
+                                dbias[j] += dz[u][j];
 #pragma unroll
                             for (int i = 0; i < W; ++i)
                                 dw[i][j] = fmaf(dz[u][j], e[(u + 4 - (W - 1) + i) % 4][j], dw[i][j]);
@@ -200,12 +205,13 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             sums[wave][i * PLANE + lane * 8 + j] = dw[i][j];
+    if constexpr (BIAS)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        sums[wave][W * PLANE + lane * 8 + j] = dbias[j];
+        for (int j = 0; j < 8; ++j)
+            sums[wave][W * PLANE + lane * 8 + j] = dbias[j];
     __syncthreads();
-    const int planes = W + (a.bias != nullptr), first = group * CONV_LANES;
-    for (int i = threadIdx.x; i < planes * PLANE; i += 256) {
+    const int first = group * CONV_LANES;
+    for (int i = threadIdx.x; i < (W + BIAS) * PLANE; i += 256) {
         const int plane = i / PLANE, c = first + i % PLANE;
         if (c < a.C)   // (weights lie channel by channel)
             to[plane < W ? (int64_t)c * W + plane : (int64_t)W * a.C + c] = sums[0][i] + sums[1][i] + sums[2][i] + sums[3][i];
@@ -213,10 +219,15 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
 }
 
 template <typename T>
-void launch_conv_grad_typed(int width, const ConvGradArgs &g, int lg, float *dweight, float *dbias, float *dA_log, float *ddt_bias, hipStream_t stream)
+void launch_conv_grad_typed(int width, const ConvGradArgs &g, int most, float *dweight, float *dbias, float *dA_log, float *ddt_bias, hipStream_t stream)
 {
     const int64_t blocks = (int64_t)g.parts * (conv_groups(g.f.C) + g.f.gates);
-    auto go = [&]<int W>() { launch_part(kvb_conv_grad_kernel<T, W>, true, false, blocks, 256, stream, g, lg); };
+    auto go = [&]<int W>() {
+        if (g.f.bias)
+            launch_part(kvb_conv_grad_kernel<T, W, true>, true, false, blocks, 256, stream, g, most);
+        else
+            launch_part(kvb_conv_grad_kernel<T, W, false>, true, false, blocks, 256, stream, g, most);
+    };
     if (g.parts == 0) {
     } else if (width == 4)
         go.template operator()<4>();

@@ -104,33 +104,57 @@ __device__ __forceinline__ Raw8<T> pack8(const float (&x)[8])
     else
         return Raw8<T>{make_uint4(pack_pair<T>(x[0], x[1]), pack_pair<T>(x[2], x[3]), pack_pair<T>(x[4], x[5]), pack_pair<T>(x[6], x[7]))};
 }
+// 8 elements that are not read again: past the caches
+__device__ __forceinline__ Raw8<float> load_raw8_nt(const float *p)
+{
+    typedef float v4 __attribute__((ext_vector_type(4)));
+    const v4 a = __builtin_nontemporal_load(reinterpret_cast<const v4 *>(p)), b = __builtin_nontemporal_load(reinterpret_cast<const v4 *>(p + 4));
+    return Raw8<float>{make_float4(a.x, a.y, a.z, a.w), make_float4(b.x, b.y, b.z, b.w)};
+}
 template <typename T>
-__device__ __forceinline__ void store8(T *p, const float (&x)[8]) { store_raw8<false, true>(p, pack8<T>(x)); }
+__device__ __forceinline__ Raw8<T> load_raw8_nt(const T *p)
+{
+    typedef uint32_t v4 __attribute__((ext_vector_type(4)));
+    const v4 a = __builtin_nontemporal_load(reinterpret_cast<const v4 *>(p));
+    return Raw8<T>{make_uint4(a.x, a.y, a.z, a.w)};
+}
 
-// A stretch of 2^lg tokens of a ragged batch, numbered as the chunks of a scan are: those of sequence b start at start[b] / 2^lg + b, so that
+template <bool STREAM, typename T>
+__device__ __forceinline__ Raw8<T> load_raw8_if(const T *p)
+{
+    if constexpr (STREAM)
+        return load_raw8_nt(p);
+    else
+        return load_raw8(p);
+}
+// STREAM: past the caches.  (Not put's stores through the L2: conv_long_prompt's 63 us became 67, norm_grad_gated's 98 137.)
+template <bool STREAM = false, typename T>
+__device__ __forceinline__ void store8(T *p, const float (&x)[8]) { store_raw8<STREAM, !STREAM>(p, pack8<T>(x)); }
+
+// A stretch of up to `most` tokens of a ragged batch, numbered as the chunks of a scan are: those of sequence b start at start[b] / most + b, so that
 // every sequence has one, an empty one too.
 struct Piece {
     int b, first, len;   // the sequence, its first token, its length
     int t0, t1;          // the tokens of the piece, counted from there; t0 = t1 in an empty sequence's only one
     bool some;           // false: there is no piece with this number
 };
-inline int64_t pieces_of(int64_t n_tokens, int64_t B, int lg) { return (n_tokens >> lg) + B; }
-__device__ __forceinline__ Piece piece_at(const int32_t *start, int n_tokens, int B, int w, int lg)   // every lane of the wave calls it
+inline int64_t pieces_of(int64_t n_tokens, int64_t B, int most) { return n_tokens / most + B; }
+__device__ __forceinline__ Piece piece_at(const int32_t *start, int n_tokens, int B, int w, int most)   // every lane of the wave calls it
 {
     const int lane = threadIdx.x % 64;
     int before = 0;   // sequences that start at or before w
     for (int b0 = 0; b0 < B; b0 += 64) {
         const int b = min(b0 + lane, B - 1);
-        const bool yes = b0 + lane < B && (min(max(start[b], 0), n_tokens) >> lg) + b <= w;
+        const bool yes = b0 + lane < B && (int)((uint32_t)min(max(start[b], 0), n_tokens) / (uint32_t)most) + b <= w;
         before += __popcll(__ballot(yes));
     }
     const int b = __builtin_amdgcn_readfirstlane(max(before - 1, 0));
     const Span s = span_of(start, n_tokens, b);
-    const int c = w - ((s.first >> lg) + b);
-    const int64_t at = (int64_t)c << lg;
+    const int c = w - ((int)((uint32_t)s.first / (uint32_t)most) + b);
+    const int64_t at = (int64_t)c * most;
     if (c < 0 || (c > 0 && at >= s.len))
         return Piece{b, s.first, s.len, 0, 0, false};
-    return Piece{b, s.first, s.len, (int)at, min(s.len, (int)at + (1 << lg)), true};
+    return Piece{b, s.first, s.len, (int)at, (int)min((int64_t)s.len, at + most), true};
 }
 
 // The gates of some tokens and heads, dealt over a wave: lane -> (token, head), heads in the next power of two of lanes.
@@ -165,7 +189,7 @@ void launch_conv(int in_dtype, int width, const ConvArgs &a, hipStream_t stream)
 void launch_conv_tokens(int in_dtype, int width, const ConvArgs &a, hipStream_t stream);
 void launch_conv_commit(int in_dtype, int width, const ConvArgs &a, hipStream_t stream);
 template <typename T>
-void launch_conv_grad_typed(int width, const ConvGradArgs &a, int lg, float *dweight, float *dbias, float *dA_log, float *ddt_bias,
+void launch_conv_grad_typed(int width, const ConvGradArgs &a, int most, float *dweight, float *dbias, float *dA_log, float *ddt_bias,
                             hipStream_t stream);                                            // kvb_conv_grad_*.hip
 template <typename TX, typename T>
 void launch_norm_typed(const NormArgs &a, hipStream_t stream);                              // kvb_norm.hip
@@ -174,41 +198,58 @@ void launch_norm_grad_typed(const NormGradArgs &a, float *dweight, hipStream_t s
 void launch_grad_norm(const ListArgs &a, float *norm, double *work, hipStream_t stream);    // kvb_clip.hip
 void launch_clip(const ListArgs &a, const float *norm, float largest, hipStream_t stream);
 
-// Chunks of the gradients of the convolution, 2^lg tokens each, and how many a wave takes: a workgroup's four waves leave one part, at most
-// CONV_PARTS of them.
-constexpr int CONV_PARTS = 256;
-constexpr int CONV_LEAST_LG = 3;   // (more than the taps reach back)
+// Pieces of the convolution, and for its gradients how many a wave takes: a workgroup's four waves leave one part.
+constexpr int CONV_LEAST = 8;   // tokens of a piece (more than the taps reach back)
 struct ConvParts {
-    int lg, parts, each;
+    int most, parts, each;
 };
-inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int)
+inline int conv_clamp(int64_t most, int64_t up) { return (int)(most < CONV_LEAST ? CONV_LEAST : most < up ? most : up); }
+constexpr int CONV_WG = 1536;
+inline int conv_most(int64_t n_tokens, int64_t B, int units)   // units: of a piece
 {
-    const int lg = 5;
-    const int64_t pieces = pieces_of(n_tokens, B, lg), each = (pieces + 4 * CONV_PARTS - 1) / (4 * CONV_PARTS);
-    const int64_t e = each < 1 ? 1 : each;
-    return ConvParts{lg, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};
+    int64_t pieces = CONV_WG * 4 / units - B;
+    if (pieces < CONV_WG * 2 / units)
+        pieces = CONV_WG * 2 / units;
+    return conv_clamp((n_tokens + pieces - 1) / (pieces < 1 ? 1 : pieces), 64);
 }
-
+constexpr int CONV_GRAD_WG = 512;
+inline int64_t conv_part_limit(int units) { return CONV_GRAD_WG / units < 1 ? 1 : CONV_GRAD_WG / units; }
+inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units)
+{
+    const int64_t limit = conv_part_limit(units), want = B < 2 * limit ? 4 * limit - B : 2 * limit;
+    const int most = conv_clamp((n_tokens + want - 1) / want, INT32_MAX);
+    const int64_t pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
+    return ConvParts{most, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};
+}
 // The most that a call of up to so many tokens and sequences needs
-inline int64_t conv_most_parts(int64_t n_tokens, int64_t B)
+inline int64_t conv_most_parts(int64_t n_tokens, int64_t B, int units)
 {
-    const int64_t n = (pieces_of(n_tokens, B, CONV_LEAST_LG) + 3) / 4;
-    return n < 1 ? 1 : n < CONV_PARTS ? n : CONV_PARTS;
+    const int64_t n = (pieces_of(n_tokens, B, CONV_LEAST) + 3) / 4, limit = conv_part_limit(units);
+    return n < 1 ? 1 : n < limit ? n : limit;
 }
 
-// Workgroups of kvb_norm_backward, each of which leaves one part.
-constexpr int NORM_PARTS = 1024;
+// Workgroups of a block of a list: several where the blocks alone do not fill the card
+constexpr int LIST_SPLIT = 4;
+inline int list_split(int blocks) { return blocks < 512 ? LIST_SPLIT : 1; }
+static_assert(KVB_LIST_BLOCK % (LIST_SPLIT * 8) == 0);
+
+// kvb_norm_backward, rows above 512 elements: vectors of 8 that a lane has of a row, threads of a row, rows of a workgroup at once
+inline int norm_vectors(int width) { return width <= 4096 ? 1 : width <= 8192 ? 2 : 4; }
+inline int norm_threads(int width) { return ((width / 8 + norm_vectors(width) - 1) / norm_vectors(width) + 63) / 64 * 64; }
+inline int norm_teams(int width) { return 512 / norm_threads(width); }
+// Its workgroups, each of which leaves one part
 inline int norm_parts(int64_t rows, int width)
 {
-    int64_t rows_of_workgroup = 1;   // at once
-    if (width <= 2048) {
+    int64_t at_once = norm_teams(width), most = 512;
+    if (width <= 512) {
         int lanes = 4;
         while (lanes < 64 && lanes * 8 < width)
             lanes *= 2;
-        rows_of_workgroup = 256 / lanes;
+        at_once = 256 / lanes;
+        most = 1024;
     }
-    const int64_t n = (rows + rows_of_workgroup - 1) / rows_of_workgroup;
-    return (int)(n < NORM_PARTS ? n : NORM_PARTS);
+    const int64_t n = (rows + at_once - 1) / at_once;
+    return (int)(n < most ? n : most);
 }
 inline int64_t norm_most_parts(int64_t rows, int width) { return norm_parts(rows, width); }
 

@@ -9,33 +9,52 @@ namespace kvb_impl {
 
 namespace {
 
+// What a row has of 8 columns, as it lies in memory
+template <typename TX, typename T>
+struct GradRaw {
+    Raw8<TX> x, dsum;
+    Raw8<T> dout, gate;
+};
 template <typename TX, typename T>
 struct Grad8 {
-    float s[8], dh[8];   // dh: dout c, times the weight where it says so
-    Raw8<T> dout, gate;
-    Raw8<TX> dsum;
+    float s[8], dh[8];   // dh: dout c
 };
 
-// EARLY: dsum too is asked for with the others (where the lane has the registers)
-template <bool EARLY, typename TX, typename T>
-__device__ __forceinline__ void load_grad(const NormGradArgs &g, int64_t token, int64_t row, int64_t in_token, int at, Grad8<TX, T> &p)
+template <typename TX, typename T>
+__device__ __forceinline__ void request(const NormGradArgs &g, int64_t token, int64_t row, int64_t in_token, int at, GradRaw<TX, T> &p)
 {
     const NormArgs &a = g.f;
-    const Raw8<TX> x = load_raw8(static_cast<const TX *>(a.x) + token * a.x_stride + in_token + at);
+    p.x = load_raw8(static_cast<const TX *>(a.x) + token * a.x_stride + in_token + at);
     p.dout = load_raw8(static_cast<const T *>(g.dout) + row * a.width + at);
     if (a.gate)
         p.gate = load_raw8(static_cast<const T *>(a.gate) + token * a.gate_stride + in_token + at);
-    if (EARLY && g.dsum)
+    if (g.dsum)
         p.dsum = load_raw8(static_cast<const TX *>(g.dsum) + row * a.width + at);
-    unpack8(x, p.s);
-    unpack8(p.dout, p.dh);
-    if (a.gate) {
+}
+template <typename TX, typename T>
+__device__ __forceinline__ void take(const NormGradArgs &g, const GradRaw<TX, T> &r, Grad8<TX, T> &p)
+{
+    unpack8(r.x, p.s);
+    unpack8(r.dout, p.dh);
+    if (g.f.gate) {
         float z[8];
-        unpack8(p.gate, z);
+        unpack8(r.gate, z);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             p.dh[j] *= z[j] * sigmoid(z[j]);
     }
+}
+// The same bits, anew: what is worked out from them is worked out again, and takes no register until then
+template <typename V>
+__device__ __forceinline__ void renew(V &x)
+{
+    static_assert(sizeof(V) % 16 == 0);
+    typedef uint32_t v4 __attribute__((ext_vector_type(4)));
+    struct Words { v4 w[sizeof(V) / 16]; } words = __builtin_bit_cast(Words, x);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(V) / 16); ++i)
+        asm volatile("" : "+v"(words.w[i]));
+    x = __builtin_bit_cast(V, words);
 }
 // sums of s^2 and dh weight s
 template <typename TX, typename T>
@@ -47,9 +66,9 @@ __device__ __forceinline__ void sums_of(const Grad8<TX, T> &p, const float (&w)[
         dot = fmaf(p.dh[j] * w[j], p.s[j], dot);
     }
 }
-template <bool EARLY, typename TX, typename T>
-__device__ __forceinline__ void finish_grad(const NormGradArgs &g, int64_t token, int64_t row, int64_t in_token, int at, const Grad8<TX, T> &p, const float (&w)[8],
-                                            float (&dw)[8], float r, float mean)
+template <typename TX, typename T>
+__device__ __forceinline__ void finish_grad(const NormGradArgs &g, int64_t token, int64_t row, int64_t in_token, int at, const GradRaw<TX, T> &raw,
+                                            const Grad8<TX, T> &p, const float (&w)[8], float (&dw)[8], float r, float mean)
 {
     const NormArgs &a = g.f;
     float ds[8], y[8];
@@ -61,8 +80,8 @@ __device__ __forceinline__ void finish_grad(const NormGradArgs &g, int64_t token
     }
     if (a.gate) {
         float z[8], d[8];
-        unpack8(p.gate, z);
-        unpack8(p.dout, d);
+        unpack8(raw.gate, z);
+        unpack8(raw.dout, d);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float t = sigmoid(z[j]);
@@ -71,7 +90,7 @@ __device__ __forceinline__ void finish_grad(const NormGradArgs &g, int64_t token
         store8(static_cast<T *>(g.dgate) + token * a.gate_stride + in_token + at, y);
     }
     if (g.dsum) {
-        unpack8(EARLY ? p.dsum : load_raw8(static_cast<const TX *>(g.dsum) + row * a.width + at), y);
+        unpack8(raw.dsum, y);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             ds[j] += y[j];
@@ -86,128 +105,176 @@ __device__ __forceinline__ void finish_grad(const NormGradArgs &g, int64_t token
 
 }  // namespace
 
-template <typename TX, typename T, int NV>
+// Rows of up to 512 elements: 2^lg lanes a row
+template <typename TX, typename T>
 __global__ __launch_bounds__(256) void kvb_norm_grad_kernel(const NormGradArgs g, int lg)
 {
-    __shared__ float sums[4][64 * 8 * NV];
+    __shared__ float sums[4][64 * 8];
     const NormArgs &a = g.f;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, lanes = 1 << lg, own = lane & (lanes - 1);
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, lanes = 1 << lg, own = lane & (lanes - 1), at = 8 * own;
     const int64_t step = (int64_t)gridDim.x * 256 >> lg;
-    float w[NV][8], dw[NV][8] = {};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = 8 * (own + i * lanes);
-        unpack8(load_raw8(static_cast<const T *>(a.weight) + (at < a.width ? at : 0)), w[i]);
-    }
+    const float n = 1.0f / (float)a.width;
+    float w[8], dw[8] = {};
+    unpack8(load_raw8(static_cast<const T *>(a.weight) + (at < a.width ? at : 0)), w);
+    // (all lanes go round as often: sums go over all lanes of a row)
     for (int64_t first = (int64_t)blockIdx.x * 256 >> lg; first < a.rows; first += step) {
         const int64_t row = first + (threadIdx.x >> lg), token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
-        Grad8<TX, T> p[NV];
+        const bool there = row < a.rows && at < a.width;
+        GradRaw<TX, T> raw;
+        Grad8<TX, T> p;
         float sq = 0.0f, dot = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = 8 * (own + i * lanes);
-            if (row < a.rows && at < a.width) {
-                load_grad<(NV < 4)>(g, token, row, in_token, at, p[i]);
-                sums_of(p[i], w[i], sq, dot);
-            }
+        if (there) {
+            request(g, token, row, in_token, at, raw);
+            take(g, raw, p);
+            sums_of(p, w, sq, dot);
         }
-        const float n = 1.0f / (float)a.width, r = __builtin_amdgcn_rsqf(sum_lanes(sq, lg) * n + a.eps), mean = sum_lanes(dot, lg) * r * n;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = 8 * (own + i * lanes);
-            if (row < a.rows && at < a.width)
-                finish_grad<(NV < 4)>(g, token, row, in_token, at, p[i], w[i], dw[i], r, mean);
-        }
+        const float r = __builtin_amdgcn_rsqf(sum_lanes(sq, lg) * n + a.eps), mean = sum_lanes(dot, lg) * r * n;
+        if (there)
+            finish_grad(g, token, row, in_token, at, raw, p, w, dw, r, mean);
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            sums[wave][(i * 64 + lane) * 8 + j] = dw[i][j];
+    for (int j = 0; j < 8; ++j)
+        sums[wave][lane * 8 + j] = dw[j];
     __syncthreads();
-    for (int c = threadIdx.x; c < a.width; c += 256) {   // column c: vector c / 8, of lane (c / 8) % lanes of each row's
-        const int i = c / 8 / lanes, l = c / 8 % lanes;
+    for (int c = threadIdx.x; c < a.width; c += 256) {   // (column c: lane c / 8 of each row's)
         float s = 0.0f;
         for (int v = 0; v < 4; ++v)
-            for (int k = l; k < 64; k += lanes)
-                s += sums[v][(i * 64 + k) * 8 + c % 8];
+            for (int l = 0; l < 64; l += lanes)
+                s += sums[v][l * 8 + c];
         g.part[(int64_t)blockIdx.x * a.width + c] = s;
     }
 }
 
-template <typename TX, typename T, int NV, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void kvb_norm_grad_row_kernel(const NormGradArgs g)
+// Longer rows: a row the waves that its vectors need with NV a lane (up to eight of 64 lanes), as many rows side by side as eight waves have.  The next
+// rows are asked for ahead; with four vectors a lane has no registers for that, nor for the weights, and works out what it needs twice.
+template <typename TX, typename T, int NV>
+__global__ __launch_bounds__(512) void kvb_norm_grad_row_kernel(const NormGradArgs g, int threads)
 {
-    __shared__ float part[2][2 * WAVES];
+    __shared__ float part[2][16], sums[NV == 1 ? 512 * 8 : 1];
     const NormArgs &a = g.f;
-    const int wave = threadIdx.x / 64;
+    const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / threads), teams = blockDim.x / threads, own = threadIdx.x - team * threads;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = threads / 64;
     float w[NV][8], dw[NV][8] = {};
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int at = 8 * (threadIdx.x + i * 64 * WAVES);
-        unpack8(load_raw8(static_cast<const T *>(a.weight) + (at < a.width ? at : 0)), w[i]);
-    }
-    int turn = 0;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-        const int64_t token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
-        Grad8<TX, T> p[NV];
-        float sq = 0.0f, dot = 0.0f;
+    auto load_weight = [&] {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at = 8 * (threadIdx.x + i * 64 * WAVES);
-            if (at < a.width) {
-                load_grad<(NV < 4)>(g, token, row, in_token, at, p[i]);
-                sums_of(p[i], w[i], sq, dot);
-            }
+            const int at = 8 * (own + i * threads);
+            unpack8(load_raw8(static_cast<const T *>(a.weight) + (at < a.width ? at : 0)), w[i]);
         }
+    };
+    if (NV < 4)
+        load_weight();
+    GradRaw<TX, T> raw[NV], next[NV];
+    auto ask = [&](int64_t row, GradRaw<TX, T> (&r)[NV]) {
+        const int64_t token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at = 8 * (own + i * threads);
+            if (at < a.width)
+                request(g, token, row, in_token, at, r[i]);
+        }
+    };
+    const int64_t first = (int64_t)blockIdx.x * teams, step = (int64_t)gridDim.x * teams;
+    if (NV < 4 && first + team < a.rows)
+        ask(first + team, next);
+    int turn = 0;
+    for (int64_t at_once = first; at_once < a.rows; at_once += step, turn ^= 1) {   // (the same for all waves)
+        const int64_t row = at_once + team, token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+        Grad8<TX, T> p[NV];
+        float sq = 0.0f, dot = 0.0f;
+        if (NV < 4) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                raw[i] = next[i];
+            if (row + step < a.rows)
+                ask(row + step, next);
+        } else {
+            ask(row, raw);
+            load_weight();
+        }
+        if (row < a.rows)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (8 * (own + i * threads) < a.width) {
+                    take(g, raw[i], p[i]);
+                    sums_of(p[i], w[i], sq, dot);
+                }
         sq = sum_lanes(sq, 6);
         dot = sum_lanes(dot, 6);
         if (threadIdx.x % 64 == 0) {   // (two sets in turn: a barrier a row)
             part[turn][wave] = sq;
-            part[turn][WAVES + wave] = dot;
+            part[turn][8 + wave] = dot;
         }
-        __syncthreads();
-        const float *q = part[turn], n = 1.0f / (float)a.width;
-        sq = q[0];
-        dot = q[WAVES];
+        lds_barrier();
+        if (row < a.rows) {
+            const float *q = part[turn] + team * waves, n = 1.0f / (float)a.width;
+            sq = q[0];
+            dot = q[8];
+            for (int v = 1; v < waves; ++v) {
+                sq += q[v];
+                dot += q[8 + v];
+            }
+            const float r = __builtin_amdgcn_rsqf(sq * n + a.eps), mean = dot * r * n;
 #pragma unroll
-        for (int v = 1; v < WAVES; ++v) {
-            sq += q[v];
-            dot += q[WAVES + v];
+            for (int i = 0; i < NV; ++i) {
+                const int at = 8 * (own + i * threads);
+                if (at < a.width) {
+                    if (NV == 4) {
+                        renew(raw[i].x);
+                        renew(raw[i].dout);
+                        if (a.gate)
+                            renew(raw[i].gate);
+                        take(g, raw[i], p[i]);
+                    }
+                    finish_grad(g, token, row, in_token, at, raw[i], p[i], w[i], dw[i], r, mean);
+                }
+            }
         }
-        const float r = __builtin_amdgcn_rsqf(sq * n + a.eps), mean = dot * r * n;
+    }
+    float *to = g.part + (int64_t)blockIdx.x * a.width;
+    if constexpr (NV == 1) {   // rows side by side
+        if (teams > 1) {
+            if (team > 0)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int at = 8 * (threadIdx.x + i * 64 * WAVES);
-            if (at < a.width)
-                finish_grad<(NV < 4)>(g, token, row, in_token, at, p[i], w[i], dw[i], r, mean);
+                for (int j = 0; j < 8; ++j)
+                    sums[(j * 512) + threadIdx.x] = dw[0][j];
+            __syncthreads();
+            if (team > 0)
+                return;
+            for (int v = 1; v < teams; ++v)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    dw[0][j] += sums[j * 512 + v * threads + threadIdx.x];
         }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int at = 8 * (threadIdx.x + i * 64 * WAVES);
+        const int at = 8 * (own + i * threads);
         if (at < a.width)
-            store8(g.part + (int64_t)blockIdx.x * a.width + at, dw[i]);
+            store8(to + at, dw[i]);
     }
 }
 
-// 64 columns a workgroup; wave v has the rows v, v + 16, ..
+// COLUMNS columns a workgroup of 1024; its rows of threads have the parts in turn
+template <int COLUMNS>
 __global__ __launch_bounds__(1024) void kvb_sums_kernel(const float *part, int parts, int64_t columns, const SumsTo to)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    constexpr int TURNS = 1024 / COLUMNS;
+    __shared__ float sums[TURNS][COLUMNS];
+    const int own = threadIdx.x % COLUMNS, turn = threadIdx.x / COLUMNS;
+    const int64_t c = (int64_t)blockIdx.x * COLUMNS + own;
     float s = 0.0f;
     if (c < columns)
 #pragma unroll 16
-        for (int p = wave; p < parts; p += 16)
+        for (int p = turn; p < parts; p += TURNS)
             s += part[p * columns + c];
-    sums[wave][lane] = s;
+    sums[turn][own] = s;
     __syncthreads();
-    if (wave != 0 || c >= columns)
+    if (turn != 0 || c >= columns)
         return;
-    for (int v = 1; v < 16; ++v)
-        s += sums[v][lane];
+#pragma unroll
+    for (int v = 1; v < TURNS; ++v)
+        s += sums[v][own];
     float *p = to.to[0];
     int64_t begin = to.begin[0];
 #pragma unroll
@@ -221,7 +288,10 @@ __global__ __launch_bounds__(1024) void kvb_sums_kernel(const float *part, int p
 
 void launch_sums(const float *part, int parts, int64_t columns, const SumsTo &to, hipStream_t stream)
 {
-    launch_part(kvb_sums_kernel, parts == 0, true, (columns + 63) / 64, 1024, stream, part, parts, columns, to);
+    if (parts > 64)
+        launch_part(kvb_sums_kernel<16>, parts == 0, true, (columns + 15) / 16, 1024, stream, part, parts, columns, to);
+    else
+        launch_part(kvb_sums_kernel<128>, parts == 0, true, (columns + 127) / 128, 1024, stream, part, parts, columns, to);
 }
 
 template <typename TX, typename T>
@@ -229,23 +299,17 @@ void launch_norm_grad_typed(const NormGradArgs &g, float *dweight, hipStream_t s
 {
     const NormArgs &a = g.f;
     const int vectors = a.width / 8;
-    if (g.parts == 0) {
-    } else if (vectors > 256) {
-        auto go = [&]<int NV, int WAVES>() { launch_part(kvb_norm_grad_row_kernel<TX, T, NV, WAVES>, true, false, g.parts, 64 * WAVES, stream, g); };
-        if (vectors <= 512)
-            go.template operator()<2, 4>();
-        else if (vectors <= 1024)
-            go.template operator()<4, 4>();
-        else
-            go.template operator()<4, 8>();
-    } else {
+    if (g.parts > 0 && vectors <= 64) {
         int lg = 2;
         while (lg < 6 && (1 << lg) < vectors)
             ++lg;
-        auto go = [&]<int NV>() { launch_part(kvb_norm_grad_kernel<TX, T, NV>, true, false, g.parts, 256, stream, g, lg); };
-        if (vectors <= 64)
+        launch_part(kvb_norm_grad_kernel<TX, T>, true, false, g.parts, 256, stream, g, lg);
+    } else if (g.parts > 0) {
+        const int nv = norm_vectors(a.width), threads = norm_threads(a.width), all = threads * norm_teams(a.width);
+        auto go = [&]<int NV>() { launch_part(kvb_norm_grad_row_kernel<TX, T, NV>, true, false, g.parts, all, stream, g, threads); };
+        if (nv == 1)
             go.template operator()<1>();
-        else if (vectors <= 128)
+        else if (nv == 2)
             go.template operator()<2>();
         else
             go.template operator()<4>();
