@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
     }
 }
 
-// T tokens of each request, a wave one of them: its taps' inputs are its ancestors and, behind the first of them, the state's rows.
+// One token of each request: the state's rows and the token's are the taps' inputs, and moved on by one row the next state.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, int units)
 {
@@ -172,123 +172,93 @@ __global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, i
     const int unit = blockIdx.x * 4 + wave, each = groups + a.gates;
     if (unit >= units)
         return;
-    const int token = unit / each, group = unit - token * each, b = token / a.T, i0 = token - b * a.T;
-    const int row = state_row(a.slot, a.n_slots, b);
-    if (row < 0)
-        return;
+    const int b = unit / each, group = unit - b * each;
     if (group == groups) {
-        gates_of<T>(a, token, 1, lane);
+        if (state_row(a.slot, a.n_slots, b) >= 0)
+            gates_of<T>(a, b, 1, lane);
         return;
     }
-    int up = -1;   // lane i: draft i's parent
-    if (a.parent) {
-        const int i = min(lane, a.T - 1), p = a.parent[(int64_t)b * a.T + i];
-        up = p < -1 || p >= i ? -1 : p;
-    } else {
-        up = lane - 1;
-    }
-    const int ch = group * CONV_LANES + lane * 8;
-    // places: a draft, or row W - 1 + place of the state
-    int place[W];
-    place[W - 1] = i0;
-#pragma unroll
-    for (int i = W - 2; i >= 0; --i)
-        place[i] = place[i + 1] >= 0 ? __builtin_amdgcn_readlane(up, place[i + 1]) : place[i + 1] - 1;
-    if (ch >= a.C)
-        return;
-    const T *x = static_cast<const T *>(a.x) + (int64_t)b * a.T * a.x_stride + ch;
-    const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch : nullptr;
-    Raw8<T> raw[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        if (place[i] >= 0)
-            raw[i] = load_raw8(x + (int64_t)place[i] * a.x_stride);
-        else
-            raw[i] = s0 ? load_raw8(s0 + (int64_t)(W - 1 + place[i]) * a.C) : Raw8<T>{};
-    }
+    const int own_ch = group * CONV_LANES + lane * 8, ch = own_ch < a.C ? own_ch : 0;
+    Raw8<T> raw[W] = {};
+    raw[W - 1] = load_raw8(static_cast<const T *>(a.x) + (int64_t)b * a.x_stride + ch);
     const Lane8<T, W> l(a, ch);
-    float z[8], e[W][8];
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-        unpack8(raw[i], e[i]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        z[j] = l.bias[j];
-#pragma unroll
-        for (int i = 0; i < W; ++i)
-            z[j] = fmaf(l.w[i][j], e[i][j], z[j]);
-    }
-    l.finish(z);
-    store8(l.to + (int64_t)token * l.to_stride, z);
-    if (a.state1) {   // (single tokens)
-        T *s1 = static_cast<T *>(a.state1) + (int64_t)row * (W - 1) * a.C + ch;
+    const int row = state_row(a.slot, a.n_slots, b);   // (behind the loads that do not need it)
+    if (row < 0 || own_ch >= a.C)
+        return;
+    const int64_t at = (int64_t)row * (W - 1) * a.C + ch;
+    if (a.state0)
 #pragma unroll
         for (int i = 0; i < W - 1; ++i)
-            store_raw8<false, true>(s1 + (int64_t)i * a.C, raw[i + 1]);
+            raw[i] = load_raw8(static_cast<const T *>(a.state0) + at + (int64_t)i * a.C);
+    float z[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        z[j] = l.bias[j];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        float e[8];
+        unpack8(raw[i], e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            z[j] = fmaf(l.w[i][j], e[j], z[j]);
+    }
+    l.finish(z);
+    store8(l.to + (int64_t)b * l.to_stride, z);
+    if (a.state1) {
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i)
+            store_raw8<false, true>(static_cast<T *>(a.state1) + at + (int64_t)i * a.C, raw[i + 1]);
     }
 }
 
-// The same, a wave all drafts of a request: every row is read once and handed from draft to draft in LDS, where a lane finds nothing but its own channels.
+// Drafts: a workgroup has all of a request's for 512 channels, a wave one of them.  A draft's taps reach back over its ancestors and then the state's rows;
+// every row is read once and found by the others in LDS, where a lane needs nothing but its own channels.
 template <typename T, int W>
-__global__ __launch_bounds__(64) void kvb_conv_drafts_kernel(const ConvArgs a)
+__global__ __launch_bounds__(64 * KVB_MAX_DRAFTS) void kvb_conv_drafts_kernel(const ConvArgs a)
 {
     __shared__ Raw8<T> rows[W - 1 + KVB_MAX_DRAFTS][64];
-    const int lane = threadIdx.x, groups = conv_groups(a.C), each = groups + a.gates, b = blockIdx.x / each, group = blockIdx.x - b * each;
-    const int row = state_row(a.slot, a.n_slots, b);
-    if (row < 0)
-        return;
+    const int lane = threadIdx.x % 64, i0 = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int groups = conv_groups(a.C), each = groups + a.gates, b = blockIdx.x / each, group = blockIdx.x - b * each, token = b * a.T + i0;
     if (group == groups) {
-        gates_of<T>(a, (int64_t)b * a.T, a.T, lane);
+        if (state_row(a.slot, a.n_slots, b) >= 0)
+            gates_of<T>(a, token, 1, lane);
         return;
     }
+    const int own_ch = group * CONV_LANES + lane * 8, ch = own_ch < a.C ? own_ch : 0;
+    const Raw8<T> own = load_raw8(static_cast<const T *>(a.x) + (int64_t)token * a.x_stride + ch);
+    const Lane8<T, W> l(a, ch);
     int up = lane - 1;   // lane i: draft i's parent
     if (a.parent) {
         const int i = min(lane, a.T - 1), p = a.parent[(int64_t)b * a.T + i];
         up = p < -1 || p >= i ? -1 : p;
     }
-    const int own_ch = group * CONV_LANES + lane * 8, ch = own_ch < a.C ? own_ch : 0;
-    const T *x = static_cast<const T *>(a.x) + (int64_t)b * a.T * a.x_stride + ch;
-    Raw8<T> state[W - 1] = {}, raw[KVB_MAX_DRAFTS];
-    if (a.state0) {
-        const T *s0 = static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch;
+    const int row = state_row(a.slot, a.n_slots, b);   // (behind the loads that do not need it)
+    if (row < 0)
+        return;
+    for (int i = i0; i < W - 1; i += a.T)
+        rows[i][lane] = a.state0 ? load_raw8(static_cast<const T *>(a.state0) + ((int64_t)row * (W - 1) + i) * a.C + ch) : Raw8<T>{};
+    rows[W - 1 + i0][lane] = own;
+    __syncthreads();
+    float z[8];
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i)
-            state[i] = load_raw8(s0 + (int64_t)i * a.C);
-    }
+    for (int j = 0; j < 8; ++j)
+        z[j] = l.bias[j];
+    int place[W];   // a draft, or row W - 1 + place of the state
+    place[W - 1] = i0;
 #pragma unroll
-    for (int i = 0; i < KVB_MAX_DRAFTS; ++i)
-        if (i < a.T)
-            raw[i] = load_raw8(x + (int64_t)i * a.x_stride);
-    const Lane8<T, W> l(a, ch);
+    for (int k = W - 2; k >= 0; --k)
+        place[k] = place[k + 1] >= 0 ? __builtin_amdgcn_readlane(up, place[k + 1]) : place[k + 1] - 1;
 #pragma unroll
-    for (int i = 0; i < W - 1; ++i)
-        rows[i][lane] = state[i];
-#pragma unroll
-    for (int i = 0; i < KVB_MAX_DRAFTS; ++i)
-        if (i < a.T)
-            rows[W - 1 + i][lane] = raw[i];
-    for (int i = 0; i < a.T; ++i) {
-        float z[8];
+    for (int k = 0; k < W; ++k) {
+        float e[8];
+        unpack8(rows[W - 1 + place[k]][lane], e);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            z[j] = l.bias[j];
-        int place[W];   // a draft, or row W - 1 + place of the state
-        place[W - 1] = i;
-#pragma unroll
-        for (int k = W - 2; k >= 0; --k)
-            place[k] = place[k + 1] >= 0 ? __builtin_amdgcn_readlane(up, place[k + 1]) : place[k + 1] - 1;
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-            float e[8];
-            unpack8(rows[W - 1 + place[k]][lane], e);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                z[j] = fmaf(l.w[k][j], e[j], z[j]);
-        }
-        l.finish(z);
-        if (own_ch < a.C)
-            store8(l.to + ((int64_t)b * a.T + i) * l.to_stride, z);
+            z[j] = fmaf(l.w[k][j], e[j], z[j]);
     }
+    l.finish(z);
+    if (own_ch < a.C)
+        store8(l.to + (int64_t)token * l.to_stride, z);
 }
 
 // The state behind the accepted drafts: the last W - 1 rows of the state and theirs.
@@ -372,12 +342,13 @@ void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 
 void launch_conv_tokens(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 {
-    const int each = conv_groups(a.C) + a.gates, units = a.B * a.T * each;
-    if (a.T > 1 && units >= 8192) {
-        with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_drafts_kernel<T, W>, true, true, a.B * each, 64, stream, a); });
-        return;
-    }
-    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_token_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units); });
+    const int each = conv_groups(a.C) + a.gates, units = a.B * each;
+    with_taps(dtype, width, [&]<typename T, int W>() {
+        if (a.T > 1)
+            launch_part(kvb_conv_drafts_kernel<T, W>, true, true, units, 64 * a.T, stream, a);
+        else
+            launch_part(kvb_conv_token_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units);
+    });
 }
 
 void launch_conv_commit(int dtype, int width, const ConvArgs &a, hipStream_t stream)

@@ -141,14 +141,18 @@ struct Piece {
 inline int64_t pieces_of(int64_t n_tokens, int64_t B, int most) { return n_tokens / most + B; }
 __device__ __forceinline__ Piece piece_at(const int32_t *start, int n_tokens, int B, int w, int most)   // every lane of the wave calls it
 {
+    // the last sequence whose first piece is w or before it: 64 candidates at a time, a 64th of what is left apart, then neighbours
     const int lane = threadIdx.x % 64;
-    int before = 0;   // sequences that start at or before w
-    for (int b0 = 0; b0 < B; b0 += 64) {
-        const int b = min(b0 + lane, B - 1);
-        const bool yes = b0 + lane < B && (int)((uint32_t)min(max(start[b], 0), n_tokens) / (uint32_t)most) + b <= w;
-        before += __popcll(__ballot(yes));
+    auto begins = [&](int b) { return (int)((uint32_t)min(max(start[b], 0), n_tokens) / (uint32_t)most) + b <= w; };
+    int b = 0, step = 1;
+    while ((int64_t)step * 64 < B)
+        step *= 64;
+    for (; step > 0; step /= 64) {
+        const int64_t at = b + (int64_t)lane * step;   // (lane 0's is known to begin, or is sequence 0)
+        const bool yes = at < B && begins((int)at);
+        b += max((int)__popcll(__ballot(yes)) - 1, 0) * step;
     }
-    const int b = __builtin_amdgcn_readfirstlane(max(before - 1, 0));
+    b = __builtin_amdgcn_readfirstlane(b);
     const Span s = span_of(start, n_tokens, b);
     const int c = w - ((int)((uint32_t)s.first / (uint32_t)most) + b);
     const int64_t at = (int64_t)c * most;
@@ -199,26 +203,28 @@ void launch_grad_norm(const ListArgs &a, float *norm, double *work, hipStream_t 
 void launch_clip(const ListArgs &a, const float *norm, float largest, hipStream_t stream);
 
 // Pieces of the convolution, and for its gradients how many a wave takes: a workgroup's four waves leave one part.
-constexpr int CONV_LEAST = 8;   // tokens of a piece (more than the taps reach back)
+constexpr int CONV_LEAST = 4;    // tokens of a piece (more than the taps reach back)
 struct ConvParts {
     int most, parts, each;
 };
-inline int conv_clamp(int64_t most, int64_t up) { return (int)(most < CONV_LEAST ? CONV_LEAST : most < up ? most : up); }
-constexpr int CONV_WG = 1536;
-inline int conv_most(int64_t n_tokens, int64_t B, int units)   // units: of a piece
+// Pieces are as long as fill the card once: waves that start behind others would run alone.  units: waves of a piece.  Where it takes no more than 8 tokens
+// a piece, a workgroup a compute unit.
+inline int conv_length(int64_t n_tokens, int64_t B, int units, int64_t workgroups, int64_t up)
 {
-    int64_t pieces = CONV_WG * 4 / units - B;
-    if (pieces < CONV_WG * 2 / units)
-        pieces = CONV_WG * 2 / units;
-    return conv_clamp((n_tokens + pieces - 1) / (pieces < 1 ? 1 : pieces), 64);
+    const int64_t few = 256 / units * 4 - B;
+    if (few > 0 && n_tokens <= 8 * few)
+        return n_tokens <= CONV_LEAST * few ? CONV_LEAST : (int)((n_tokens + few - 1) / few);
+    const int64_t most = workgroups / units < 1 ? 4 : workgroups / units * 4, pieces = B < most / 2 ? most - B : most / 2, length = (n_tokens + pieces - 1) / pieces;
+    return (int)(length < CONV_LEAST ? CONV_LEAST : length < up ? length : up);
 }
-constexpr int CONV_GRAD_WG = 512;
+constexpr int CONV_WG = 1536;
+inline int conv_most(int64_t n_tokens, int64_t B, int units) { return conv_length(n_tokens, B, units, CONV_WG, 64); }
+constexpr int CONV_GRAD_WG = 512;   // (two a compute unit: their registers)
 inline int64_t conv_part_limit(int units) { return CONV_GRAD_WG / units < 1 ? 1 : CONV_GRAD_WG / units; }
 inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units)
 {
-    const int64_t limit = conv_part_limit(units), want = B < 2 * limit ? 4 * limit - B : 2 * limit;
-    const int most = conv_clamp((n_tokens + want - 1) / want, INT32_MAX);
-    const int64_t pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
+    const int most = conv_length(n_tokens, B, units, CONV_GRAD_WG, INT32_MAX);
+    const int64_t limit = conv_part_limit(units), pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
     return ConvParts{most, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};
 }
 // The most that a call of up to so many tokens and sequences needs
