@@ -15,15 +15,15 @@ struct Part8 {
     Raw8<T> gate;
 };
 
-template <typename TX, typename T>
+template <bool STREAM, typename TX, typename T>
 __device__ __forceinline__ void load_part(const NormArgs &a, int64_t token, int64_t row, int64_t in_token, int at, Part8<TX, T> &p)
 {
-    const Raw8<TX> x = load_raw8(static_cast<const TX *>(a.x) + token * a.x_stride + in_token + at);
+    const Raw8<TX> x = load_raw8_if<STREAM>(static_cast<const TX *>(a.x) + token * a.x_stride + in_token + at);
     Raw8<TX> res{};
     if (a.res)
         res = load_raw8(static_cast<const TX *>(a.res) + row * a.width + at);
     if (a.gate)
-        p.gate = load_raw8(static_cast<const T *>(a.gate) + token * a.gate_stride + in_token + at);
+        p.gate = load_raw8_if<STREAM>(static_cast<const T *>(a.gate) + token * a.gate_stride + in_token + at);
     unpack8(x, p.s);
     if (a.res) {
         float y[8];
@@ -62,7 +62,7 @@ __device__ __forceinline__ float squares(const float (&s)[8], float sum)
 }  // namespace
 
 // 2^lg lanes a row, NV vectors of 8 a lane
-template <typename TX, typename T, int NV>
+template <typename TX, typename T, int NV, bool STREAM>
 __global__ __launch_bounds__(256) void kvb_norm_kernel(const NormArgs a, int lg)
 {
     const int lane = threadIdx.x % 64, lanes = 1 << lg, own = lane & (lanes - 1);
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void kvb_norm_kernel(const NormArgs a, int lg)
         for (int i = 0; i < NV; ++i) {
             const int at = 8 * (own + i * lanes);
             if (row < a.rows && at < a.width) {
-                load_part(a, token, row, in_token, at, p[i]);
+                load_part<STREAM>(a, token, row, in_token, at, p[i]);
                 sum = squares(p[i].s, sum);
             }
         }
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void kvb_norm_kernel(const NormArgs a, int lg)
 }
 
 // a workgroup a row
-template <typename TX, typename T, int NV, int WAVES>
+template <typename TX, typename T, int NV, int WAVES, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES) void kvb_norm_row_kernel(const NormArgs a)
 {
     __shared__ float part[WAVES];
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * WAVES) void kvb_norm_row_kernel(const NormArgs
         const int at = 8 * (threadIdx.x + i * 64 * WAVES);
         if (at < a.width) {
             w[i] = load_raw8(static_cast<const T *>(a.weight) + at);
-            load_part(a, token, row, in_token, at, p[i]);
+            load_part<STREAM>(a, token, row, in_token, at, p[i]);
             sum = squares(p[i].s, sum);
         }
     }
@@ -137,9 +137,17 @@ __global__ __launch_bounds__(64 * WAVES) void kvb_norm_row_kernel(const NormArgs
 template <typename TX, typename T>
 void launch_norm_typed(const NormArgs &a, hipStream_t stream)
 {
+    // x and the gate past the caches where they fill much of the last level: what reads the results next finds more of them there
+    const int64_t read = a.rows * a.width * (int64_t)(sizeof(TX) + (a.gate ? sizeof(T) : 0) + (a.res ? sizeof(TX) : 0));
+    const bool stream_x = read > 96 << 20;
     const int vectors = a.width / 8;
     if (vectors > 256 || (vectors > 64 && a.rows < 1024)) {
-        auto go = [&]<int NV, int WAVES>() { launch_part(kvb_norm_row_kernel<TX, T, NV, WAVES>, true, true, a.rows, 64 * WAVES, stream, a); };
+        auto go = [&]<int NV, int WAVES>() {
+            if (stream_x)
+                launch_part(kvb_norm_row_kernel<TX, T, NV, WAVES, true>, true, true, a.rows, 64 * WAVES, stream, a);
+            else
+                launch_part(kvb_norm_row_kernel<TX, T, NV, WAVES, false>, true, true, a.rows, 64 * WAVES, stream, a);
+        };
         if (vectors <= 256)
             go.template operator()<1, 4>();
         else if (vectors <= 512)
@@ -154,7 +162,12 @@ void launch_norm_typed(const NormArgs &a, hipStream_t stream)
     while (lg < 6 && (1 << lg) < vectors)
         ++lg;
     const int64_t rows_of_workgroup = 256 >> lg, n = (a.rows + rows_of_workgroup - 1) / rows_of_workgroup, blocks = n < 2048 ? n : 2048;
-    auto go = [&]<int NV>() { launch_part(kvb_norm_kernel<TX, T, NV>, true, true, blocks, 256, stream, a, lg); };
+    auto go = [&]<int NV>() {
+        if (stream_x)
+            launch_part(kvb_norm_kernel<TX, T, NV, true>, true, true, blocks, 256, stream, a, lg);
+        else
+            launch_part(kvb_norm_kernel<TX, T, NV, false>, true, true, blocks, 256, stream, a, lg);
+    };
     if (vectors <= 64)
         go.template operator()<1>();
     else if (vectors <= 128)
