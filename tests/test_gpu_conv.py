@@ -128,13 +128,11 @@ def test_rows_of_one_projection_and_rows_of_no_sequence(dtype):
     check_sequences(c, o, s1, c.state0)
 
 
-def test_large_launch_takes_longer_pieces():
-    """From 2^16 tokens times groups of 512 channels on a wave takes 32 tokens, not 8"""
+def test_large_calls():
+    """Longer pieces, and above 64 MiB x past the caches"""
     c = Case([4100, 1, 0, 2000, 31], 8, 16, 128, 4, "bf16", seed=3)
-    groups = -(-c.C // 512)
-    assert c.N * groups < 1 << 16
     big = Case([8000, 1, 0, 3000, 31], 8, 16, 128, 4, "bf16", seed=3)
-    assert big.N * groups >= 1 << 16
+    assert c.N * c.C * 2 <= 64 << 20 < big.N * big.C * 2
     for c in (c, big):
         o, s1 = run(c)
         # (the formulas for some stretches: whole sequences in 64 bits with bounds take long)
@@ -238,6 +236,19 @@ def test_single_tokens(B, W, heads, d, dtype):
     kvb.kvb_conv_decode(c.sh, c.ta, c.slot, c.n_slots, c.x, c.a, c.b, None, None, *mine)
     torch.cuda.synchronize()
     check_sequences(c, mine, None, None)
+
+
+@pytest.mark.parametrize("B", [64, 65, 200, 4096, 4097, 5000])
+def test_many_sequences(B):
+    """Sequences of one token or none, found among up to thousands: what kvb_conv_decode gives for those that have one"""
+    lens = [0 if b % 7 == 3 else 1 for b in range(B)]
+    c = Case(lens, 1, 2, 32, 4, "f32", seed=B, bias=True)
+    o, s1 = run(c)
+    some = torch.tensor([b for b in range(B) if lens[b]], device="cuda")
+    mine, state = c.outs(), c.state0.clone()
+    kvb.kvb_conv_decode(kvb.shape(len(some), 1, 2, 32, 32, 1, c.code), c.ta, c.slot[some].contiguous(), B, c.x, c.a, c.b, state, state, *mine)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(mine, o)) and torch.equal(s1, state)
 
 
 def random_tree(T, gen):

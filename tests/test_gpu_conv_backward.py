@@ -125,8 +125,15 @@ def test_no_tokens():
     assert all((r[n] == 0).all() for n in ("dweight", "dbias", "dA_log", "ddt_bias"))
 
 
-def test_long_sequences_where_a_wave_takes_several_pieces():
-    """From 32768 tokens on a part is more than four pieces of 32.  The weights' gradient of a long sequence is that of its halves together."""
+def test_a_wave_takes_several_short_sequences():
+    """More sequences than waves: 300, 224 waves for each 512 channels"""
+    c = Case([(b * 5 + b // 7) % 5 for b in range(300)], 8, 16, 128, 4, "bf16", seed=7, bias=True)
+    g = grads_of(c)
+    check_backward(c, g, backward(c, g))
+
+
+def test_long_sequences():
+    """Pieces of some forty tokens; the sums over tokens"""
     c = Case([20001, 20000], 1, 1, 32, 4, "bf16", seed=4)
     g = grads_of(c)
     whole = backward(c, g)
@@ -145,8 +152,8 @@ def test_long_sequences_where_a_wave_takes_several_pieces():
             want[:, i] += t.v.sum(0)
             size[:, i] += t.v.abs().sum(0)
             worst[:, i] += t.e.sum(0)
-    # two pieces of 32 a wave, four waves, up to 256 parts in 16 sums
-    check(whole["dweight"], V(want, worst + (64 + 4 + 16 + 16) * size), "dweight")
+    # a piece a wave, four waves, up to 256 parts in 16 sums or 64
+    check(whole["dweight"], V(want, worst + (64 + 4 + 16 + 64) * size), "dweight")
 
 
 def test_the_same_bits_and_a_replayed_graph():

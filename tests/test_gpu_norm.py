@@ -116,6 +116,20 @@ def test_rows_that_lie_apart(n, heads, width):
         assert (row[:, :8] == FILL).all() and (row[:, 8 + heads * width:] == FILL).all() and not (y == FILL).any()
 
 
+@pytest.mark.parametrize("n, heads, width, gate, res", [(13000, 32, 64, True, False), (26000, 1, 1000, False, True), (7000, 1, 4096, False, True)])
+def test_large_calls(n, heads, width, gate, res):
+    """Above 96 MiB of x, residual and gate these pass the caches: the same bits as smaller calls give"""
+    c = Rows(n, heads, width, "bf16", gate=gate, res=res)
+    assert n * heads * width * 4 > 96 << 20
+    s, out = forward(c)
+    for lo in range(0, n, n // 3):
+        hi, part = min(n, lo + n // 3), torch.empty_like(out[lo:lo + n // 3])
+        sums = torch.empty_like(part) if res else None
+        kvb.kvb_norm(kvb.rows(hi - lo, heads, width, c.code, eps=EPS, scale=c.scale), c.x[lo:hi], c.res[lo:hi] if res else None, c.gate[lo:hi] if gate else None, c.weight, sums, part)
+        torch.cuda.synchronize()
+        assert torch.equal(part, out[lo:hi]) and (not res or torch.equal(sums, s[lo:hi]))
+
+
 def test_in_place():
     """The residual's stream in place; out over x and over the gate"""
     c = Rows(100, 1, 1024, "bf16", res=True)
