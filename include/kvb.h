@@ -4,7 +4,7 @@
  * C ABI of the library.  Every pointer marked "device" is device memory owned
  * by the caller; the compute calls never allocate, free or synchronise, and
  * enqueue all work on the caller's HIP stream (`stream` is a hipStream_t passed
- * as void*; NULL = the default stream).  The two structs are host memory and are
+ * as void*; NULL = the default stream).  The structs are host memory and are
  * read only during the call.  The only state the library keeps is two
  * thread-local words on the host: the timer armed for the calling thread's next
  * launch (kvb_timer_arm) and the HIP error code behind the last KVB_EHIP.
@@ -377,6 +377,7 @@ int kvb_accept(const kvb_vocab *vocab, const int32_t *n_drafts, const int32_t *p
  * Around the recurrence: what makes a layer's q, k, v, g and beta from the rows of its projection (kvb_conv and its forms), the norms ahead of a
  * block and behind the recurrence (kvb_norm), and the norm of all gradients together (kvb_grad_norm, kvb_clip).
  */
+#define KVB_MIN_EPS   1e-30f   /* least eps of kvb_taps and kvb_rows */
 #define KVB_CONV_UNIT 1   /* kvb_taps.flags: q and k are divided by sqrt(sum of squares over the head + eps) */
 
 typedef struct kvb_taps {
@@ -391,7 +392,7 @@ typedef struct kvb_taps {
     int64_t      b_stride;
     int32_t      width;      /* 2, 3 or 4 taps                                                                                   */
     int32_t      flags;      /* KVB_CONV_UNIT                                                                                    */
-    float        eps;        /* above 0 with KVB_CONV_UNIT                                                                       */
+    float        eps;        /* at least KVB_MIN_EPS with KVB_CONV_UNIT                                                          */
 } kvb_taps;
 
 /*
@@ -468,7 +469,7 @@ typedef struct kvb_rows {
     int32_t width;        /* elements of a row: a multiple of 8, 8..KVB_MAX_WIDTH                                                         */
     int32_t dtype;        /* of gate, weight and out: KVB_F32, KVB_BF16 or KVB_F16                                                        */
     int32_t x_dtype;      /* of x, res and sum: KVB_F32 or dtype                                                                          */
-    float   eps;          /* above 0                                                                                                      */
+    float   eps;          /* at least KVB_MIN_EPS                                                                                        */
     float   scale;        /* of x where there is a residual, 1 where there is none                                                        */
 } kvb_rows;
 

@@ -242,7 +242,7 @@ int check_taps(const kvb_shape *sh, const kvb_taps *ta)
     for (const int64_t s : {ta->a_stride, ta->b_stride})
         if (s != 0 && (s < sh->Hv || s > 1 << 26))
             return KVB_EINVAL;
-    if (ta->width < 1 || (ta->flags & ~KVB_CONV_UNIT) != 0 || !std::isfinite(ta->eps) || ((ta->flags & KVB_CONV_UNIT) && !(ta->eps > 0.0f)))
+    if (ta->width < 1 || (ta->flags & ~KVB_CONV_UNIT) != 0 || !std::isfinite(ta->eps) || ((ta->flags & KVB_CONV_UNIT) && !(ta->eps >= KVB_MIN_EPS)))
         return KVB_EINVAL;
     return ta->width >= 2 && ta->width <= 4 ? KVB_OK : KVB_EUNSUPPORTED;
 }
@@ -334,7 +334,7 @@ int check_rows(const kvb_rows *ro)
             return KVB_EUNSUPPORTED;
     if (ro->x_dtype != KVB_F32 && ro->x_dtype != ro->dtype)
         return KVB_EUNSUPPORTED;
-    if (!(ro->eps > 0.0f) || !std::isfinite(ro->eps) || !std::isfinite(ro->scale))
+    if (!(ro->eps >= KVB_MIN_EPS) || !std::isfinite(ro->eps) || !std::isfinite(ro->scale))
         return KVB_EINVAL;
     const int64_t w = (int64_t)ro->heads * ro->width, size[2] = {ro->x_dtype == KVB_F32 ? 4 : 2, ro->dtype == KVB_F32 ? 4 : 2}, stride[2] = {ro->x_stride, ro->gate_stride};
     for (int i = 0; i < 2; ++i)

@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
                         }
                         sq = sum_to16(sq, lgh);
                         dot = sum_to16(dot, lgh);
-                        const float r = unit ? __builtin_amdgcn_rsqf(sq + a.eps) : 1.0f, c = unit ? r * r * r * dot : 0.0f;
+                        const float r = unit ? __builtin_amdgcn_rsqf(sq + a.eps) : 1.0f, c = unit ? r * dot * r * r : 0.0f;   // (r dot first: for a row of zeros it is 0)
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
                             d[j] = fmaf(r, d[j], -c * z[j]);   // dy

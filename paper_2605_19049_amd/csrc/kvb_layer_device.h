@@ -93,6 +93,9 @@ __device__ __forceinline__ float sum_lanes(float x, int lg)   // lg 2..6
     return x;
 }
 
+// (rows are at most 2^31 - 1: a division in 32 bits)
+__device__ __forceinline__ int64_t token_of(const NormArgs &a, int64_t row) { return a.heads == 1 ? row : (int64_t)((uint32_t)row / (uint32_t)a.heads); }
+
 // 1 / (1 + exp(-z))
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.442695041f * z)); }
 
@@ -127,7 +130,10 @@ __device__ __forceinline__ Raw8<T> load_raw8_if(const T *p)
     else
         return load_raw8(p);
 }
-// STREAM: past the caches.  (Not put's stores through the L2: conv_long_prompt's 63 us became 67, norm_grad_gated's 98 137.)
+// Results are left in the caches by plain stores: what comes next reads them.  us, kvb_conv of 8191 tokens (bf16, 16 + 32 heads of 128) with plain
+// stores / past the caches 59.7 / 55.3 alone, 576 / 585 with the kvb_scan that reads them; 24 sequences of 750 in all 562 / 572; kvb_norm, 18000 x 32 heads of 128,
+// gated, 88 / 84 alone, 405 / 416 with the matrix product that reads it.  Through the L2 as they are made (put): 66.6; kvb_norm_backward 137 instead of 98.
+// STREAM: past them all the same, for what would push out what is read again (kvb_clip).
 template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T *p, const float (&x)[8]) { store_raw8<STREAM, !STREAM>(p, pack8<T>(x)); }
 
@@ -207,23 +213,26 @@ constexpr int CONV_LEAST = 4;    // tokens of a piece (more than the taps reach 
 struct ConvParts {
     int most, parts, each;
 };
-// Pieces are as long as fill the card once: waves that start behind others would run alone.  units: waves of a piece.  Where it takes no more than 8 tokens
-// a piece, a workgroup a compute unit.
-inline int conv_length(int64_t n_tokens, int64_t B, int units, int64_t workgroups, int64_t up)
+// Pieces so long that the workgroups of four of them come out as `rounds` for each compute unit at most, the fewest with which a piece is no longer than `enough`
+// tokens: what starts behind others runs alone, and a short piece pays for its weights and the inputs ahead of it.  units: waves of a piece.
+// us, kvb_conv, 16 + 32 heads of 128, bf16, W = 4, enough 8 / 16: 1000 tokens 11.8 / 11.6, 2000 19.0 / 16.7; 8191 tokens in 4 rounds 66, 5 59.1, 6 59.2, 7 61.3,
+// 9 60.1.  kvb_conv_backward, whose registers let two workgroups share a compute unit: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112.
+inline int conv_length(int64_t n_tokens, int64_t B, int units, int rounds, int enough, int64_t up)
 {
-    const int64_t few = 256 / units * 4 - B;
-    if (few > 0 && n_tokens <= 8 * few)
-        return n_tokens <= CONV_LEAST * few ? CONV_LEAST : (int)((n_tokens + few - 1) / few);
-    const int64_t most = workgroups / units < 1 ? 4 : workgroups / units * 4, pieces = B < most / 2 ? most - B : most / 2, length = (n_tokens + pieces - 1) / pieces;
+    int64_t length = up;
+    for (int k = 1; k <= rounds; ++k) {
+        const int64_t most = 256 * k / units * 4, pieces = most < 4 ? 4 : B < most / 2 ? most - B : most / 2;
+        length = (n_tokens + pieces - 1) / pieces;
+        if (length <= enough)
+            break;
+    }
     return (int)(length < CONV_LEAST ? CONV_LEAST : length < up ? length : up);
 }
-constexpr int CONV_WG = 1536;
-inline int conv_most(int64_t n_tokens, int64_t B, int units) { return conv_length(n_tokens, B, units, CONV_WG, 64); }
-constexpr int CONV_GRAD_WG = 512;   // (two a compute unit: their registers)
-inline int64_t conv_part_limit(int units) { return CONV_GRAD_WG / units < 1 ? 1 : CONV_GRAD_WG / units; }
+inline int conv_most(int64_t n_tokens, int64_t B, int units) { return conv_length(n_tokens, B, units, 6, 16, 64); }
+inline int64_t conv_part_limit(int units) { return 512 / units < 1 ? 1 : 512 / units; }
 inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units)
 {
-    const int most = conv_length(n_tokens, B, units, CONV_GRAD_WG, INT32_MAX);
+    const int most = conv_length(n_tokens, B, units, 2, 12, INT32_MAX);
     const int64_t limit = conv_part_limit(units), pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
     return ConvParts{most, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};
 }
@@ -243,21 +252,33 @@ static_assert(KVB_LIST_BLOCK % (LIST_SPLIT * 8) == 0);
 inline int norm_vectors(int width) { return width <= 4096 ? 1 : width <= 8192 ? 2 : 4; }
 inline int norm_threads(int width) { return ((width / 8 + norm_vectors(width) - 1) / norm_vectors(width) + 63) / 64 * 64; }
 inline int norm_teams(int width) { return 512 / norm_threads(width); }
-// Its workgroups, each of which leaves one part
-inline int norm_parts(int64_t rows, int width)
+// Turns that rows take if each is a workgroup's
+inline int64_t norm_turns(int64_t rows, int width)
 {
-    int64_t at_once = norm_teams(width), most = 512;
+    int64_t at_once = norm_teams(width);
     if (width <= 512) {
         int lanes = 4;
         while (lanes < 64 && lanes * 8 < width)
             lanes *= 2;
         at_once = 256 / lanes;
-        most = 1024;
     }
-    const int64_t n = (rows + at_once - 1) / at_once;
-    return (int)(n < most ? n : most);
+    return (rows + at_once - 1) / at_once;
 }
-inline int64_t norm_most_parts(int64_t rows, int width) { return norm_parts(rows, width); }
+// Its workgroups, each of which leaves one part.  us with 1024 / 512, rows of up to 512 elements: 948 turns (bf16, 128 wide, gated) 13.6 / 11.9, 4000 20.7 / 24, 8000
+// 39.6 / 40.9, 16384 (x in fp32) 95.6 / 91.4, 36000 153.0 / 151.8.  Longer rows: what more parts there are is as much as rows.
+inline int norm_parts(int64_t rows, int width)
+{
+    const int64_t n = norm_turns(rows, width);
+    if (width > 512)
+        return (int)(n < 512 ? n : 512);
+    return (int)(n <= 256 ? n : n <= 1024 ? (n + 1) / 2 : n < 12288 ? 1024 : 512);
+}
+// The most that a call of up to so many rows needs
+inline int64_t norm_most_parts(int64_t rows, int width)
+{
+    const int64_t n = norm_turns(rows, width), most = width > 512 ? 512 : 1024;
+    return n < most ? n : most;
+}
 
 }  // namespace kvb_impl
 #endif  // KVB_LAYER_DEVICE_H

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void kvb_norm_kernel(const NormArgs a, int lg)
     }
     // (all lanes go round as often: sums go over all lanes of a row)
     for (int64_t first = (int64_t)blockIdx.x * 256 >> lg; first < a.rows; first += step) {
-        const int64_t row = first + (threadIdx.x >> lg), token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+        const int64_t row = first + (threadIdx.x >> lg), token = token_of(a, row), in_token = (row - token * a.heads) * a.width;
         Part8<TX, T> p[NV];
         float sum = 0.0f;
 #pragma unroll
@@ -101,7 +101,7 @@ template <typename TX, typename T, int NV, int WAVES, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES) void kvb_norm_row_kernel(const NormArgs a)
 {
     __shared__ float part[WAVES];
-    const int64_t row = blockIdx.x, token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+    const int64_t row = blockIdx.x, token = token_of(a, row), in_token = (row - token * a.heads) * a.width;
     Part8<TX, T> p[NV];
     Raw8<T> w[NV];
     float sum = 0.0f;

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void kvb_norm_grad_kernel(const NormGradArgs g
     unpack8(load_raw8(static_cast<const T *>(a.weight) + (at < a.width ? at : 0)), w);
     // (all lanes go round as often: sums go over all lanes of a row)
     for (int64_t first = (int64_t)blockIdx.x * 256 >> lg; first < a.rows; first += step) {
-        const int64_t row = first + (threadIdx.x >> lg), token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+        const int64_t row = first + (threadIdx.x >> lg), token = token_of(a, row), in_token = (row - token * a.heads) * a.width;
         const bool there = row < a.rows && at < a.width;
         GradRaw<TX, T> raw;
         Grad8<TX, T> p;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(512) void kvb_norm_grad_row_kernel(const NormGradAr
         load_weight();
     GradRaw<TX, T> raw[NV], next[NV];
     auto ask = [&](int64_t row, GradRaw<TX, T> (&r)[NV]) {
-        const int64_t token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+        const int64_t token = token_of(a, row), in_token = (row - token * a.heads) * a.width;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int at = 8 * (own + i * threads);
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(512) void kvb_norm_grad_row_kernel(const NormGradAr
         ask(first + team, next);
     int turn = 0;
     for (int64_t at_once = first; at_once < a.rows; at_once += step, turn ^= 1) {   // (the same for all waves)
-        const int64_t row = at_once + team, token = a.heads == 1 ? row : row / a.heads, in_token = (row - token * a.heads) * a.width;
+        const int64_t row = at_once + team, token = token_of(a, row), in_token = (row - token * a.heads) * a.width;
         Grad8<TX, T> p[NV];
         float sq = 0.0f, dot = 0.0f;
         if (NV < 4) {

@@ -19,6 +19,7 @@ STATUS_BADPATH = 2
 STORE_STREAM, STORE_RESIDENT, STORE_FILL_APART = 1, 2, 4
 FILL_APART = 32   # words from one slot's fill to the next with STORE_FILL_APART
 CONV_UNIT = 1
+MIN_EPS = 1e-30
 MAX_WIDTH = 16384
 LIST_BLOCK = 16384
 
@@ -398,6 +399,10 @@ def _check_layouts(fn_name, args):
     if fn_name in _CONV_NAMES:
         seqs_too = fn_name in ("kvb_conv", "kvb_conv_backward")
         _check_conv(_CONV_NAMES[fn_name], args[0], args[1], args[2] if seqs_too else None, args[3 if seqs_too else 2:])
+    elif fn_name == "kvb_clip":
+        li, to = getattr(args[0], "of", None), getattr(args[1], "of", None)
+        if li is not None and to is not None and (li.sizes, li.types) != (to.sizes, to.types):
+            raise ValueError("kvb_clip: tensors of other sizes or types than those they are made from")
     elif fn_name == "kvb_norm":
         _check_norm(_NORM, args[0], args[1:])
     elif fn_name == "kvb_norm_backward":
@@ -554,7 +559,9 @@ class TensorList:
 
     def c(self):
         some = bool(self.tensors)
-        return KvbList(*((_ptr(x) if some else None) for x in (self._data, self._size, self._type, self._first)), len(self.tensors), self.blocks)
+        li = KvbList(*((_ptr(x) if some else None) for x in (self._data, self._size, self._type, self._first)), len(self.tensors), self.blocks)
+        li.of = self
+        return li
 
 
 def grad_norm_work(li):

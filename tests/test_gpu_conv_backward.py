@@ -156,6 +156,34 @@ def test_long_sequences():
     check(whole["dweight"], V(want, worst + (64 + 4 + 16 + 64) * size), "dweight")
 
 
+def test_zero_rows_with_the_least_eps():
+    """Rows of zeros have keys of zero; what reaches them is the gradient over sqrt(eps), and nothing that is not a number"""
+    c = Case([20], 1, 2, 64, 4, "f32", seed=9)
+    c.x.zero_()
+    c.state0.zero_()
+    g = grads_of(c)
+    c.ta = kvb.taps(c.weight, width=4, A_log=c.A_log, dt_bias=c.dt_bias, eps=kvb.MIN_EPS)
+    c.taps = lambda unit=True: c.ta
+    r = backward(c, g)
+    assert all(torch.isfinite(y).all() for y in r.values() if y is not None)
+    dz = 0.5 * g["dk"].double().flatten(1) * 1e15   # silu's slope at 0, 1 / sqrt(1e-30)
+    w = c.weight[64:128].double()
+    want = sum(w[:, i] * torch.nn.functional.pad(dz, (0, 0, 0, 3))[3 - i:23 - i] for i in range(4))
+    assert ((r["dx"][:, 64:128].double() - want).abs() <= 32 * 2.0 ** -24 * sum(w[:, i].abs() * torch.nn.functional.pad(dz.abs(), (0, 0, 0, 3))[3 - i:23 - i] for i in range(4))).all()
+
+
+def test_timers():
+    """From the first kernel's begin to the last one's end"""
+    c = Case([3000], 2, 4, 128, 4, "bf16", seed=10)
+    g, timer = grads_of(c), kvb.Timer()
+    for call in (lambda: run(c), lambda: backward(c, g)):
+        call()
+        timer.arm()
+        call()
+        assert 1.0 < timer.us() < 1e4
+    timer.close()
+
+
 def test_the_same_bits_and_a_replayed_graph():
     c = Case([70, 3, 130], 2, 4, 128, 4, "bf16", seed=5)
     g = grads_of(c)

@@ -71,7 +71,7 @@ def test_shapes(bad, code):
     (dict(weight=None), kvb.EINVAL), (dict(weight=A + 2), kvb.EINVAL), (dict(bias=A + 8), kvb.EINVAL), (dict(A_log=A + 2), kvb.EINVAL), (dict(dt_bias=A + 1), kvb.EINVAL),
     (dict(x_stride=C - 8), kvb.EINVAL), (dict(x_stride=C + 4), kvb.EINVAL), (dict(x_stride=1 << 26), kvb.EINVAL), (dict(a_stride=3), kvb.EINVAL),
     (dict(b_stride=(1 << 26) + 1), kvb.EINVAL), (dict(width=0), kvb.EINVAL), (dict(width=1), kvb.EUNSUPPORTED), (dict(width=5), kvb.EUNSUPPORTED),
-    (dict(flags=2), kvb.EINVAL), (dict(eps=0.0), kvb.EINVAL), (dict(eps=-1.0), kvb.EINVAL), (dict(eps=float("nan")), kvb.EINVAL), (dict(eps=float("inf")), kvb.EINVAL)])
+    (dict(flags=2), kvb.EINVAL), (dict(eps=0.0), kvb.EINVAL), (dict(eps=1e-31), kvb.EINVAL), (dict(eps=-1.0), kvb.EINVAL), (dict(eps=float("nan")), kvb.EINVAL), (dict(eps=float("inf")), kvb.EINVAL)])
 def test_taps(bad, code):
     for f in FORMS:
         # (a bias goes with its gradient)
@@ -162,7 +162,7 @@ def norm_back(ro=None, **kw):
 @pytest.mark.parametrize("bad, code", [
     (dict(n_tokens=-1), kvb.EINVAL), (dict(heads=0), kvb.EINVAL), (dict(width=0), kvb.EINVAL), (dict(width=12), kvb.EINVAL), (dict(width=16392), kvb.EINVAL),
     (dict(dtype=3), kvb.EUNSUPPORTED), (dict(x_dtype=7), kvb.EUNSUPPORTED), (dict(x_dtype=kvb.F16), kvb.EUNSUPPORTED), (dict(dtype=kvb.F32, x_dtype=kvb.BF16), kvb.EUNSUPPORTED),
-    (dict(eps=0.0), kvb.EINVAL), (dict(eps=float("nan")), kvb.EINVAL), (dict(eps=float("inf")), kvb.EINVAL), (dict(scale=float("inf")), kvb.EINVAL),
+    (dict(eps=0.0), kvb.EINVAL), (dict(eps=1e-31), kvb.EINVAL), (dict(eps=float("nan")), kvb.EINVAL), (dict(eps=float("inf")), kvb.EINVAL), (dict(scale=float("inf")), kvb.EINVAL),
     (dict(x_stride=64), kvb.EINVAL), (dict(x_stride=132), kvb.EINVAL), (dict(gate_stride=129), kvb.EINVAL), (dict(gate_stride=1 << 26), kvb.EINVAL),
     (dict(n_tokens=2 ** 31 - 1), kvb.EINVAL), (dict(heads=1 << 20), kvb.EINVAL)])
 def test_rows(bad, code):
@@ -210,6 +210,14 @@ def test_tensor_lists():
     li = kvb.TensorList([torch.zeros(5), torch.zeros(kvb.LIST_BLOCK + 1, dtype=torch.bfloat16), torch.zeros(0), torch.zeros(2, 3, dtype=torch.float16)])
     assert li.blocks == 4 and li._first.tolist() == [0, 1, 3, 3, 4] and li._type.tolist() == [kvb.F32, kvb.BF16, kvb.F32, kvb.F16]
     assert li._size.tolist() == [5, kvb.LIST_BLOCK + 1, 0, 6] and li._data.tolist() == [t.data_ptr() for t in li.tensors]
+    other = [torch.ones_like(t) for t in li.tensors]
+    empty = kvb.KvbList(None, None, None, None, 0, 0)
+    for i, t in enumerate((torch.zeros(4), torch.zeros(kvb.LIST_BLOCK + 2, dtype=torch.bfloat16), torch.zeros(1), torch.zeros(6))):   # another size or type
+        with pytest.raises(ValueError, match="sizes or types"):
+            kvb.kvb_clip(li.c(), kvb.TensorList(other[:i] + [t] + other[i + 1:]).c(), A, 1.0, stream=0)
+    with pytest.raises(ValueError, match="sizes or types"):
+        kvb.bind("kvb_clip", li.c(), kvb.TensorList(other[:3]).c(), A, 1.0, 0)
+    assert kvb.kvb_clip(kvb.TensorList([], device="cpu").c(), empty, A, 1.0, stream=0) == kvb.OK
     for bad in (torch.zeros(3, dtype=torch.float64), torch.zeros(3, dtype=torch.int32), torch.zeros(4, 6)[:, ::2], torch.zeros(4, 6).t()):
         with pytest.raises(ValueError):
             kvb.TensorList([torch.zeros(2), bad])
