@@ -3,6 +3,9 @@
 // A workgroup takes KVB_LIST_BLOCK elements of one tensor.  Squares are exact and summed in fp64: no range is left, and the norm does not
 // depend on how the tensors are cut by more than its last bit.  Addresses need only an element's alignment: whole 16 bytes lie between a
 // few elements at either end.
+// Bounded by memory: 43 M bf16 elements are read in 15.6 us (5.5 TB/s, eight loads of a thread on their way; four: 24.6), then read once more and written in 26.8; both with the
+// norm between them 45 us.  Results go past the caches: what of the tensors the first pass left there is then still there (plain stores: 54 us; 134 M
+// elements in place, read by an addition next: the same either way).  Eleven small tensors 9.1 us, three launches.
 #include "kvb_layer_device.h"
 
 namespace kvb_impl {

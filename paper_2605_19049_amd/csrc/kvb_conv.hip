@@ -3,7 +3,11 @@
 //     z_t = bias + sum_i w_i E_{t+i},  y = z / (1 + exp(-z)),  q, k = y / sqrt(sum y^2 + eps) over a head,  v = y
 //     g = -exp(A_log) log(1 + exp(a + dt_bias)),  beta = 1 / (1 + exp(-b))
 // A lane has 8 channels, so that loads and stores are 16 bytes (16-bit types), a head is 4, 8 or 16 neighbouring lanes and its sum of squares
-// stays inside a row of 16.  A wave has 512 channels; the units behind the channels' are the gates'.
+// stays inside a row of 16.  A wave has 512 channels; the units behind the channels' are the gates'.  All arithmetic is fp32; what is rounded
+// is the result, once, to its own type.
+// Bounded by memory: 8191 tokens, 16 + 32 heads of 128, bf16, 272 MB in 59 us or 4.6 TB/s (a copy: 5.0 .. 5.2), of which the vector units are busy some 40: 130
+// instructions for a token's 8 channels, two of them slow (exp2, rcp).  Small calls are bounded by the chain launch, start, slot, inputs: a prompt of 37 tokens 4.9 us, a
+// single token 3.8, 64 of them 4.0, 512 11.6 (67 MB, 5.8 TB/s, some of it from the last level).
 #include "kvb_layer_device.h"
 
 namespace kvb_impl {
@@ -212,7 +216,8 @@ __global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, i
 }
 
 // Drafts: a workgroup has all of a request's for 512 channels, a wave one of them.  A draft's taps reach back over its ancestors and then the state's rows;
-// every row is read once and found by the others in LDS, where a lane needs nothing but its own channels.
+// every row is read once and found by the others in LDS, where a lane needs nothing but its own channels.  us with the commit behind it, tree of 4 for
+// 128 requests, bf16, 16 + 32 heads of 128: 13.3; each draft reading its rows by itself 14.2; a wave all drafts of a request 13.9 (but 256 requests of 8: 28.3, here 30.5).
 template <typename T, int W>
 __global__ __launch_bounds__(64 * KVB_MAX_DRAFTS) void kvb_conv_drafts_kernel(const ConvArgs a)
 {
@@ -329,8 +334,9 @@ void with_taps(int dtype, int width, F &&f)
 
 void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 {
-    const int each = conv_groups(a.C) + a.gates, most = conv_most(a.n_tokens, a.B, each), units = (int)(pieces_of(a.n_tokens, a.B, most) * each);
-    // x past the caches where it and what is made from it fill half of the last level: what reads the results next finds more of them there
+    const int each = conv_groups(a.C) + a.gates, most = conv_most(a.n_tokens, a.B, each, dtype == KVB_F32), units = (int)(pieces_of(a.n_tokens, a.B, most) * each);
+    // x past the caches where it and what is made from it fill half of the last level: what reads the results next finds more of them there.  us with the
+    // kvb_scan behind it, plain / past them: 300 tokens 38.2 / 38.9, 1024 84.7 / 85.2, 4096 (64 MiB) 286.3 / 286.0, 8191 576 / 571, 24 sequences of 750 562 / 558.
     const bool stream_x = (int64_t)a.n_tokens * a.C * (dtype == KVB_F32 ? 4 : 2) > 64 << 20;
     with_taps(dtype, width, [&]<typename T, int W>() {
         if (stream_x)

@@ -2,10 +2,14 @@
 //     dy = r (dn - r^2 y (y.dn)) for q and k, dn for v          dz = dy (s + y (1 - s))
 //     dE_e = sum_i w_i dz_{e-i}                                 dw_i = sum_t dz_t E_{t+i},  dbias = sum_t dz_t
 //     da = -exp(A_log) dg / (1 + exp(-(a + dt_bias))),  db = dbeta beta (1 - beta),  dA_log = sum dg g,  ddt_bias = sum da
-// A wave walks forward over 32 tokens of 512 channels and W - 1 more (whose dz its last inputs need), the last W inputs and dz in registers.
+// A wave walks forward over a piece's tokens of 512 channels and W - 1 more (whose dz its last inputs need), the last W inputs and dz in registers.
 // E's rows ahead of the first input are the state's: their gradient is dstate0; the last W - 1 rows get dstate1 as well.  Sums over tokens stay
 // in registers, then the four waves of a workgroup add theirs in LDS and leave one part; kvb_sums_kernel adds the parts in order, so
 // the same inputs give the same bits.
+// Bounded by memory and the vector units about alike: 4 x 2048 tokens, 16 + 32 heads of 128, bf16, 408 MB (a copy: 80 us) take 97 us, 5 of them the sums; the vector units are
+// busy 64 of them (counters: 32.6 M instructions), with two waves a SIMD (216 registers), so what counts is that all of those have as much to do: pieces as
+// long as fill the card once (three rounds of shorter ones took 136), and the groups of q and k, which have norms, on one compute unit with
+// those of v, which do not (group by group in the launch: 97, piece by piece: 106).
 #ifndef KVB_CONV_GRAD_KERNEL_H
 #define KVB_CONV_GRAD_KERNEL_H
 
@@ -36,7 +40,7 @@ __device__ __forceinline__ void gate_grads(const ConvGradArgs &g, int64_t t0, in
 template <typename T, int W, bool BIAS>
 __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g, int most)
 {
-    constexpr int AHEAD = 2;   // tokens asked for ahead
+    constexpr int AHEAD = 2;   // tokens asked for ahead (4: 98.5 us instead of 97.0, for the registers)
     constexpr int PLANE = CONV_LANES;
     __shared__ float sums[4][(W + BIAS) * PLANE];
     const ConvArgs &a = g.f;

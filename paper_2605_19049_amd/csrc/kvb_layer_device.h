@@ -216,7 +216,7 @@ struct ConvParts {
 // Pieces so long that the workgroups of four of them come out as `rounds` for each compute unit at most, the fewest with which a piece is no longer than `enough`
 // tokens: what starts behind others runs alone, and a short piece pays for its weights and the inputs ahead of it.  units: waves of a piece.
 // us, kvb_conv, 16 + 32 heads of 128, bf16, W = 4, enough 8 / 16: 1000 tokens 11.8 / 11.6, 2000 19.0 / 16.7; 8191 tokens in 4 rounds 66, 5 59.1, 6 59.2, 7 61.3,
-// 9 60.1.  kvb_conv_backward, whose registers let two workgroups share a compute unit: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112.
+// 9 60.1; fp32, 5284 tokens, W = 3, in 3 80.8, 4 84.4, 6 83.9.  kvb_conv_backward, whose registers let two workgroups share a compute unit: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112.
 inline int conv_length(int64_t n_tokens, int64_t B, int units, int rounds, int enough, int64_t up)
 {
     int64_t length = up;
@@ -228,7 +228,7 @@ inline int conv_length(int64_t n_tokens, int64_t B, int units, int rounds, int e
     }
     return (int)(length < CONV_LEAST ? CONV_LEAST : length < up ? length : up);
 }
-inline int conv_most(int64_t n_tokens, int64_t B, int units) { return conv_length(n_tokens, B, units, 6, 16, 64); }
+inline int conv_most(int64_t n_tokens, int64_t B, int units, bool wide) { return conv_length(n_tokens, B, units, wide ? 3 : 6, 16, 64); }
 inline int64_t conv_part_limit(int units) { return 512 / units < 1 ? 1 : 512 / units; }
 inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units)
 {
