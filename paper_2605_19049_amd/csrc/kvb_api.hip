@@ -270,8 +270,8 @@ ConvArgs conv_args(const kvb_shape *sh, const kvb_taps *ta, const void *x, const
     const int64_t C = conv_channels(sh);
     r.x = x, r.a = a, r.b = b, r.weight = ta->weight, r.bias = ta->bias, r.A_log = ta->A_log, r.dt_bias = ta->dt_bias, r.state0 = state0;
     r.x_stride = ta->x_stride ? ta->x_stride : C, r.a_stride = ta->a_stride ? ta->a_stride : sh->Hv, r.b_stride = ta->b_stride ? ta->b_stride : sh->Hv;
-    r.q_stride = r.k_stride = (int64_t)sh->Hk * sh->dk, r.v_stride = (int64_t)sh->Hv * sh->dv;
-    r.B = sh->B, r.T = 1, r.Hk = sh->Hk, r.Hv = sh->Hv, r.d = sh->dk, r.C = (int)C, r.gates = a != nullptr, r.unit = ta->flags & KVB_CONV_UNIT, r.eps = ta->eps;
+    r.q_stride = r.k_stride = sh->Hk * sh->dk, r.v_stride = sh->Hv * sh->dv;
+    r.B = sh->B, r.Hk = sh->Hk, r.Hv = sh->Hv, r.d = sh->dk, r.C = (int)C, r.gates = a != nullptr, r.unit = ta->flags & KVB_CONV_UNIT, r.eps = ta->eps;
     return r;
 }
 void conv_seqs(ConvArgs &r, const kvb_seqs *sq)
@@ -309,10 +309,13 @@ int conv_tokens_common(const kvb_shape *sh, const kvb_taps *ta, const int32_t *s
     if (sh->B == 0)
         return KVB_OK;
     ConvArgs r = conv_args(sh, ta, x, a, b, state0);
-    r.slot = slot, r.n_slots = n_slots, r.T = T, r.parent = parent, r.state1 = state1;
+    r.slot = slot, r.n_slots = n_slots, r.state1 = state1;
     r.q = q, r.k = k, r.v = v, r.g = g, r.beta = beta;
     g_launch_status = hipSuccess;
-    launch_conv_tokens(sh->in_dtype, ta->width, r, static_cast<hipStream_t>(stream));
+    if (T > 1)
+        launch_conv_drafts(sh->in_dtype, ta->width, ConvDraftArgs{r, parent, T}, static_cast<hipStream_t>(stream));
+    else
+        launch_conv_token(sh->in_dtype, ta->width, r, static_cast<hipStream_t>(stream));
     return finish_launch();
 }
 
@@ -419,10 +422,10 @@ int kvb_conv_commit(const kvb_shape *shape, const kvb_taps *taps, const int32_t 
         return KVB_EINVAL;
     if (shape->B == 0)
         return KVB_OK;
-    ConvArgs r = conv_args(shape, taps, x, nullptr, nullptr, state0);
-    r.slot = slot, r.n_slots = n_slots, r.T = T, r.path = path, r.accepted = accepted, r.state1 = state1;
+    const ConvArgs r = conv_args(shape, taps, x, nullptr, nullptr, state0);
     g_launch_status = hipSuccess;
-    launch_conv_commit(shape->in_dtype, taps->width, r, static_cast<hipStream_t>(stream));
+    launch_conv_commit(shape->in_dtype, taps->width, ConvCommitArgs{x, state0, state1, slot, path, accepted, r.x_stride, shape->B, T, n_slots, r.C},
+                       static_cast<hipStream_t>(stream));
     return finish_launch();
 }
 

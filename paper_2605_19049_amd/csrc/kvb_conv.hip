@@ -24,7 +24,8 @@ struct Lane8 {
     bool unit;           // q or k, to be of length one
     float eps;
 
-    __device__ __forceinline__ Lane8(const ConvArgs &a, int ch) : lg(a.d == 128 ? 4 : a.d == 64 ? 3 : 2), eps(a.eps)
+    // (strides: elements from a token's q to the next one's, and of k and v)
+    __device__ __forceinline__ Lane8(const ConvBase &a, int ch, int64_t q_stride, int64_t k_stride, int64_t v_stride) : lg(a.d == 128 ? 4 : a.d == 64 ? 3 : 2), eps(a.eps)
     {
         const T *wp = static_cast<const T *>(a.weight) + (int64_t)ch * W;
         Raw8<T> raw[W], rb{};
@@ -45,8 +46,9 @@ struct Lane8 {
         const int nq = a.Hk * a.d;
         unit = a.unit && ch < 2 * nq;
         to = ch < nq ? static_cast<T *>(a.q) + ch : ch < 2 * nq ? static_cast<T *>(a.k) + (ch - nq) : static_cast<T *>(a.v) + (ch - 2 * nq);
-        to_stride = ch < nq ? a.q_stride : ch < 2 * nq ? a.k_stride : a.v_stride;
+        to_stride = ch < nq ? q_stride : ch < 2 * nq ? k_stride : v_stride;
     }
+    __device__ __forceinline__ Lane8(const ConvBase &a, int ch) : Lane8(a, ch, a.Hk * a.d, a.Hk * a.d, a.Hv * a.d) {}   // packed
     // y from z, and of length one
     __device__ __forceinline__ void finish(float (&z)[8]) const
     {
@@ -66,7 +68,7 @@ struct Lane8 {
 
 // Gates of the tokens t0 .. t1-1
 template <typename T>
-__device__ __forceinline__ void gates_of(const ConvArgs &a, int64_t t0, int n, int lane)
+__device__ __forceinline__ void gates_of(const ConvBase &a, int64_t t0, int n, int lane)
 {
     const GateLanes l = gate_lanes(a.Hv, lane);
     for (int h = l.head; h < a.Hv; h += l.heads) {
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
                 raw[u] = load_raw8_if<STREAM>(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
         };
         request(p.t0);
-        const Lane8<T, W> l(a, ch);
+        const Lane8<T, W> l(a, ch, a.q_stride, a.k_stride, a.v_stride);
         float e[W - 1 + U][8];
 #pragma unroll
         for (int i = 0; i < W - 1; ++i)
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
 
 // One token of each request: the state's rows and the token's are the taps' inputs, and moved on by one row the next state.
 template <typename T, int W>
-__global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, int units)
+__global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvTokenArgs a, int units)
 {
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
     const int unit = blockIdx.x * 4 + wave, each = groups + a.gates;
@@ -217,9 +219,10 @@ __global__ __launch_bounds__(256) void kvb_conv_token_kernel(const ConvArgs a, i
 
 // Drafts: a workgroup has all of a request's for 512 channels, a wave one of them.  A draft's taps reach back over its ancestors and then the state's rows;
 // every row is read once and found by the others in LDS, where a lane needs nothing but its own channels.  us with the commit behind it, tree of 4 for
-// 128 requests, bf16, 16 + 32 heads of 128: 13.3; each draft reading its rows by itself 14.2; a wave all drafts of a request 13.9 (but 256 requests of 8: 28.3, here 30.5).
+// 128 requests, bf16, 16 + 32 heads of 128: 12.5 (13.3 with launch arguments of 250 bytes instead of 180, and so
+// were: each draft reading its rows by itself 14.2, a wave all drafts of a request 13.9, but 256 requests of 8 28.3, here 30.5).
 template <typename T, int W>
-__global__ __launch_bounds__(64 * KVB_MAX_DRAFTS) void kvb_conv_drafts_kernel(const ConvArgs a)
+__global__ __launch_bounds__(64 * KVB_MAX_DRAFTS) void kvb_conv_drafts_kernel(const ConvDraftArgs a)
 {
     __shared__ Raw8<T> rows[W - 1 + KVB_MAX_DRAFTS][64];
     const int lane = threadIdx.x % 64, i0 = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(64 * KVB_MAX_DRAFTS) void kvb_conv_drafts_kernel(co
 
 // The state behind the accepted drafts: the last W - 1 rows of the state and theirs.
 template <typename T, int W>
-__global__ __launch_bounds__(256) void kvb_conv_commit_kernel(const ConvArgs a, int units)
+__global__ __launch_bounds__(256) void kvb_conv_commit_kernel(const ConvCommitArgs a, int units)
 {
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
     const int unit = blockIdx.x * 4 + wave;
@@ -346,18 +349,19 @@ void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
     });
 }
 
-void launch_conv_tokens(int dtype, int width, const ConvArgs &a, hipStream_t stream)
+void launch_conv_token(int dtype, int width, const ConvTokenArgs &a, hipStream_t stream)
 {
-    const int each = conv_groups(a.C) + a.gates, units = a.B * each;
-    with_taps(dtype, width, [&]<typename T, int W>() {
-        if (a.T > 1)
-            launch_part(kvb_conv_drafts_kernel<T, W>, true, true, units, 64 * a.T, stream, a);
-        else
-            launch_part(kvb_conv_token_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units);
-    });
+    const int units = a.B * (conv_groups(a.C) + a.gates);
+    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_token_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units); });
 }
 
-void launch_conv_commit(int dtype, int width, const ConvArgs &a, hipStream_t stream)
+void launch_conv_drafts(int dtype, int width, const ConvDraftArgs &a, hipStream_t stream)
+{
+    const int units = a.B * (conv_groups(a.C) + a.gates);
+    with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_drafts_kernel<T, W>, true, true, units, 64 * a.T, stream, a); });
+}
+
+void launch_conv_commit(int dtype, int width, const ConvCommitArgs &a, hipStream_t stream)
 {
     const int units = a.B * conv_groups(a.C);
     with_taps(dtype, width, [&]<typename T, int W>() { launch_part(kvb_conv_commit_kernel<T, W>, true, true, (units + 3) / 4, 256, stream, a, units); });

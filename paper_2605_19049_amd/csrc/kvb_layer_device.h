@@ -10,21 +10,38 @@ namespace kvb_impl {
 // ---------------------------------------------------------------------------
 // arguments
 // ---------------------------------------------------------------------------
-struct ConvArgs {
+// (A launch pays for its arguments, some half a microsecond for 100 bytes: each form of the convolution has no more than it needs.)
+struct ConvBase {
     const void *x, *a, *b;            // rows of C, Hv and Hv elements
     const void *weight, *bias;        // [C][width], [C] or nullptr
     const float *A_log, *dt_bias;     // [Hv]
     const void *state0;               // [n_slots][width - 1][C] or nullptr: zero
-    void *state1;                     // the same, or nullptr: not wanted
     void *q, *k, *v;
     float *g, *beta;                  // [n_tokens][Hv]
-    const int32_t *start, *slot;      // whole sequences: [B + 1]; [B] or nullptr
-    const int32_t *parent;            // drafts: [B][T] or nullptr: a chain
-    const int32_t *path, *accepted;   // commit: [B][T] or nullptr: 0, 1, ..; [B]
-    int64_t x_stride, a_stride, b_stride, q_stride, k_stride, v_stride;
-    int32_t B, T, n_slots, n_tokens, Hk, Hv, d, C;
-    int32_t gates, unit;              // whether there are gates; whether q and k get length one
+    const int32_t *slot;              // [B], or nullptr for whole sequences: row b
+    int64_t x_stride, a_stride, b_stride;
+    int32_t B, n_slots, Hk, Hv, d, C;
+    int16_t gates, unit;              // whether there are gates; whether q and k get length one
     float eps;
+};
+struct ConvTokenArgs : ConvBase {
+    void *state1;                     // as state0, or nullptr: not wanted
+};
+struct ConvDraftArgs : ConvBase {
+    const int32_t *parent;            // [B][T] or nullptr: a chain
+    int32_t T;
+};
+struct ConvArgs : ConvTokenArgs {
+    const int32_t *start;             // [B + 1]
+    int64_t q_stride, k_stride, v_stride;
+    int32_t n_tokens;
+};
+struct ConvCommitArgs {
+    const void *x, *state0;
+    void *state1;
+    const int32_t *slot, *path, *accepted;   // path: [B][T] or nullptr: 0, 1, ..
+    int64_t x_stride;
+    int32_t B, T, n_slots, C;
 };
 
 struct ConvGradArgs {
@@ -196,8 +213,9 @@ void launch_sums(const float *part, int parts, int64_t columns, const SumsTo &to
 
 // (in_dtype and width are checked by the caller)
 void launch_conv(int in_dtype, int width, const ConvArgs &a, hipStream_t stream);          // kvb_conv.hip
-void launch_conv_tokens(int in_dtype, int width, const ConvArgs &a, hipStream_t stream);
-void launch_conv_commit(int in_dtype, int width, const ConvArgs &a, hipStream_t stream);
+void launch_conv_token(int in_dtype, int width, const ConvTokenArgs &a, hipStream_t stream);
+void launch_conv_drafts(int in_dtype, int width, const ConvDraftArgs &a, hipStream_t stream);
+void launch_conv_commit(int in_dtype, int width, const ConvCommitArgs &a, hipStream_t stream);
 template <typename T>
 void launch_conv_grad_typed(int width, const ConvGradArgs &a, int most, float *dweight, float *dbias, float *dA_log, float *ddt_bias,
                             hipStream_t stream);                                            // kvb_conv_grad_*.hip
