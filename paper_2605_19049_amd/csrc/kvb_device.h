@@ -10,6 +10,8 @@
 //   kvb_scan_device.h    whole sequences: kvb_scan_kernel.h (kvb_scan_prep_kernel, kvb_scan_kernel), kvb_scan_token_kernel.h,
 //                        kvb_scan_grad_kernel.h (kvb_scan_reverse_kernel, kvb_scan_grad_kernel); instantiated by kvb_scan_*.hip
 //   kvb_accept.hip       kvb_accept_row_kernel, kvb_accept_sum_kernel, kvb_accept_find_kernel
+//   kvb_layer_device.h   around the recurrence: kvb_conv.hip, kvb_conv_grad_kernel.h (instantiated by kvb_conv_grad_*.hip), kvb_norm.hip,
+//                        kvb_norm_grad.hip, kvb_clip.hip
 //   kvb_api.hip          argument checks, the extern "C" entry points, the kernel timer
 //
 // Element types (Sec. 4.1: 16-bit vectors and records beside a fp32 state): TIn is the type of
