@@ -504,7 +504,7 @@ int kvb_norm_backward(const kvb_rows *rows, const void *x, const void *gate, con
 
 #define KVB_LIST_BLOCK 16384
 
-typedef struct kvb_list {       /* some tensors; all arrays are on the device                                        */
+typedef struct kvb_list {       /* some tensors, none of which share memory; all arrays are on the device            */
     void *const   *data;        /* [n] addresses, each aligned to its elements                                       */
     const int64_t *size;        /* [n] elements, 0 is fine                                                           */
     const int32_t *type;        /* [n] KVB_F32, KVB_BF16 or KVB_F16                                                  */

@@ -384,6 +384,14 @@ def _check_conv(names, sh, ta, sq, args):
             _check_packed(what, x)
 
 
+def _check_apart(li, to):
+    """No tensor of one TensorList shares memory with another than its own of the other"""
+    every = sorted([(*span, 0) for span in li.spans] + [(*span, 1) for span in to.spans])
+    for a, b in zip(every, every[1:]):   # (those of one list are apart: an overlap is one of neighbours)
+        if b[0] < a[1] and a[:3] != b[:3]:
+            raise ValueError("kvb_clip: tensor %d shares memory with another one's source or result" % a[2])
+
+
 def _check_norm(names, ro, args):
     said = {"x": ro.x_stride, "dx": ro.x_stride, "gate": ro.gate_stride, "dgate": ro.gate_stride}
     for what, x in zip(names, args):
@@ -401,8 +409,10 @@ def _check_layouts(fn_name, args):
         _check_conv(_CONV_NAMES[fn_name], args[0], args[1], args[2] if seqs_too else None, args[3 if seqs_too else 2:])
     elif fn_name == "kvb_clip":
         li, to = getattr(args[0], "of", None), getattr(args[1], "of", None)
-        if li is not None and to is not None and (li.sizes, li.types) != (to.sizes, to.types):
-            raise ValueError("kvb_clip: tensors of other sizes or types than those they are made from")
+        if li is not None and to is not None and li is not to:
+            if (li.sizes, li.types) != (to.sizes, to.types):
+                raise ValueError("kvb_clip: tensors of other sizes or types than those they are made from")
+            _check_apart(li, to)
     elif fn_name == "kvb_norm":
         _check_norm(_NORM, args[0], args[1:])
     elif fn_name == "kvb_norm_backward":
@@ -544,6 +554,11 @@ class TensorList:
             if t.dtype not in codes:
                 raise ValueError("a tensor of %s: float32, bfloat16 and float16 are wanted" % t.dtype)
             _check_packed("a tensor", t)
+        # by address: (first byte, behind the last one, number)
+        self.spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i) for i, t in enumerate(self.tensors) if t.numel())
+        for a, b in zip(self.spans, self.spans[1:]):
+            if b[0] < a[1]:
+                raise ValueError("tensors %d and %d share memory" % (a[2], b[2]))
         where = {t.device for t in self.tensors}
         if len(where) > 1:
             raise ValueError("tensors on several devices: %s" % sorted(map(str, where)))

@@ -223,6 +223,23 @@ def test_tensor_lists():
             kvb.TensorList([torch.zeros(2), bad])
 
 
+def test_tensors_that_share_memory():
+    """The same tensor twice would count twice and be cut twice"""
+    flat = torch.zeros(100)
+    for bad in ([flat, flat], [flat[:50], flat[49:]], [flat, torch.zeros(3), flat[10:20]]):
+        with pytest.raises(ValueError, match="share memory"):
+            kvb.TensorList(bad)
+    kvb.TensorList([flat[:50], flat[50:], flat[10:10], flat[20:20]])   # parts, and parts of nothing
+    li = kvb.TensorList([flat[:50], flat[50:]])
+    fine, moved, swapped = kvb.TensorList([flat[:50], torch.zeros(50)]), kvb.TensorList([torch.zeros(50), flat[10:60]]), kvb.TensorList([flat[50:], flat[:50]])
+    kvb.bind("kvb_clip", li.c(), fine.c(), A, 1.0, 0)
+    kvb.bind("kvb_clip", li.c(), li.c(), A, 1.0, 0)
+    kvb.bind("kvb_clip", li.c(), kvb.TensorList([flat[:50], flat[50:]]).c(), A, 1.0, 0)
+    for to in (moved, swapped):
+        with pytest.raises(ValueError, match="shares memory"):
+            kvb.bind("kvb_clip", li.c(), to.c(), A, 1.0, 0)
+
+
 def test_layouts():
     """Tensors that do not lie as the structs say are refused by name; those that do go through to the library (which refuses B = -1)"""
     N, Hk, Hv, d = 6, 2, 4, 64
