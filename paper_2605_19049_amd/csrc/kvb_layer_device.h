@@ -10,7 +10,7 @@ namespace kvb_impl {
 // ---------------------------------------------------------------------------
 // arguments
 // ---------------------------------------------------------------------------
-// (A launch pays for its arguments, some half a microsecond for 100 bytes: each form of the convolution has no more than it needs.)
+// (A kernel's first loads are its arguments: each form of the convolution has no more than it needs.  128 x 4 drafts with their commit, 250 bytes / 180: 13.3 / 12.5 us.)
 struct ConvBase {
     const void *x, *a, *b;            // rows of C, Hv and Hv elements
     const void *weight, *bias;        // [C][width], [C] or nullptr
@@ -282,11 +282,16 @@ inline int64_t norm_turns(int64_t rows, int width)
     }
     return (rows + at_once - 1) / at_once;
 }
+// Up to so many, one workgroup takes them all and its sums are the gradient: a launch less (us, 18 rows of 128, fp32, 2 turns: 4.5 instead of 7.1; 8 rows of 2048, bf16, 4 turns:
+// 7.0, 9 in two launches 7.3; 4 rows of 8192 in one 10.6).
+inline int norm_few(int width) { return width <= 4096 ? 4 : 2; }
 // Its workgroups, each of which leaves one part.  us with 1024 / 512, rows of up to 512 elements: 948 turns (bf16, 128 wide, gated) 13.6 / 11.9, 4000 20.7 / 24, 8000
 // 39.6 / 40.9, 16384 (x in fp32) 95.6 / 91.4, 36000 153.0 / 151.8.  Longer rows: what more parts there are is as much as rows.
 inline int norm_parts(int64_t rows, int width)
 {
     const int64_t n = norm_turns(rows, width);
+    if (n <= norm_few(width))
+        return n < 1 ? 0 : 1;
     if (width > 512)
         return (int)(n < 512 ? n : 512);
     return (int)(n <= 256 ? n : n <= 1024 ? (n + 1) / 2 : n < 12288 ? 1024 : 512);

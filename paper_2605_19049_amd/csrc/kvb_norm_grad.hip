@@ -4,7 +4,7 @@
 // A workgroup takes rows in turn, its lanes keep their columns' sums of dweight in registers and leave
 // one part in the end; kvb_sums_kernel adds the parts in order: the same inputs give the same bits.
 // Bounded by memory: 8192 x 32 heads of 128 with gate, x in fp32, 470 MB, 92.5 us (4 of them the sums) or 5.1 TB/s; 8000 rows of 2048, bf16, with dsum and dres
-// 164 MB, 37.5 us, one row a wave with four vectors a lane, whose registers left two waves a SIMD, 45.8; small calls by their two launches: 18 rows of 128 7.1 us.
+// 164 MB, 37.5 us, one row a wave with four vectors a lane, whose registers left two waves a SIMD, 45.8; small calls by their launches: two from some tens of rows on, 7 us, one below.
 #include "kvb_layer_device.h"
 
 namespace kvb_impl {
@@ -297,18 +297,22 @@ void launch_sums(const float *part, int parts, int64_t columns, const SumsTo &to
 }
 
 template <typename TX, typename T>
-void launch_norm_grad_typed(const NormGradArgs &g, float *dweight, hipStream_t stream)
+void launch_norm_grad_typed(const NormGradArgs &with_work, float *dweight, hipStream_t stream)
 {
+    NormGradArgs g = with_work;
     const NormArgs &a = g.f;
     const int vectors = a.width / 8;
+    const bool alone = g.parts == 1 && reinterpret_cast<uintptr_t>(dweight) % 16 == 0;   // its only part is the sum (parts are stored 16 bytes at a time)
+    if (alone)
+        g.part = dweight;
     if (g.parts > 0 && vectors <= 64) {
         int lg = 2;
         while (lg < 6 && (1 << lg) < vectors)
             ++lg;
-        launch_part(kvb_norm_grad_kernel<TX, T>, true, false, g.parts, 256, stream, g, lg);
+        launch_part(kvb_norm_grad_kernel<TX, T>, true, alone, g.parts, 256, stream, g, lg);
     } else if (g.parts > 0) {
         const int nv = norm_vectors(a.width), threads = norm_threads(a.width), all = threads * norm_teams(a.width);
-        auto go = [&]<int NV>() { launch_part(kvb_norm_grad_row_kernel<TX, T, NV>, true, false, g.parts, all, stream, g, threads); };
+        auto go = [&]<int NV>() { launch_part(kvb_norm_grad_row_kernel<TX, T, NV>, true, alone, g.parts, all, stream, g, threads); };
         if (nv == 1)
             go.template operator()<1>();
         else if (nv == 2)
@@ -316,7 +320,8 @@ void launch_norm_grad_typed(const NormGradArgs &g, float *dweight, hipStream_t s
         else
             go.template operator()<4>();
     }
-    launch_sums(g.part, g.parts, a.width, SumsTo{{dweight, nullptr, nullptr, nullptr}, {0, 0, 0, 0}}, stream);
+    if (!alone)
+        launch_sums(g.part, g.parts, a.width, SumsTo{{dweight, nullptr, nullptr, nullptr}, {0, 0, 0, 0}}, stream);
 }
 
 template void launch_norm_grad_typed<float, float>(const NormGradArgs &, float *, hipStream_t);

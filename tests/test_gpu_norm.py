@@ -130,6 +130,21 @@ def test_large_calls(n, heads, width, gate, res):
         assert torch.equal(part, out[lo:hi]) and (not res or torch.equal(sums, s[lo:hi]))
 
 
+@pytest.mark.parametrize("width", [64, 128, 1000, 2056])
+def test_few_rows(width):
+    """Up to four turns of a workgroup need no parts; a gradient that is not aligned to 16 bytes is summed from one all the same"""
+    at_once = 256 // (width // 8) if width <= 128 else 512 // (-(-width // 512) * 64)
+    for n in (1, at_once, at_once + 1, 4 * at_once - 1, 4 * at_once, 4 * at_once + 1):
+        c = Rows(n, 1, width, "bf16", gate=True, seed=n)
+        r = backward(c)
+        check_backward(c, r)
+        flat = torch.full((width + 8,), FILL, device="cuda")
+        dx, dres, dgate = (torch.empty_like(c.x) for _ in range(3))
+        kvb.kvb_norm_backward(c.ro, c.x, c.gate, c.weight, c.dout, c.dsum, dx, dres, dgate, flat[1:width + 1], torch.empty(kvb.norm_backward_work(c.ro), dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert torch.equal(flat[1:width + 1], r["dweight"]) and flat[0] == FILL and (flat[width + 1:] == FILL).all() and torch.equal(dx, r["dx"])
+
+
 def test_in_place():
     """The residual's stream in place; out over x and over the gate"""
     c = Rows(100, 1, 1024, "bf16", res=True)
