@@ -325,7 +325,8 @@ int64_t conv_columns(const ConvArgs &r, int width) { return (int64_t)(width + (r
 int64_t conv_grad_work_bytes(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
 {
     const int64_t C = conv_channels(sh), columns = (ta->width + 1) * C + 2 * sh->Hv;
-    return 4 * columns * conv_most_parts(sq->n_tokens, sh->B, conv_groups((int)C));
+    const bool wide = sh->in_dtype == KVB_F32;
+    return 4 * columns * conv_most_parts(sq->n_tokens, sh->B, grad_groups((int)C, wide ? GRAD_CHANNELS<float> : GRAD_CHANNELS<bf16_t>), wide);
 }
 
 int check_rows(const kvb_rows *ro)
@@ -460,7 +461,8 @@ int kvb_conv_backward(const kvb_shape *shape, const kvb_taps *taps, const kvb_se
     conv_seqs(r.f, seqs);
     r.f.gates = gates;
     r.dq = dq, r.dk = dk, r.dv = dv, r.dg = dg, r.dbeta = dbeta, r.dstate1 = dstate1, r.dx = dx, r.da = da, r.db = db, r.dstate0 = dstate0;
-    const ConvParts parts = conv_parts(seqs->n_tokens, shape->B, conv_groups(r.f.C) + gates);
+    const bool wide = shape->in_dtype == KVB_F32;
+    const ConvParts parts = conv_parts(seqs->n_tokens, shape->B, grad_groups(r.f.C, wide ? GRAD_CHANNELS<float> : GRAD_CHANNELS<bf16_t>) + gates, wide);
     r.part = static_cast<float *>(work), r.parts = parts.parts, r.each = parts.each, r.columns = (int)conv_columns(r.f, taps->width);
     g_launch_status = hipSuccess;
     hipStream_t hs = static_cast<hipStream_t>(stream);

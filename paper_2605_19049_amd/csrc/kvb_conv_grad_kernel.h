@@ -2,14 +2,15 @@
 //     dy = r (dn - r^2 y (y.dn)) for q and k, dn for v          dz = dy (s + y (1 - s))
 //     dE_e = sum_i w_i dz_{e-i}                                 dw_i = sum_t dz_t E_{t+i},  dbias = sum_t dz_t
 //     da = -exp(A_log) dg / (1 + exp(-(a + dt_bias))),  db = dbeta beta (1 - beta),  dA_log = sum dg g,  ddt_bias = sum da
-// A wave walks forward over a piece's tokens of 512 channels and W - 1 more (whose dz its last inputs need), the last W inputs and dz in registers.
+// A wave walks forward over a piece's tokens of 512 channels (fp32: 256) and W - 1 more (whose dz its last inputs need), the last W inputs and dz in registers.
 // E's rows ahead of the first input are the state's: their gradient is dstate0; the last W - 1 rows get dstate1 as well.  Sums over tokens stay
 // in registers, then the four waves of a workgroup add theirs in LDS and leave one part; kvb_sums_kernel adds the parts in order, so
 // the same inputs give the same bits.
-// Bounded by memory and the vector units about alike: 4 x 2048 tokens, 16 + 32 heads of 128, bf16, 408 MB (a copy: 80 us) take 97 us, 5 of them the sums; the vector units are
-// busy 64 of them (counters: 32.6 M instructions), with two waves a SIMD (216 registers), so what counts is that all of those have as much to do: pieces as
-// long as fill the card once (three rounds of shorter ones took 136), and the groups of q and k, which have norms, on one compute unit with
-// those of v, which do not (group by group in the launch: 97, piece by piece: 106).
+// Bounded by memory: 4 x 2048 tokens, 16 + 32 heads of 128, bf16, 408 MB (a copy: 80 us) take 97 us, 5 of them the sums and some 6 the launch and what stands ahead of a piece's first
+// token.  The vector units are busy 64 of them (counters: 32.6 M instructions; without norms the call takes 96), with two waves a SIMD (216 registers), so what counts is that all
+// of those have as much to do: pieces as long as fill the card once (three rounds of shorter ones took 136), and the groups of q and k on one compute
+// unit with those of v (group by group in the launch: 97, piece by piece: 106).  Calls of some hundred tokens: the chain of launch, start, slot, inputs, then half a
+// microsecond a token.
 #ifndef KVB_CONV_GRAD_KERNEL_H
 #define KVB_CONV_GRAD_KERNEL_H
 
@@ -41,10 +42,10 @@ template <typename T, int W, bool BIAS>
 __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g, int most)
 {
     constexpr int AHEAD = 2;   // tokens asked for ahead (4: 98.5 us instead of 97.0, for the registers)
-    constexpr int PLANE = CONV_LANES;
+    constexpr int V = GRAD_CHANNELS<T>, PLANE = 64 * V;
     __shared__ float sums[4][(W + BIAS) * PLANE];
     const ConvArgs &a = g.f;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = grad_groups(a.C, V);
     const int group = blockIdx.x / g.parts, part = blockIdx.x - group * g.parts;
     float *to = g.part + (int64_t)part * g.columns;
 
@@ -75,24 +76,24 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
         return;
     }
 
-    const int own_ch = group * CONV_LANES + lane * 8;
+    const int own_ch = group * PLANE + lane * V;
     const bool active = own_ch < a.C;
-    const int ch = active ? own_ch : 0, nq = a.Hk * a.d, lgh = a.d == 128 ? 4 : a.d == 64 ? 3 : 2;
-    float w[W][8], bias[8] = {}, dw[W][8] = {}, dbias[8] = {};
+    const int ch = active ? own_ch : 0, nq = a.Hk * a.d, lgh = (a.d == 128 ? 4 : a.d == 64 ? 3 : 2) + (V == 4);
+    float w[W][V], bias[V] = {}, dw[W][V] = {}, dbias[V] = {};
     {
         const T *wp = static_cast<const T *>(a.weight) + (int64_t)ch * W;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            float y[8];
-            unpack8(load_raw8(wp + 8 * i), y);
+            float y[V];
+            unpack(load_raw<V>(wp + V * i), y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                w[(8 * i + j) % W][(8 * i + j) / W] = y[j];
+            for (int j = 0; j < V; ++j)
+                w[(V * i + j) % W][(V * i + j) / W] = y[j];
         }
         if constexpr (BIAS)
-            unpack8(load_raw8(static_cast<const T *>(a.bias) + ch), bias);
+            unpack(load_raw<V>(static_cast<const T *>(a.bias) + ch), bias);
     }
-    const bool unit = a.unit && ch < 2 * nq, any_unit = a.unit && group * CONV_LANES < 2 * nq;   // of the lane; of some lane of the wave
+    const bool unit = a.unit && ch < 2 * nq, any_unit = a.unit && group * PLANE < 2 * nq;   // of the lane; of some lane of the wave
     const T *dn_first = ch < nq ? static_cast<const T *>(g.dq) + ch : ch < 2 * nq ? static_cast<const T *>(g.dk) + (ch - nq) : static_cast<const T *>(g.dv) + (ch - 2 * nq);
     const int64_t dn_stride = ch < nq ? a.q_stride : ch < 2 * nq ? a.k_stride : a.v_stride;
 
@@ -107,24 +108,24 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
         const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + state_at : nullptr, *ds1 = g.dstate1 ? static_cast<const T *>(g.dstate1) + state_at : nullptr;
         T *ds0 = g.dstate0 ? static_cast<T *>(g.dstate0) + state_at : nullptr;
         const int end = p.t1 + W - 1, known = min(end, p.len);   // dz behind the sequence's end is zero
-        float e[4][8], dz[4][8] = {};   // row t + W - 1 of E, and dz_t, at t % 4
+        float e[4][V], dz[4][V] = {};   // row t + W - 1 of E, and dz_t, at t % 4
 #pragma unroll
         for (int i = 0; i < W - 1; ++i) {
             const int at = p.t0 + i;   // of E: token at - (W - 1)
-            Raw8<T> r{};
+            decltype(load_raw<V>(x)) r{};
             if (at >= W - 1)
-                r = load_raw8(x + (int64_t)(at - (W - 1)) * a.x_stride);
+                r = load_raw<V>(x + (int64_t)(at - (W - 1)) * a.x_stride);
             else if (s0)
-                r = load_raw8(s0 + (int64_t)at * a.C);
-            unpack8(r, e[(i + 4 - (W - 1)) % 4]);
+                r = load_raw<V>(s0 + (int64_t)at * a.C);
+            unpack(r, e[(i + 4 - (W - 1)) % 4]);
         }
-        Raw8<T> rx[AHEAD], rn[AHEAD];
+        decltype(load_raw<V>(x)) rx[AHEAD], rn[AHEAD];
         if (known > 0)
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const int64_t t = min(p.t0 + u, known - 1);
-                rx[u] = load_raw8(x + t * a.x_stride);
-                rn[u] = load_raw8(dn + t * dn_stride);
+                rx[u] = load_raw<V>(x + t * a.x_stride);
+                rn[u] = load_raw<V>(dn + t * dn_stride);
             }
         for (int t4 = p.t0; t4 < end; t4 += 4)
             static_for<4>([&](auto U) {
@@ -133,16 +134,16 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
                 if (t >= end)
                     return;
                 if (t < known) {
-                    float d[8], z[8], s[8], sq = 0.0f, dot = 0.0f;
-                    unpack8(rx[u % AHEAD], e[u]);
-                    unpack8(rn[u % AHEAD], d);
+                    float d[V], z[V], s[V], sq = 0.0f, dot = 0.0f;
+                    unpack(rx[u % AHEAD], e[u]);
+                    unpack(rn[u % AHEAD], d);
                     {
                         const int64_t next = min(t + AHEAD, known - 1);
-                        rx[u % AHEAD] = load_raw8(x + next * a.x_stride);
-                        rn[u % AHEAD] = load_raw8(dn + next * dn_stride);
+                        rx[u % AHEAD] = load_raw<V>(x + next * a.x_stride);
+                        rn[u % AHEAD] = load_raw<V>(dn + next * dn_stride);
                     }
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < V; ++j) {
                         z[j] = bias[j];
 #pragma unroll
                         for (int i = 0; i < W; ++i)
@@ -152,23 +153,23 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
                     }
                     if (any_unit) {
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
+                        for (int j = 0; j < V; ++j) {
                             sq = fmaf(z[j], z[j], sq);
                             dot = fmaf(z[j], d[j], dot);
                         }
-                        sq = sum_to16(sq, lgh);
-                        dot = sum_to16(dot, lgh);
+                        sq = V == 8 ? sum_to16(sq, lgh) : sum_to32(sq, lgh);
+                        dot = V == 8 ? sum_to16(dot, lgh) : sum_to32(dot, lgh);
                         const float r = unit ? __builtin_amdgcn_rsqf(sq + a.eps) : 1.0f, c = unit ? r * dot * r * r : 0.0f;   // (r dot first: for a row of zeros it is 0)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
+                        for (int j = 0; j < V; ++j)
                             d[j] = fmaf(r, d[j], -c * z[j]);   // dy
                     }
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
+                    for (int j = 0; j < V; ++j)
                         dz[u][j] = d[j] * fmaf(z[j], 1.0f - s[j], s[j]);
                     if (t < p.t1)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
+                        for (int j = 0; j < V; ++j) {
                             if constexpr (BIAS)
                                 dbias[j] += dz[u][j];
 #pragma unroll
@@ -177,29 +178,29 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
                         }
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
+                    for (int j = 0; j < V; ++j)
                         dz[u][j] = 0.0f;
                 }
                 if (t >= p.t0 + W - 1 || p.t0 == 0) {   // row t of E
-                    float de[8];
+                    float de[V];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < V; ++j) {
                         de[j] = w[0][j] * dz[u][j];
 #pragma unroll
                         for (int i = 1; i < W; ++i)
                             de[j] = fmaf(w[i][j], dz[(u + 4 - i) % 4][j], de[j]);
                     }
                     if (t >= p.len && ds1) {
-                        float more[8];
-                        unpack8(load_raw8(ds1 + (int64_t)(t - p.len) * a.C), more);
+                        float more[V];
+                        unpack(load_raw<V>(ds1 + (int64_t)(t - p.len) * a.C), more);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j)
+                        for (int j = 0; j < V; ++j)
                             de[j] += more[j];
                     }
                     if (t >= W - 1)
-                        store8(dx + (int64_t)(t - (W - 1)) * a.x_stride, de);
+                        store_values(dx + (int64_t)(t - (W - 1)) * a.x_stride, de);
                     else if (ds0)
-                        store8(ds0 + (int64_t)t * a.C, de);
+                        store_values(ds0 + (int64_t)t * a.C, de);
                 }
             });
     }
@@ -207,14 +208,14 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
 #pragma unroll
     for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            sums[wave][i * PLANE + lane * 8 + j] = dw[i][j];
+        for (int j = 0; j < V; ++j)
+            sums[wave][i * PLANE + lane * V + j] = dw[i][j];
     if constexpr (BIAS)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            sums[wave][W * PLANE + lane * 8 + j] = dbias[j];
+        for (int j = 0; j < V; ++j)
+            sums[wave][W * PLANE + lane * V + j] = dbias[j];
     __syncthreads();
-    const int first = group * CONV_LANES;
+    const int first = group * PLANE;
     for (int i = threadIdx.x; i < (W + BIAS) * PLANE; i += 256) {
         const int plane = i / PLANE, c = first + i % PLANE;
         if (c < a.C)   // (weights lie channel by channel)
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
 template <typename T>
 void launch_conv_grad_typed(int width, const ConvGradArgs &g, int most, float *dweight, float *dbias, float *dA_log, float *ddt_bias, hipStream_t stream)
 {
-    const int64_t blocks = (int64_t)g.parts * (conv_groups(g.f.C) + g.f.gates);
+    const int64_t blocks = (int64_t)g.parts * (grad_groups(g.f.C, GRAD_CHANNELS<T>) + g.f.gates);
     auto go = [&]<int W>() {
         if (g.f.bias)
             launch_part(kvb_conv_grad_kernel<T, W, true>, true, false, blocks, 256, stream, g, most);

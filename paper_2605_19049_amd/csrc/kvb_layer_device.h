@@ -100,6 +100,13 @@ __device__ __forceinline__ float sum_to16(float x, int lg)   // lg 2..4
     const float z = add_lane<0x140>(x);
     return lg > 3 ? z : x;
 }
+__device__ __forceinline__ float sum_to32(float x, int lg)   // lg 3..5
+{
+    x = sum_to16(x, lg < 4 ? lg : 4);
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);   // rows 0, 0, 2, 2 and 1, 1, 3, 3
+    const float y = __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
+    return lg > 4 ? y : x;
+}
 __device__ __forceinline__ float sum_lanes(float x, int lg)   // lg 2..6
 {
     x = sum_to16(x, lg);
@@ -124,6 +131,24 @@ __device__ __forceinline__ Raw8<T> pack8(const float (&x)[8])
     else
         return Raw8<T>{make_uint4(pack_pair<T>(x[0], x[1]), pack_pair<T>(x[2], x[3]), pack_pair<T>(x[4], x[5]), pack_pair<T>(x[6], x[7]))};
 }
+// V elements (8 or 4), raw and converted
+template <int V, typename T>
+__device__ __forceinline__ auto load_raw(const T *p)
+{
+    if constexpr (V == 8)
+        return load_raw8(p);
+    else
+        return load_raw4(p);
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw8<T> &r, float (&o)[8]) { unpack8(r, o); }
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw4<T> &r, float (&o)[4])
+{
+    const float4 x = unpack4(r);
+    o[0] = x.x, o[1] = x.y, o[2] = x.z, o[3] = x.w;
+}
+
 // 8 elements that are not read again: past the caches
 __device__ __forceinline__ Raw8<float> load_raw8_nt(const float *p)
 {
@@ -153,6 +178,11 @@ __device__ __forceinline__ Raw8<T> load_raw8_if(const T *p)
 // STREAM: past them all the same, for what would push out what is read again (kvb_clip).
 template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T *p, const float (&x)[8]) { store_raw8<STREAM, !STREAM>(p, pack8<T>(x)); }
+
+template <typename T>
+__device__ __forceinline__ void store_values(T *p, const float (&x)[8]) { store8(p, x); }
+template <typename T>
+__device__ __forceinline__ void store_values(T *p, const float (&x)[4]) { store4<false, true>(p, make_float4(x[0], x[1], x[2], x[3])); }
 
 // A stretch of up to `most` tokens of a ragged batch, numbered as the chunks of a scan are: those of sequence b start at start[b] / most + b, so that
 // every sequence has one, an empty one too.
@@ -204,6 +234,12 @@ __device__ __forceinline__ float softplus(float y) { return fmaxf(y, 0.0f) + log
 constexpr int CONV_LANES = 512;   // channels of a wave: 8 a lane
 __host__ __device__ constexpr int conv_groups(int C) { return (C + CONV_LANES - 1) / CONV_LANES; }
 
+// kvb_conv_backward: 16 bytes a lane.  us, fp32, 4 / 8 channels a lane: 3 x 2048 tokens, 16 + 32 heads of 128, 135 / 138; 5 x up to 150, 2 + 4 heads of 64, 9.1 / 10.7; 700 tokens,
+// 4 + 8 heads of 128, 12.9 / 14.6; 2 x 6000, 8 + 16 heads, W = 2, 127 / 132 (2 x 5000, 8 + 8 heads, 92 / 86).  bf16: 4 x 2048 tokens 100 / 97, 4 x 4096 185 / 181, 200 x up to 64 88 / 102.
+template <typename T>
+constexpr int GRAD_CHANNELS = 16 / (int)sizeof(T);
+__host__ __device__ constexpr int grad_groups(int C, int channels) { return (C + 64 * channels - 1) / (64 * channels); }
+
 // Sums of columns over `parts` rows, in a fixed order.  Columns from begin[i] on go to to[i], whose last one may be followed by more ranges.
 struct SumsTo {
     float *to[4];
@@ -234,7 +270,8 @@ struct ConvParts {
 // Pieces so long that the workgroups of four of them come out as `rounds` for each compute unit at most, the fewest with which a piece is no longer than `enough`
 // tokens: what starts behind others runs alone, and a short piece pays for its weights and the inputs ahead of it.  units: waves of a piece.
 // us, kvb_conv, 16 + 32 heads of 128, bf16, W = 4, enough 8 / 16: 1000 tokens 11.8 / 11.6, 2000 19.0 / 16.7; 8191 tokens in 4 rounds 66, 5 59.1, 6 59.2, 7 61.3,
-// 9 60.1; fp32, 5284 tokens, W = 3, in 3 80.8, 4 84.4, 6 83.9.  kvb_conv_backward, whose registers let two workgroups share a compute unit: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112.
+// 9 60.1; fp32, 5284 tokens, W = 3, in 3 80.8, 4 84.4, 6 83.9.  kvb_conv_backward, bf16: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112;
+// fp32, 3 x 2048 tokens in 2 147, 3 135, 4 139.
 inline int conv_length(int64_t n_tokens, int64_t B, int units, int rounds, int enough, int64_t up)
 {
     int64_t length = up;
@@ -247,17 +284,19 @@ inline int conv_length(int64_t n_tokens, int64_t B, int units, int rounds, int e
     return (int)(length < CONV_LEAST ? CONV_LEAST : length < up ? length : up);
 }
 inline int conv_most(int64_t n_tokens, int64_t B, int units, bool wide) { return conv_length(n_tokens, B, units, wide ? 3 : 6, 16, 64); }
-inline int64_t conv_part_limit(int units) { return 512 / units < 1 ? 1 : 512 / units; }
-inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units)
+// Those of kvb_conv_backward that fit a compute unit at once: its registers (fp32: of half as many channels) leave each SIMD two waves (three)
+constexpr int grad_rounds(bool wide) { return wide ? 3 : 2; }
+inline int64_t conv_part_limit(int units, bool wide) { return 256 * grad_rounds(wide) / units < 1 ? 1 : 256 * grad_rounds(wide) / units; }
+inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units, bool wide)
 {
-    const int most = conv_length(n_tokens, B, units, 2, 12, INT32_MAX);
-    const int64_t limit = conv_part_limit(units), pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
+    const int most = conv_length(n_tokens, B, units, grad_rounds(wide), 12, INT32_MAX);
+    const int64_t limit = conv_part_limit(units, wide), pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
     return ConvParts{most, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};
 }
 // The most that a call of up to so many tokens and sequences needs
-inline int64_t conv_most_parts(int64_t n_tokens, int64_t B, int units)
+inline int64_t conv_most_parts(int64_t n_tokens, int64_t B, int units, bool wide)
 {
-    const int64_t n = (pieces_of(n_tokens, B, CONV_LEAST) + 3) / 4, limit = conv_part_limit(units);
+    const int64_t n = (pieces_of(n_tokens, B, CONV_LEAST) + 3) / 4, limit = conv_part_limit(units, wide);
     return n < 1 ? 1 : n < limit ? n : limit;
 }
 
