@@ -406,7 +406,8 @@ typedef struct kvb_taps {
  *   q, k, v device, written: [n_tokens, Hk or Hv, dk] in_dtype, strides of seqs
  *   g, beta device, written: [n_tokens, Hv] fp32
  * All arithmetic is fp32, results are rounded once.  What is written must not overlap x, a and b.
- * Rows of skipped sequences (slot outside 0..n_slots-1) are not written.
+ * Rows of skipped sequences (slot outside 0..n_slots-1) are not written.  A call that would take 2^32 threads is refused, here and below: 64 for each sequence (and each 64 tokens of one), token
+ * or draft and 512 channels or the gates.
  */
 int kvb_conv(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs, const void *x, const void *a, const void *b,
              const void *state0, void *state1, void *q, void *k, void *v, float *g, float *beta, void *stream);
@@ -482,7 +483,7 @@ typedef struct kvb_rows {
  *   gate    device [n_tokens, heads, width] dtype, or NULL: none       weight  device [width] dtype
  *   sum     device, written: s, packed, or NULL: not wanted.  Without a residual NULL.  May be res, or x where that lies packed
  *   out     device, written: [n_tokens, heads, width] dtype, packed.  May be x (of the same type) or gate where they lie packed
- * All arithmetic is fp32; squares above the range of fp32 make a row 0.
+ * All arithmetic is fp32; squares above the range of fp32 make a row 0.  Rows above 2048 elements: at most 2^24 - 2, above 8192 half as many.
  */
 int kvb_norm(const kvb_rows *rows, const void *x, const void *res, const void *gate, const void *weight, void *sum, void *out, void *stream);
 
@@ -496,7 +497,7 @@ int kvb_norm(const kvb_rows *rows, const void *x, const void *res, const void *g
  *   dgate    device, written: dtype, lies as gate does; NULL if and only if there is no gate
  *   dweight  device [width] fp32, written
  *   work     device, kvb_norm_backward_work(rows) bytes, 16-byte aligned; means nothing before and after the call.  It grows with n_tokens
- * The same inputs give the same bits.
+ * What is written must not overlap what is read otherwise.  The same inputs give the same bits.
  */
 int64_t kvb_norm_backward_work(const kvb_rows *rows);
 int kvb_norm_backward(const kvb_rows *rows, const void *x, const void *gate, const void *weight, const void *dout, const void *dsum, void *dx,

@@ -246,8 +246,10 @@ int check_taps(const kvb_shape *sh, const kvb_taps *ta)
         return KVB_EINVAL;
     return ta->width >= 2 && ta->width <= 4 ? KVB_OK : KVB_EUNSUPPORTED;
 }
-// Workgroups of four waves, one for each unit
-bool conv_units_fit(const kvb_shape *sh, int64_t tokens) { return tokens <= INT32_MAX / (conv_groups((int)conv_channels(sh)) + 1); }
+// The threads of a launch are counted in 32 bits: 4 waves each that the last workgroup of four may have too many
+constexpr int64_t MOST_WAVES = UINT32_MAX / 64 - 4;
+// A wave for each unit of each of them
+bool conv_units_fit(const kvb_shape *sh, int64_t tokens) { return tokens <= MOST_WAVES / (conv_groups((int)conv_channels(sh)) + 1); }
 
 // The inputs of a convolution's tokens, and whether there are gates
 int check_conv_inputs(const kvb_shape *sh, const kvb_taps *ta, bool tokens, const void *x, const void *a, const void *b, const void *state0)
@@ -289,7 +291,9 @@ int check_conv_seqs(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
     rc = check_seqs(&own, sq);
     if (rc != KVB_OK)
         return rc;
-    return conv_units_fit(sh, pieces_of(sq->n_tokens, sh->B, CONV_LEAST)) ? KVB_OK : KVB_EINVAL;
+    const int each = conv_groups((int)conv_channels(sh)) + 1;
+    const int64_t least = pieces_of(sq->n_tokens, sh->B, CONV_LEAST);   // (of kvb_conv_backward, which has few waves for many of them)
+    return least <= INT32_MAX / each && conv_units_fit(sh, pieces_of(sq->n_tokens, sh->B, conv_most(sq->n_tokens, sh->B, each, sh->in_dtype == KVB_F32))) ? KVB_OK : KVB_EINVAL;
 }
 // T tokens of each of B requests
 int conv_tokens_common(const kvb_shape *sh, const kvb_taps *ta, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent, const void *x,
@@ -488,6 +492,8 @@ int kvb_norm(const kvb_rows *rows, const void *x, const void *res, const void *g
     if (!x || !weight || !out || (!res && (sum || rows->scale != 1.0f)))
         return KVB_EINVAL;
     const NormArgs a = norm_args(rows, x, res, gate, weight, sum, out);
+    if (rows->width > 2048 && a.rows > MOST_WAVES / (rows->width > 8192 ? 8 : 4))   // a workgroup a row
+        return KVB_EINVAL;
     g_launch_status = hipSuccess;
     rc = norm_types(rows, [&]<typename TX, typename T>() { launch_norm_typed<TX, T>(a, static_cast<hipStream_t>(stream)); });
     if (rc != KVB_OK)

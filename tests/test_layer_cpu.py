@@ -106,6 +106,18 @@ def test_sequences():
     assert conv(sh=shape(Hk=1024, Hv=1024), sq=seqs(n_tokens=2 ** 31 - 1)) == kvb.EINVAL   # more units than a launch has
 
 
+def test_calls_that_a_launch_does_not_hold():
+    """2^32 threads: 64 for each 512 channels of a piece, token or draft, and for its gates"""
+    small = dict(Hk=1, Hv=1, dk=32, dv=32)
+    assert conv(sh=shape(B=2 ** 30 - 1, **small), sq=seqs(n_tokens=0)) == kvb.EINVAL
+    assert conv(sh=shape(B=2 ** 25, **small)) == kvb.EINVAL
+    assert decode(sh=shape(B=2 ** 25, **small)) == kvb.EINVAL
+    assert verify(sh=shape(B=2 ** 23, **small)) == kvb.EINVAL
+    assert commit(sh=shape(B=2 ** 25, **small)) == kvb.EINVAL
+    assert norm(ro=rows(n_tokens=2 ** 24, heads=1, width=2056)) == kvb.EINVAL
+    assert norm(ro=rows(n_tokens=2 ** 23, heads=1, width=8200)) == kvb.EINVAL
+
+
 def test_gradients():
     for bad in (dict(x=None), dict(dq=None), dict(dk=A + 8), dict(dv=None), dict(dg=None), dict(dbeta=A + 2), dict(dstate1=A + 8), dict(dx=None), dict(dx=A + 8), dict(da=None),
                 dict(db=None), dict(db=A + 1), dict(dweight=None), dict(dweight=A + 2), dict(dbias=A), dict(dA_log=None), dict(ddt_bias=None), dict(dstate0=A),
