@@ -289,6 +289,8 @@ constexpr int grad_rounds(bool wide) { return wide ? 3 : 2; }
 inline int64_t conv_part_limit(int units, bool wide) { return 256 * grad_rounds(wide) / units < 1 ? 1 : 256 * grad_rounds(wide) / units; }
 inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units, bool wide)
 {
+    if (B == 0)   // (tokens of nobody)
+        return ConvParts{CONV_LEAST, 0, 1};
     const int most = conv_length(n_tokens, B, units, grad_rounds(wide), 12, INT32_MAX);
     const int64_t limit = conv_part_limit(units, wide), pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
     return ConvParts{most, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};

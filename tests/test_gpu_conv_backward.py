@@ -125,6 +125,17 @@ def test_no_tokens():
     assert all((r[n] == 0).all() for n in ("dweight", "dbias", "dA_log", "ddt_bias"))
 
 
+def test_tokens_of_nobody():
+    c = Case([5, 8], 1, 2, 32, 3, "f32", bias=True)
+    d = grads_of(c)
+    c.sh, c.start = kvb.shape(0, c.Hk, c.Hv, c.d, c.d, 1, kvb.F32), c.start[:1]
+    r = backward(c, d)
+    for name in ("dweight", "dbias", "dA_log", "ddt_bias"):
+        assert (r[name] == 0).all(), name
+    for name in ("dx", "da", "db", "dstate0"):
+        assert (r[name] == FILL).all(), name
+
+
 def test_a_wave_takes_several_short_sequences():
     """More sequences than waves: 300, 224 waves for each 512 channels"""
     c = Case([(b * 5 + b // 7) % 5 for b in range(300)], 8, 16, 128, 4, "bf16", seed=7, bias=True)
