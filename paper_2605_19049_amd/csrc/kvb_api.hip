@@ -291,9 +291,7 @@ int check_conv_seqs(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
     rc = check_seqs(&own, sq);
     if (rc != KVB_OK)
         return rc;
-    const int each = conv_groups((int)conv_channels(sh)) + 1;
-    const int64_t least = pieces_of(sq->n_tokens, sh->B, CONV_LEAST);   // (of kvb_conv_backward, which has few waves for many of them)
-    return least <= INT32_MAX / each && conv_units_fit(sh, pieces_of(sq->n_tokens, sh->B, conv_most(sq->n_tokens, sh->B, each, sh->in_dtype == KVB_F32))) ? KVB_OK : KVB_EINVAL;
+    return conv_units_fit(sh, conv_deal(sq->n_tokens, sh->B, conv_groups((int)conv_channels(sh)) + 1, sh->in_dtype == KVB_F32).stretches) ? KVB_OK : KVB_EINVAL;
 }
 // T tokens of each of B requests
 int conv_tokens_common(const kvb_shape *sh, const kvb_taps *ta, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent, const void *x,
@@ -467,15 +465,15 @@ int kvb_conv_backward(const kvb_shape *shape, const kvb_taps *taps, const kvb_se
     r.dq = dq, r.dk = dk, r.dv = dv, r.dg = dg, r.dbeta = dbeta, r.dstate1 = dstate1, r.dx = dx, r.da = da, r.db = db, r.dstate0 = dstate0;
     const bool wide = shape->in_dtype == KVB_F32;
     const ConvParts parts = conv_parts(seqs->n_tokens, shape->B, grad_groups(r.f.C, wide ? GRAD_CHANNELS<float> : GRAD_CHANNELS<bf16_t>) + gates, wide);
-    r.part = static_cast<float *>(work), r.parts = parts.parts, r.each = parts.each, r.columns = (int)conv_columns(r.f, taps->width);
+    r.part = static_cast<float *>(work), r.parts = parts.parts, r.columns = (int)conv_columns(r.f, taps->width);
     g_launch_status = hipSuccess;
     hipStream_t hs = static_cast<hipStream_t>(stream);
     if (shape->in_dtype == KVB_F32)
-        launch_conv_grad_typed<float>(taps->width, r, parts.most, dweight, dbias, dA_log, ddt_bias, hs);
+        launch_conv_grad_typed<float>(taps->width, r, parts.length, dweight, dbias, dA_log, ddt_bias, hs);
     else if (shape->in_dtype == KVB_BF16)
-        launch_conv_grad_typed<bf16_t>(taps->width, r, parts.most, dweight, dbias, dA_log, ddt_bias, hs);
+        launch_conv_grad_typed<bf16_t>(taps->width, r, parts.length, dweight, dbias, dA_log, ddt_bias, hs);
     else
-        launch_conv_grad_typed<f16_t>(taps->width, r, parts.most, dweight, dbias, dA_log, ddt_bias, hs);
+        launch_conv_grad_typed<f16_t>(taps->width, r, parts.length, dweight, dbias, dA_log, ddt_bias, hs);
     return finish_launch();
 }
 

@@ -6,7 +6,7 @@
 // stays inside a row of 16.  A wave has 512 channels; the units behind the channels' are the gates'.  All arithmetic is fp32; what is rounded
 // is the result, once, to its own type.
 // Bounded by memory: 8191 tokens, 16 + 32 heads of 128, bf16, 272 MB in 59 us or 4.6 TB/s (a copy: 5.0 .. 5.2), of which the vector units are busy some 40: 130
-// instructions for a token's 8 channels, two of them slow (exp2, rcp).  Small calls are bounded by the chain launch, start, slot, inputs: a prompt of 37 tokens 4.9 us, a
+// instructions for a token's 8 channels, two of them slow (exp2, rcp).  Small calls are bounded by the chain launch, start, slot, inputs: a prompt of 37 tokens 4.6 us, a
 // single token 3.8, 64 of them 4.0, 512 11.6 (67 MB, 5.8 TB/s, some of it from the last level).
 #include "kvb_layer_device.h"
 
@@ -85,9 +85,9 @@ __device__ __forceinline__ void gates_of(const ConvBase &a, int64_t t0, int n, i
 
 }  // namespace
 
-// Whole sequences: a wave takes up to `most` tokens of one of them, with the taps' inputs in registers.
+// Whole sequences: a wave takes the tokens of `length` places one after the other, with the taps' inputs in registers.
 template <typename T, int W, bool STREAM>
-__global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int units, int most)
+__global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int units, int64_t length)
 {
     constexpr int U = 4;   // tokens at a time
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
@@ -95,78 +95,87 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
     if (unit >= units)
         return;
     const int w = unit / each, group = unit - w * each;
-    const Piece p = piece_at(a.start, a.n_tokens, a.B, w, most);
-    const int row = state_row(a.slot, a.n_slots, p.b);
-    if (!p.some || row < 0)
-        return;
+    const int64_t from = w * length;
+    Shares shares(a, from, from + length, W - 1);
     if (group == groups) {
-        gates_of<T>(a, (int64_t)p.first + p.t0, p.t1 - p.t0, lane);
+        while (shares.more()) {
+            const Share p = shares.take();
+            if (p.some)
+                gates_of<T>(a, (int64_t)p.first + p.t0, p.t1 - p.t0, lane);
+        }
         return;
     }
     const int ch = group * CONV_LANES + lane * 8;
     if (ch >= a.C)
         return;
-    const T *x = static_cast<const T *>(a.x) + (int64_t)p.first * a.x_stride + ch;
-    const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + (int64_t)row * (W - 1) * a.C + ch : nullptr;
-    auto input_at = [&](int e) {   // row e of E
-        if (e >= W - 1)
-            return load_raw8(x + (int64_t)(e - (W - 1)) * a.x_stride);
-        return s0 ? load_raw8(s0 + (int64_t)e * a.C) : Raw8<T>{};
-    };
-    if (p.t0 < p.t1) {
-        Raw8<T> raw[U], before[W - 1];
-#pragma unroll
-        for (int i = 0; i < W - 1; ++i)
-            before[i] = input_at(p.t0 + i);
-        auto request = [&](int t) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                raw[u] = load_raw8_if<STREAM>(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
+    while (shares.more()) {
+        const Share p = shares.take();
+        if (!p.some)
+            continue;
+        const T *x = static_cast<const T *>(a.x) + (int64_t)p.first * a.x_stride + ch;
+        const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + (int64_t)p.row * (W - 1) * a.C + ch : nullptr;
+        auto input_at = [&](int e) {   // row e of E
+            if (e >= W - 1)
+                return load_raw8(x + (int64_t)(e - (W - 1)) * a.x_stride);
+            return s0 ? load_raw8(s0 + (int64_t)e * a.C) : Raw8<T>{};
         };
-        request(p.t0);
-        const Lane8<T, W> l(a, ch, a.q_stride, a.k_stride, a.v_stride);
-        float e[W - 1 + U][8];
-#pragma unroll
-        for (int i = 0; i < W - 1; ++i)
-            unpack8(before[i], e[i]);
-        for (int t = p.t0; t < p.t1; t += U) {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                unpack8(raw[u], e[W - 1 + u]);
-            if (t + U < p.t1)
-                request(t + U);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (t + u < p.t1) {
-                    float z[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        z[j] = l.bias[j];
-#pragma unroll
-                        for (int i = 0; i < W; ++i)
-                            z[j] = fmaf(l.w[i][j], e[u + i][j], z[j]);
-                    }
-                    l.finish(z);
-                    store8(l.to + ((int64_t)p.first + t + u) * l.to_stride, z);
-                }
-            }
+        if (p.t0 < p.t1) {
+            Raw8<T> raw[U], before[W - 1];
 #pragma unroll
             for (int i = 0; i < W - 1; ++i)
+                before[i] = input_at(p.t0 + i);
+            auto request = [&](int t) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    e[i][j] = e[U + i][j];
+                for (int u = 0; u < U; ++u)
+                    raw[u] = load_raw8_if<STREAM>(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
+            };
+            request(p.t0);
+            const Lane8<T, W> l(a, ch, a.q_stride, a.k_stride, a.v_stride);
+            T *out = l.to + ((int64_t)p.first + p.t0) * l.to_stride;
+            float e[W - 1 + U][8];
+#pragma unroll
+            for (int i = 0; i < W - 1; ++i)
+                unpack8(before[i], e[i]);
+            for (int t = p.t0; t < p.t1; t += U) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    unpack8(raw[u], e[W - 1 + u]);
+                if (t + U < p.t1)
+                    request(t + U);
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (t + u < p.t1) {
+                        float z[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            z[j] = l.bias[j];
+#pragma unroll
+                            for (int i = 0; i < W; ++i)
+                                z[j] = fmaf(l.w[i][j], e[u + i][j], z[j]);
+                        }
+                        l.finish(z);
+                        store8(out, z);
+                        out += l.to_stride;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < W - 1; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        e[i][j] = e[U + i][j];
+            }
         }
-    }
-    // The first piece's wave writes the last state: nobody else reads the first one's rows, which it may lie in.
-    if (p.t0 == 0 && a.state1) {
-        T *s1 = static_cast<T *>(a.state1) + (int64_t)row * (W - 1) * a.C + ch;
-        Raw8<T> last[W - 1];
+        // Who has the first token writes the last state: nobody else reads the first one's rows, which it may lie in.
+        if (p.t0 == 0 && a.state1) {
+            T *s1 = static_cast<T *>(a.state1) + (int64_t)p.row * (W - 1) * a.C + ch;
+            Raw8<T> last[W - 1];
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i)
-            last[i] = input_at(p.len + i);
+            for (int i = 0; i < W - 1; ++i)
+                last[i] = input_at(p.len + i);
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i)
-            store_raw8<false, true>(s1 + (int64_t)i * a.C, last[i]);
+            for (int i = 0; i < W - 1; ++i)
+                store_raw8<false, true>(s1 + (int64_t)i * a.C, last[i]);
+        }
     }
 }
 
@@ -337,15 +346,17 @@ void with_taps(int dtype, int width, F &&f)
 
 void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 {
-    const int each = conv_groups(a.C) + a.gates, most = conv_most(a.n_tokens, a.B, each, dtype == KVB_F32), units = (int)(pieces_of(a.n_tokens, a.B, most) * each);
+    const int each = conv_groups(a.C) + a.gates;
+    const ConvDeal deal = conv_deal(a.n_tokens, a.B, each, dtype == KVB_F32);
+    const int units = (int)(deal.stretches * each);
     // x past the caches where it and what is made from it fill half of the last level: what reads the results next finds more of them there.  us with the
     // kvb_scan behind it, plain / past them: 300 tokens 38.2 / 38.9, 1024 84.7 / 85.2, 4096 (64 MiB) 286.3 / 286.0, 8191 576 / 571, 24 sequences of 750 562 / 558.
     const bool stream_x = (int64_t)a.n_tokens * a.C * (dtype == KVB_F32 ? 4 : 2) > 64 << 20;
     with_taps(dtype, width, [&]<typename T, int W>() {
         if (stream_x)
-            launch_part(kvb_conv_kernel<T, W, true>, true, true, (units + 3) / 4, 256, stream, a, units, most);
+            launch_part(kvb_conv_kernel<T, W, true>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
         else
-            launch_part(kvb_conv_kernel<T, W, false>, true, true, (units + 3) / 4, 256, stream, a, units, most);
+            launch_part(kvb_conv_kernel<T, W, false>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
     });
 }
 

@@ -3,6 +3,6 @@
 
 namespace kvb_impl {
 
-template void launch_conv_grad_typed<bf16_t>(int, const ConvGradArgs &, int, float *, float *, float *, float *, hipStream_t);
+template void launch_conv_grad_typed<bf16_t>(int, const ConvGradArgs &, int64_t, float *, float *, float *, float *, hipStream_t);
 
 }  // namespace kvb_impl

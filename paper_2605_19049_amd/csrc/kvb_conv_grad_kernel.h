@@ -2,14 +2,14 @@
 //     dy = r (dn - r^2 y (y.dn)) for q and k, dn for v          dz = dy (s + y (1 - s))
 //     dE_e = sum_i w_i dz_{e-i}                                 dw_i = sum_t dz_t E_{t+i},  dbias = sum_t dz_t
 //     da = -exp(A_log) dg / (1 + exp(-(a + dt_bias))),  db = dbeta beta (1 - beta),  dA_log = sum dg g,  ddt_bias = sum da
-// A wave walks forward over a piece's tokens of 512 channels (fp32: 256) and W - 1 more (whose dz its last inputs need), the last W inputs and dz in registers.
+// A wave walks forward over its tokens of 512 channels (fp32: 256) and W - 1 more (whose dz its last inputs need), the last W inputs and dz in registers.
 // E's rows ahead of the first input are the state's: their gradient is dstate0; the last W - 1 rows get dstate1 as well.  Sums over tokens stay
 // in registers, then the four waves of a workgroup add theirs in LDS and leave one part; kvb_sums_kernel adds the parts in order, so
 // the same inputs give the same bits.
-// Bounded by memory: 4 x 2048 tokens, 16 + 32 heads of 128, bf16, 408 MB (a copy: 80 us) take 97 us, 5 of them the sums and some 6 the launch and what stands ahead of a piece's first
+// Bounded by memory: 4 x 2048 tokens, 16 + 32 heads of 128, bf16, 408 MB (a copy: 80 us) take 97 us, 5 of them the sums and some 6 the launch and what stands ahead of a wave's first
 // token.  The vector units are busy 64 of them (counters: 32.6 M instructions; without norms the call takes 96), with two waves a SIMD (216 registers), so what counts is that all
-// of those have as much to do: pieces as long as fill the card once (three rounds of shorter ones took 136), and the groups of q and k on one compute
-// unit with those of v (group by group in the launch: 97, piece by piece: 106).  Calls of some hundred tokens: the chain of launch, start, slot, inputs, then half a
+// of those have as much to do: stretches as long as fill the card once (three rounds of shorter ones took 136), and the groups of q and k on one compute
+// unit with those of v (group by group in the launch: 97, stretch by stretch: 106).  Calls of some hundred tokens: the chain of launch, start, slot, inputs, then half a
 // microsecond a token.
 #ifndef KVB_CONV_GRAD_KERNEL_H
 #define KVB_CONV_GRAD_KERNEL_H
@@ -18,7 +18,7 @@
 
 namespace kvb_impl {
 
-// Gradients of the gates of a piece's tokens; the sums over them in the lanes of the first token
+// Gradients of the gates of some tokens; the sums over them in the lanes of the first token
 template <typename T>
 __device__ __forceinline__ void gate_grads(const ConvGradArgs &g, int64_t t0, int n, int h, const GateLanes &l, float &dA, float &ddt)
 {
@@ -39,7 +39,7 @@ __device__ __forceinline__ void gate_grads(const ConvGradArgs &g, int64_t t0, in
 }
 
 template <typename T, int W, bool BIAS>
-__global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g, int most)
+__global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g, int64_t length)
 {
     constexpr int AHEAD = 2;   // tokens asked for ahead (4: 98.5 us instead of 97.0, for the registers)
     constexpr int V = GRAD_CHANNELS<T>, PLANE = 64 * V;
@@ -48,15 +48,16 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = grad_groups(a.C, V);
     const int group = blockIdx.x / g.parts, part = blockIdx.x - group * g.parts;
     float *to = g.part + (int64_t)part * g.columns;
+    const int64_t from = (part * 4 + wave) * length, behind = from + length;   // the wave's places
 
     if (group == groups) {
         const GateLanes l = gate_lanes(a.Hv, lane);
         for (int h0 = 0; h0 < a.Hv; h0 += l.heads) {
             const int h = h0 + l.head;
             float dA = 0.0f, ddt = 0.0f;
-            for (int i = 0; i < g.each; ++i) {
-                const Piece p = piece_at(a.start, a.n_tokens, a.B, (part * 4 + wave) * g.each + i, most);
-                if (p.t0 < p.t1 && state_row(a.slot, a.n_slots, p.b) >= 0 && h < a.Hv)
+            for (Shares shares(a, from, behind, W - 1); shares.more();) {
+                const Share p = shares.take();
+                if (p.some && p.t0 < p.t1 && h < a.Hv)
                     gate_grads<T>(g, (int64_t)p.first + p.t0, p.t1 - p.t0, h, l, dA, ddt);
             }
             sums[wave][lane] = dA;
@@ -97,14 +98,13 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
     const T *dn_first = ch < nq ? static_cast<const T *>(g.dq) + ch : ch < 2 * nq ? static_cast<const T *>(g.dk) + (ch - nq) : static_cast<const T *>(g.dv) + (ch - 2 * nq);
     const int64_t dn_stride = ch < nq ? a.q_stride : ch < 2 * nq ? a.k_stride : a.v_stride;
 
-    for (int n = 0; n < g.each; ++n) {
-        const Piece p = piece_at(a.start, a.n_tokens, a.B, (part * 4 + wave) * g.each + n, most);
-        const int row = state_row(a.slot, a.n_slots, p.b);
-        if (!p.some || row < 0 || !active)
+    for (Shares shares(a, from, behind, W - 1); shares.more();) {
+        const Share p = shares.take();
+        if (!p.some || !active)
             continue;
         const T *x = static_cast<const T *>(a.x) + (int64_t)p.first * a.x_stride + ch, *dn = dn_first + (int64_t)p.first * dn_stride;
         T *dx = static_cast<T *>(g.dx) + (int64_t)p.first * a.x_stride + ch;
-        const int64_t state_at = (int64_t)row * (W - 1) * a.C + ch;
+        const int64_t state_at = (int64_t)p.row * (W - 1) * a.C + ch;
         const T *s0 = a.state0 ? static_cast<const T *>(a.state0) + state_at : nullptr, *ds1 = g.dstate1 ? static_cast<const T *>(g.dstate1) + state_at : nullptr;
         T *ds0 = g.dstate0 ? static_cast<T *>(g.dstate0) + state_at : nullptr;
         const int end = p.t1 + W - 1, known = min(end, p.len);   // dz behind the sequence's end is zero
@@ -224,14 +224,14 @@ __global__ __launch_bounds__(256) void kvb_conv_grad_kernel(const ConvGradArgs g
 }
 
 template <typename T>
-void launch_conv_grad_typed(int width, const ConvGradArgs &g, int most, float *dweight, float *dbias, float *dA_log, float *ddt_bias, hipStream_t stream)
+void launch_conv_grad_typed(int width, const ConvGradArgs &g, int64_t length, float *dweight, float *dbias, float *dA_log, float *ddt_bias, hipStream_t stream)
 {
     const int64_t blocks = (int64_t)g.parts * (grad_groups(g.f.C, GRAD_CHANNELS<T>) + g.f.gates);
     auto go = [&]<int W>() {
         if (g.f.bias)
-            launch_part(kvb_conv_grad_kernel<T, W, true>, true, false, blocks, 256, stream, g, most);
+            launch_part(kvb_conv_grad_kernel<T, W, true>, true, false, blocks, 256, stream, g, length);
         else
-            launch_part(kvb_conv_grad_kernel<T, W, false>, true, false, blocks, 256, stream, g, most);
+            launch_part(kvb_conv_grad_kernel<T, W, false>, true, false, blocks, 256, stream, g, length);
     };
     if (g.parts == 0) {
     } else if (width == 4)

@@ -1,5 +1,5 @@
 // What the kernels around the recurrence share (kvb_conv.hip, kvb_conv_grad_*.hip, kvb_norm.hip, kvb_norm_grad.hip, kvb_clip.hip): their
-// arguments, sums over neighbouring lanes, pieces of ragged sequences, sums of columns.
+// arguments, sums over neighbouring lanes, shares of ragged sequences, sums of columns.
 #ifndef KVB_LAYER_DEVICE_H
 #define KVB_LAYER_DEVICE_H
 
@@ -52,7 +52,7 @@ struct ConvGradArgs {
     void *dx, *da, *db;               // strides of x, a, b
     void *dstate0;                    // or nullptr: not wanted
     float *part;                      // [parts][columns]
-    int32_t parts, each, columns;     // chunks of a wave; columns of a part: width and bias planes of C, then dA_log and ddt_bias
+    int32_t parts, columns;           // columns of a part: width and bias planes of C, then dA_log and ddt_bias
 };
 
 struct NormArgs {
@@ -184,35 +184,69 @@ __device__ __forceinline__ void store_values(T *p, const float (&x)[8]) { store8
 template <typename T>
 __device__ __forceinline__ void store_values(T *p, const float (&x)[4]) { store4<false, true>(p, make_float4(x[0], x[1], x[2], x[3])); }
 
-// A stretch of up to `most` tokens of a ragged batch, numbered as the chunks of a scan are: those of sequence b start at start[b] / most + b, so that
-// every sequence has one, an empty one too.
-struct Piece {
-    int b, first, len;   // the sequence, its first token, its length
-    int t0, t1;          // the tokens of the piece, counted from there; t0 = t1 in an empty sequence's only one
-    bool some;           // false: there is no piece with this number
-};
-inline int64_t pieces_of(int64_t n_tokens, int64_t B, int most) { return n_tokens / most + B; }
-__device__ __forceinline__ Piece piece_at(const int32_t *start, int n_tokens, int B, int w, int most)   // every lane of the wave calls it
+// A ragged batch laid out by what it costs: sequence b takes the places start[b] + SEQUENCE b up to start[b + 1] + SEQUENCE (b + 1), the first SEQUENCE of them
+// for itself (its bounds, its row of the states and the inputs ahead of it, asked for one after the other), then one a token.  A stretch of
+// these places is a part of one sequence, or whole ones and a part of one at either end; each wave has one.
+// us, against pieces of one sequence each (numbered start[b] / length + b, so that some numbers were nobody's), 1000 sequences of up to 20 tokens, 4 + 8 heads, kvb_conv 34.8 / 31.2,
+// kvb_conv_backward 72.6 / 58.2; 200 of up to 64, 8 + 16 heads, 32.0 / 31.0 and 102.7 / 54.6; 24 of up to 1500, 4 + 8 heads, 36.3 / 36.7; one of 8191, 16 + 32 heads, 58.9 / 58.6;
+// 4 of 2048, backward, 97.2 / 97.4.  SEQUENCE 4 / 6 / 12: backward, 200 sequences 53.1 / 52.9 / 56.6, 4 of 2048 98.3 / 98.3 / 96.4; 24 of up to 1500 37.9 / 37.1.
+constexpr int SEQUENCE = 8;
+inline int64_t places_of(int64_t n_tokens, int64_t B) { return n_tokens + SEQUENCE * B; }
+__device__ __forceinline__ int64_t place_of(const int32_t *start, int n_tokens, int b) { return min(max(start[b], 0), n_tokens) + (int64_t)SEQUENCE * b; }
+// The sequence that has the place, or the one before it
+__device__ __forceinline__ int sequence_at(const int32_t *start, int n_tokens, int B, int64_t place)   // every lane of the wave calls it
 {
-    // the last sequence whose first piece is w or before it: 64 candidates at a time, a 64th of what is left apart, then neighbours
+    // 64 candidates at a time, a 64th of what is left apart, then neighbours
     const int lane = threadIdx.x % 64;
-    auto begins = [&](int b) { return (int)((uint32_t)min(max(start[b], 0), n_tokens) / (uint32_t)most) + b <= w; };
     int b = 0, step = 1;
     while ((int64_t)step * 64 < B)
         step *= 64;
     for (; step > 0; step /= 64) {
         const int64_t at = b + (int64_t)lane * step;   // (lane 0's is known to begin, or is sequence 0)
-        const bool yes = at < B && begins((int)at);
+        const bool yes = at < B && place_of(start, n_tokens, (int)at) <= place;
         b += max((int)__popcll(__ballot(yes)) - 1, 0) * step;
     }
-    b = __builtin_amdgcn_readfirstlane(b);
-    const Span s = span_of(start, n_tokens, b);
-    const int c = w - ((int)((uint32_t)s.first / (uint32_t)most) + b);
-    const int64_t at = (int64_t)c * most;
-    if (c < 0 || (c > 0 && at >= s.len))
-        return Piece{b, s.first, s.len, 0, 0, false};
-    return Piece{b, s.first, s.len, (int)at, (int)min((int64_t)s.len, at + most), true};
+    return __builtin_amdgcn_readfirstlane(b);
 }
+// What some places have of a sequence
+struct Share {
+    int first, len, row;   // its first token, its length, its row of the states
+    int t0, t1;            // the tokens, counted from there; t0 = t1 in an empty sequence, which is where it begins
+    bool some;             // false: nothing (no token, a skipped sequence)
+};
+// One after the other; as one is taken the bounds and the slot of the next are asked for.  Where two waves share a sequence the first one has `least` tokens of it or
+// all: a state reaches no further than that, so that who has t0 = 0 alone reads and writes it.
+struct Shares {
+    const int32_t *start, *slot;
+    int n_tokens, n_slots, B;
+    int64_t from, to;
+    int b, least, bound, next_bound, next_row;   // the next sequence; tokens of its first part at least; its bounds and its row
+    // (every lane of the wave calls it)
+    __device__ __forceinline__ Shares(const ConvArgs &a, int64_t from, int64_t to, int least)
+        : start(a.start), slot(a.slot), n_tokens(a.n_tokens), n_slots(a.n_slots), B(a.B), from(from), to(to), b(sequence_at(a.start, a.n_tokens, a.B, from)), least(least)
+    {
+        bound = __builtin_amdgcn_readfirstlane(start[b]);
+        ask();
+    }
+    __device__ __forceinline__ void ask()   // (b < B)
+    {
+        next_bound = __builtin_amdgcn_readfirstlane(start[b + 1]);
+        next_row = __builtin_amdgcn_readfirstlane(slot ? slot[b] : b);
+    }
+    __device__ __forceinline__ bool more() const { return b < B && min(max(bound, 0), n_tokens) + (int64_t)SEQUENCE * b < to; }
+    __device__ __forceinline__ Share take()
+    {
+        const int first = min(max(bound, 0), n_tokens), len = min(max(next_bound, first), n_tokens) - first, row = next_row;
+        const int64_t begin = first + (int64_t)SEQUENCE * b, token = begin + SEQUENCE;
+        auto cut = [&](int64_t t) { return t <= 0 ? 0 : (int)min(max(t, (int64_t)least), (int64_t)len); };
+        const int t0 = cut(from - token), t1 = cut(to - token);
+        const bool some = row >= 0 && row < n_slots && (t0 < t1 || (len == 0 && begin >= from));
+        bound = next_bound;
+        if (++b < B)
+            ask();
+        return Share{first, len, row, t0, t1, some};
+    }
+};
 
 // The gates of some tokens and heads, dealt over a wave: lane -> (token, head), heads in the next power of two of lanes.
 struct GateLanes {
@@ -253,7 +287,7 @@ void launch_conv_token(int in_dtype, int width, const ConvTokenArgs &a, hipStrea
 void launch_conv_drafts(int in_dtype, int width, const ConvDraftArgs &a, hipStream_t stream);
 void launch_conv_commit(int in_dtype, int width, const ConvCommitArgs &a, hipStream_t stream);
 template <typename T>
-void launch_conv_grad_typed(int width, const ConvGradArgs &a, int most, float *dweight, float *dbias, float *dA_log, float *ddt_bias,
+void launch_conv_grad_typed(int width, const ConvGradArgs &a, int64_t length, float *dweight, float *dbias, float *dA_log, float *ddt_bias,
                             hipStream_t stream);                                            // kvb_conv_grad_*.hip
 template <typename TX, typename T>
 void launch_norm_typed(const NormArgs &a, hipStream_t stream);                              // kvb_norm.hip
@@ -262,43 +296,47 @@ void launch_norm_grad_typed(const NormGradArgs &a, float *dweight, hipStream_t s
 void launch_grad_norm(const ListArgs &a, float *norm, double *work, hipStream_t stream);    // kvb_clip.hip
 void launch_clip(const ListArgs &a, const float *norm, float largest, hipStream_t stream);
 
-// Pieces of the convolution, and for its gradients how many a wave takes: a workgroup's four waves leave one part.
-constexpr int CONV_LEAST = 4;    // tokens of a piece (more than the taps reach back)
-struct ConvParts {
-    int most, parts, each;
-};
-// Pieces so long that the workgroups of four of them come out as `rounds` for each compute unit at most, the fewest with which a piece is no longer than `enough`
-// tokens: what starts behind others runs alone, and a short piece pays for its weights and the inputs ahead of it.  units: waves of a piece.
+// Places of a wave: as many as make the workgroups of four waves come out as `rounds` for each compute unit at most, the fewest with which they are no more than 16:
+// what starts behind others runs alone, and few tokens pay for their weights and the inputs ahead of them.  units: waves of a stretch.
 // us, kvb_conv, 16 + 32 heads of 128, bf16, W = 4, enough 8 / 16: 1000 tokens 11.8 / 11.6, 2000 19.0 / 16.7; 8191 tokens in 4 rounds 66, 5 59.1, 6 59.2, 7 61.3,
 // 9 60.1; fp32, 5284 tokens, W = 3, in 3 80.8, 4 84.4, 6 83.9.  kvb_conv_backward, bf16: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112;
 // fp32, 3 x 2048 tokens in 2 147, 3 135, 4 139.
-inline int conv_length(int64_t n_tokens, int64_t B, int units, int rounds, int enough, int64_t up)
+constexpr int CONV_LEAST = 4;   // places of a wave at least
+inline int64_t conv_length(int64_t places, int units, int rounds)
 {
-    int64_t length = up;
-    for (int k = 1; k <= rounds; ++k) {
-        const int64_t most = 256 * k / units * 4, pieces = most < 4 ? 4 : B < most / 2 ? most - B : most / 2;
-        length = (n_tokens + pieces - 1) / pieces;
-        if (length <= enough)
-            break;
+    int64_t length = INT64_MAX;
+    for (int k = 1; k <= rounds && length > 16; ++k) {
+        const int64_t most = 256 * k / units * 4, waves = most < 4 ? 4 : most;
+        length = (places + waves - 1) / waves;
     }
-    return (int)(length < CONV_LEAST ? CONV_LEAST : length < up ? length : up);
+    return length < CONV_LEAST ? CONV_LEAST : length;
 }
-inline int conv_most(int64_t n_tokens, int64_t B, int units, bool wide) { return conv_length(n_tokens, B, units, wide ? 3 : 6, 16, 64); }
+struct ConvDeal {
+    int64_t length, stretches;
+};
+inline ConvDeal conv_deal(int64_t n_tokens, int64_t B, int units, bool wide)
+{
+    const int64_t places = places_of(n_tokens, B), most = conv_length(places, units, wide ? 3 : 6), length = most < 64 ? most : 64;
+    return ConvDeal{length, (places + length - 1) / length};
+}
+struct ConvParts {
+    int64_t length;
+    int parts;   // a workgroup's four waves leave one
+};
 // Those of kvb_conv_backward that fit a compute unit at once: its registers (fp32: of half as many channels) leave each SIMD two waves (three)
 constexpr int grad_rounds(bool wide) { return wide ? 3 : 2; }
 inline int64_t conv_part_limit(int units, bool wide) { return 256 * grad_rounds(wide) / units < 1 ? 1 : 256 * grad_rounds(wide) / units; }
 inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units, bool wide)
 {
     if (B == 0)   // (tokens of nobody)
-        return ConvParts{CONV_LEAST, 0, 1};
-    const int most = conv_length(n_tokens, B, units, grad_rounds(wide), 12, INT32_MAX);
-    const int64_t limit = conv_part_limit(units, wide), pieces = pieces_of(n_tokens, B, most), each = (pieces + 4 * limit - 1) / (4 * limit), e = each < 1 ? 1 : each;
-    return ConvParts{most, (int)((pieces + 4 * e - 1) / (4 * e)), (int)e};
+        return ConvParts{CONV_LEAST, 0};
+    const int64_t places = places_of(n_tokens, B), length = conv_length(places, units, grad_rounds(wide));
+    return ConvParts{length, (int)((places + 4 * length - 1) / (4 * length))};
 }
 // The most that a call of up to so many tokens and sequences needs
 inline int64_t conv_most_parts(int64_t n_tokens, int64_t B, int units, bool wide)
 {
-    const int64_t n = (pieces_of(n_tokens, B, CONV_LEAST) + 3) / 4, limit = conv_part_limit(units, wide);
+    const int64_t n = (places_of(n_tokens, B) + 4 * CONV_LEAST - 1) / (4 * CONV_LEAST), limit = conv_part_limit(units, wide);
     return n < 1 ? 1 : n < limit ? n : limit;
 }
 

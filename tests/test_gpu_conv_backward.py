@@ -5,7 +5,7 @@ import torch
 from paper_2605_19049_amd import kvb
 from layer_reference import V, f64, gates, softplus, zeros
 from running_error import U, check
-from test_gpu_conv import FILL, Case, run
+from test_gpu_conv import EPS, FILL, Case, run
 
 pytestmark = pytest.mark.gpu
 
@@ -141,6 +141,55 @@ def test_a_wave_takes_several_short_sequences():
     c = Case([(b * 5 + b // 7) % 5 for b in range(300)], 8, 16, 128, 4, "bf16", seed=7, bias=True)
     g = grads_of(c)
     check_backward(c, g, backward(c, g))
+
+
+def test_parts_of_sequences():
+    """Waves that have the end of a sequence, whole ones, empty ones and the beginning of another, rows of nobody ahead and behind"""
+    c = Case([(b * 11 + b // 5) % 31 * (b % 4 != 2) for b in range(130)], 3, 6, 64, 3, "f32", seed=11, bias=True, n_slots=140, lead=9, tail=4)
+    c.slot[17], c.slot[60] = -1, 140
+    g = grads_of(c)
+    check_backward(c, g, backward(c, g), skipped=(17, 60))
+
+
+def sum_of_sizes(c, g):
+    """sum over tokens of |dz E| for each weight, in 64 bits"""
+    lens = (c.start[1:] - c.start[:-1]).long().cpu()
+    first, slot = c.start[:-1].long().cpu().repeat_interleave(lens), c.slot.long().cpu().repeat_interleave(lens)
+    token = torch.arange(int(c.start[0]), int(c.start[-1]))
+    x, state, w = (y.double().cpu() for y in (c.x, c.state0, c.weight))
+    E = []
+    for i in range(c.W):
+        at = token - first + i   # the row of E
+        E.append(torch.where((at >= c.W - 1)[:, None], x[(token + i - (c.W - 1)).clamp(min=0)], state[slot, at.clamp(max=c.W - 2)]))
+    z = sum(w[:, i] * E[i] for i in range(c.W)).requires_grad_()
+    y = z * torch.sigmoid(z)
+    h = y.unflatten(1, (-1, c.d))
+    n = torch.cat([h[:, :2 * c.Hk] / (h[:, :2 * c.Hk].square().sum(-1, keepdim=True) + EPS).sqrt(), h[:, 2 * c.Hk:]], 1)
+    dn = torch.cat([g[k][token] for k in ("dq", "dk", "dv")], 1).double().cpu()
+    (dz,) = torch.autograd.grad((n * dn).sum(), z)
+    return torch.stack([(dz * e).abs().sum(0) for e in E], 1)
+
+
+@pytest.mark.parametrize("B", [64, 65, 4096, 4097, 6000])
+def test_many_sequences(B):
+    """Found among up to thousands, two of three empty: token by token the bits of the call that has the others alone"""
+    lens = [0 if b % 3 else 1 + b % 4 for b in range(B)]
+    c = Case(lens, 1, 2, 32, 4, "f32", seed=B)
+    g = grads_of(c)
+    r = backward(c, g)
+    some = torch.tensor([n > 0 for n in lens], device="cuda")
+    none = c.slot[~some].long()
+    assert torch.equal(r["dstate0"][none], g["dstate1"][none])
+    c.slot, c.start = c.slot[some].contiguous(), torch.cat([c.start[:1], c.start[1:][some]])
+    c.sh = kvb.shape(len(c.slot), 1, 2, 32, 32, 1, c.code)
+    alone = backward(c, g)
+    for n in ("dx", "da", "db"):
+        assert torch.equal(r[n], alone[n]), n
+    slots = c.slot.long()
+    assert torch.equal(r["dstate0"][slots], alone["dstate0"][slots])
+    # both are sums of the same numbers dz E: up to 40 tokens a wave, 4 waves, up to 384 parts as 64 sums of 6 each, so fewer than 128 roundings of what their sizes add up to
+    size = sum_of_sizes(c, g)
+    assert ((r["dweight"] - alone["dweight"]).abs().double().cpu() <= 2 * 128 * U * size).all()
 
 
 def test_long_sequences():

@@ -107,10 +107,10 @@ def test_sequences():
 
 
 def test_calls_that_a_launch_does_not_hold():
-    """2^32 threads: 64 for each 512 channels of a piece, token or draft, and for its gates"""
+    """2^32 threads: 64 for each 512 channels of up to 64 tokens (a sequence is as much as 8 more), of a token or draft, and for its gates"""
     small = dict(Hk=1, Hv=1, dk=32, dv=32)
     assert conv(sh=shape(B=2 ** 30 - 1, **small), sq=seqs(n_tokens=0)) == kvb.EINVAL
-    assert conv(sh=shape(B=2 ** 25, **small)) == kvb.EINVAL
+    assert conv(sh=shape(B=2 ** 29, **small)) == kvb.EINVAL
     assert decode(sh=shape(B=2 ** 25, **small)) == kvb.EINVAL
     assert verify(sh=shape(B=2 ** 23, **small)) == kvb.EINVAL
     assert commit(sh=shape(B=2 ** 25, **small)) == kvb.EINVAL
