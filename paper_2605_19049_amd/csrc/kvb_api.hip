@@ -291,7 +291,7 @@ int check_conv_seqs(const kvb_shape *sh, const kvb_taps *ta, const kvb_seqs *sq)
     rc = check_seqs(&own, sq);
     if (rc != KVB_OK)
         return rc;
-    return conv_units_fit(sh, conv_deal(sq->n_tokens, sh->B, conv_groups((int)conv_channels(sh)) + 1, sh->in_dtype == KVB_F32).stretches) ? KVB_OK : KVB_EINVAL;
+    return conv_units_fit(sh, conv_deal(sq->n_tokens, sh->B, conv_groups((int)conv_channels(sh)) + 1, sh->in_dtype == KVB_F32, false).stretches) ? KVB_OK : KVB_EINVAL;
 }
 // T tokens of each of B requests
 int conv_tokens_common(const kvb_shape *sh, const kvb_taps *ta, const int32_t *slot, int32_t n_slots, int32_t T, const int32_t *parent, const void *x,

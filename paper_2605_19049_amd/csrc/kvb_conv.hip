@@ -85,11 +85,14 @@ __device__ __forceinline__ void gates_of(const ConvBase &a, int64_t t0, int n, i
 
 }  // namespace
 
-// Whole sequences: a wave takes the tokens of `length` places one after the other, with the taps' inputs in registers.
-template <typename T, int W, bool STREAM>
-__global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int units, int64_t length)
+// Whole sequences: a wave takes the tokens of `length` places one after the other, with the taps' inputs in registers, and asks for four tokens ahead: one as one is taken (16
+// bits, x from the caches); four as the four ahead of them are done; or (LARGE) before those are begun.  LARGE leaves a SIMD three waves for its registers, the others
+// four (fp32: three).  us, one / four / LARGE: 300 tokens 5.7 / 6.1 / 5.8, 1000 10.9 / 11.1 / 11.3, 2000 16.1 / 16.1 / 16.5; 24 sequences of up to 1500, 4 + 8 heads, past the caches
+// 36.2 / 34.8 / 36.3, one of 8191 62.2 / 62.0 / 58.6; fp32, 5284 tokens, W = 3, 81 / 75 / 81.
+template <typename T, int W, bool STREAM, bool LARGE>
+__global__ __launch_bounds__(256, LARGE || sizeof(T) == 4 ? 3 : 4) void kvb_conv_kernel(const ConvArgs a, int units, int64_t length)
 {
-    constexpr int U = 4;   // tokens at a time
+    constexpr bool ONE = sizeof(T) == 2 && !STREAM;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), groups = conv_groups(a.C);
     const int unit = blockIdx.x * 4 + wave, each = groups + a.gates;
     if (unit >= units)
@@ -120,49 +123,52 @@ __global__ __launch_bounds__(256) void kvb_conv_kernel(const ConvArgs a, int uni
             return s0 ? load_raw8(s0 + (int64_t)e * a.C) : Raw8<T>{};
         };
         if (p.t0 < p.t1) {
-            Raw8<T> raw[U], before[W - 1];
+            Raw8<T> raw[4], next[4], before[W - 1];
 #pragma unroll
             for (int i = 0; i < W - 1; ++i)
                 before[i] = input_at(p.t0 + i);
-            auto request = [&](int t) {
+            auto request = [&](int t, Raw8<T> (&to)[4]) {
+                if (t < p.t1)
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    raw[u] = load_raw8_if<STREAM>(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
+                    for (int u = 0; u < 4; ++u)
+                        to[u] = load_raw8_if<STREAM>(x + (int64_t)min(t + u, p.t1 - 1) * a.x_stride);
             };
-            request(p.t0);
+            request(p.t0, LARGE ? next : raw);
             const Lane8<T, W> l(a, ch, a.q_stride, a.k_stride, a.v_stride);
             T *out = l.to + ((int64_t)p.first + p.t0) * l.to_stride;
-            float e[W - 1 + U][8];
+            float e[4][8];   // row t + W - 1 of E at (t - t0) % 4
 #pragma unroll
             for (int i = 0; i < W - 1; ++i)
-                unpack8(before[i], e[i]);
-            for (int t = p.t0; t < p.t1; t += U) {
+                unpack8(before[i], e[i + 4 - (W - 1)]);
+            for (int t4 = p.t0; t4 < p.t1; t4 += 4) {
+                if constexpr (LARGE) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    unpack8(raw[u], e[W - 1 + u]);
-                if (t + U < p.t1)
-                    request(t + U);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (t + u < p.t1) {
-                        float z[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            z[j] = l.bias[j];
-#pragma unroll
-                            for (int i = 0; i < W; ++i)
-                                z[j] = fmaf(l.w[i][j], e[u + i][j], z[j]);
-                        }
-                        l.finish(z);
-                        store8(out, z);
-                        out += l.to_stride;
-                    }
+                    for (int u = 0; u < 4; ++u)
+                        raw[u] = next[u];
+                    request(t4 + 4, next);
                 }
+                static_for<4>([&](auto at) {
+                    constexpr int u = at();
+                    if (t4 + u >= p.t1)
+                        return;
+                    unpack8(raw[u], e[u]);
+                    if constexpr (ONE)
+                        if (t4 + u + 4 < p.t1)
+                            raw[u] = load_raw8(x + (int64_t)(t4 + u + 4) * a.x_stride);
+                    float z[8];
 #pragma unroll
-                for (int i = 0; i < W - 1; ++i)
+                    for (int j = 0; j < 8; ++j) {
+                        z[j] = l.bias[j];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        e[i][j] = e[U + i][j];
+                        for (int i = 0; i < W; ++i)
+                            z[j] = fmaf(l.w[i][j], e[(u + 4 - (W - 1) + i) % 4][j], z[j]);
+                    }
+                    l.finish(z);
+                    store8(out, z);
+                    out += l.to_stride;
+                });
+                if constexpr (!ONE && !LARGE)
+                    request(t4 + 4, raw);
             }
         }
         // Who has the first token writes the last state: nobody else reads the first one's rows, which it may lie in.
@@ -346,17 +352,25 @@ void with_taps(int dtype, int width, F &&f)
 
 void launch_conv(int dtype, int width, const ConvArgs &a, hipStream_t stream)
 {
-    const int each = conv_groups(a.C) + a.gates;
-    const ConvDeal deal = conv_deal(a.n_tokens, a.B, each, dtype == KVB_F32);
-    const int units = (int)(deal.stretches * each);
     // x past the caches where it and what is made from it fill half of the last level: what reads the results next finds more of them there.  us with the
-    // kvb_scan behind it, plain / past them: 300 tokens 38.2 / 38.9, 1024 84.7 / 85.2, 4096 (64 MiB) 286.3 / 286.0, 8191 576 / 571, 24 sequences of 750 562 / 558.
-    const bool stream_x = (int64_t)a.n_tokens * a.C * (dtype == KVB_F32 ? 4 : 2) > 64 << 20;
+    // kvb_scan behind it, plain / past them: 300 tokens 38.2 / 38.9, 1024 84.7 / 85.2, 4096 (64 MiB) 286.3 / 286.0, 8191 576 / 571, 24 sequences of 750 562 / 558.  Not
+    // in fp32, where a lane's 32 bytes are two loads that a line has to stay for: 3 x 2048 tokens 96.7 / 89.7 without.
+    // Above 100 MiB (with the results more than the last level has) memory does less for more waves: LARGE in six rounds / the others in four: 3000 tokens
+    // 25.6 / 23.4, 24 sequences of up to 1500, 4 + 8 heads (71 MiB) 36.0 / 34.7, 5500 (86 MiB) 39.1 / 37.9, 6200 45.3 / 44.9, 7000 (109 MiB) 51.0 / 53.8, 8191 58.8 / 62.3.
+    const int each = conv_groups(a.C) + a.gates;
+    const int64_t bytes = (int64_t)a.n_tokens * a.C * (dtype == KVB_F32 ? 4 : 2);
+    const bool stream_x = bytes > 64 << 20, large = bytes > 100 << 20;
+    const ConvDeal deal = conv_deal(a.n_tokens, a.B, each, dtype == KVB_F32, large);
+    const int units = (int)(deal.stretches * each);
     with_taps(dtype, width, [&]<typename T, int W>() {
-        if (stream_x)
-            launch_part(kvb_conv_kernel<T, W, true>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
+        if constexpr (sizeof(T) == 4)
+            launch_part(kvb_conv_kernel<T, W, false, false>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
+        else if (large)
+            launch_part(kvb_conv_kernel<T, W, true, true>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
+        else if (stream_x)
+            launch_part(kvb_conv_kernel<T, W, true, false>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
         else
-            launch_part(kvb_conv_kernel<T, W, false>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
+            launch_part(kvb_conv_kernel<T, W, false, false>, true, true, (units + 3) / 4, 256, stream, a, units, deal.length);
     });
 }
 

@@ -299,7 +299,7 @@ void launch_clip(const ListArgs &a, const float *norm, float largest, hipStream_
 // Places of a wave: as many as make the workgroups of four waves come out as `rounds` for each compute unit at most, the fewest with which they are no more than 16:
 // what starts behind others runs alone, and few tokens pay for their weights and the inputs ahead of them.  units: waves of a stretch.
 // us, kvb_conv, 16 + 32 heads of 128, bf16, W = 4, enough 8 / 16: 1000 tokens 11.8 / 11.6, 2000 19.0 / 16.7; 8191 tokens in 4 rounds 66, 5 59.1, 6 59.2, 7 61.3,
-// 9 60.1; fp32, 5284 tokens, W = 3, in 3 80.8, 4 84.4, 6 83.9.  kvb_conv_backward, bf16: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112;
+// 9 60.1; 200 sequences of up to 64, 8 + 16 heads, in 3 29.9, 4 28.8, 5 32.1, 8 32.4; fp32, 5284 tokens, W = 3, in 3 80.8, 4 84.4, 6 83.9.  kvb_conv_backward, bf16: 4 x 2048 tokens in 1.75 rounds 115, 2 104, 4 112;
 // fp32, 3 x 2048 tokens in 2 147, 3 135, 4 139.
 constexpr int CONV_LEAST = 4;   // places of a wave at least
 inline int64_t conv_length(int64_t places, int units, int rounds)
@@ -314,9 +314,9 @@ inline int64_t conv_length(int64_t places, int units, int rounds)
 struct ConvDeal {
     int64_t length, stretches;
 };
-inline ConvDeal conv_deal(int64_t n_tokens, int64_t B, int units, bool wide)
+inline ConvDeal conv_deal(int64_t n_tokens, int64_t B, int units, bool wide, bool large)
 {
-    const int64_t places = places_of(n_tokens, B), most = conv_length(places, units, wide ? 3 : 6), length = most < 64 ? most : 64;
+    const int64_t places = places_of(n_tokens, B), most = conv_length(places, units, wide ? 3 : large ? 6 : 4), length = most < 64 ? most : 64;
     return ConvDeal{length, (places + length - 1) / length};
 }
 struct ConvParts {

@@ -148,6 +148,28 @@ def test_large_calls():
             assert torch.equal(s1[int(c.slot[b])], want)
 
 
+@pytest.mark.parametrize("W, dtype", [(4, "bf16"), (3, "f16"), (2, "bf16"), (4, "f32")])
+def test_the_same_bits_in_calls_of_any_size(W, dtype):
+    """Above 100 MiB (in 16 bits) x is asked for in another way, and in each form a call is cut up as it fits"""
+    c = Case([9000, 1, 0, 5000, 31], 8, 16, 128, W, dtype, seed=4, bias=W == 2)
+    assert c.N * c.C * 2 > 100 << 20
+    o, s1 = run(c)
+    starts, slots = c.start, c.slot
+    for b in range(5):
+        c.start, c.slot = starts[b:b + 2].contiguous(), slots[b:b + 1].contiguous()
+        c.sh, c.sq = kvb.shape(1, c.Hk, c.Hv, c.d, c.d, 1, c.code), kvb.seqs(c.start, c.N, c.n_slots, slot=c.slot)
+        mine, state = run(c)
+        at, row = slice(c.ends[b], c.ends[b + 1]), int(slots[b])
+        assert all(torch.equal(x[at], y[at]) for x, y in zip(o, mine)) and torch.equal(s1[row], state[row])
+    # a call of no more tokens than the sequence has
+    c.x, c.a, c.b, c.N = (*(y[c.ends[3]:c.ends[4]] for y in (c.x, c.a, c.b)), 5000)
+    c.start, c.slot = torch.tensor([0, 5000], dtype=torch.int32, device="cuda"), slots[3:4].contiguous()
+    c.sq = kvb.seqs(c.start, c.N, c.n_slots, slot=c.slot)
+    mine, state = run(c)
+    at, row = slice(c.ends[3], c.ends[4]), int(slots[3])
+    assert all(torch.equal(x[at], y) for x, y in zip(o, mine)) and torch.equal(s1[row], state[row])
+
+
 def test_state_in_place_and_none():
     for lens in ([2], [1, 0, 3, 100]):
         c = Case(lens, 2, 2, 64, 4, "bf16", seed=7)
