@@ -516,7 +516,8 @@ typedef struct kvb_list {       /* some tensors, none of which share memory; all
 
 /*
  * kvb_grad_norm -- norm = the root of the sum of squares of all elements (summed in fp64).
- *   norm  device fp32 [1], written       work  device, kvb_grad_norm_work(list) bytes, 8-byte aligned; means nothing before and after the call
+ *   norm  device fp32 [1], written       work  device, kvb_grad_norm_work(list) bytes, 8-byte aligned; means nothing before and after the call.  It grows with
+ *                                              blocks and depends on nothing else: what it gives for the longest list serves shorter ones
  */
 int64_t kvb_grad_norm_work(const kvb_list *list);
 int kvb_grad_norm(const kvb_list *list, float *norm, void *work, void *stream);

@@ -529,7 +529,7 @@ int kvb_norm_backward(const kvb_rows *rows, const void *x, const void *gate, con
 int64_t kvb_grad_norm_work(const kvb_list *list)
 {
     const int rc = check_list(list);
-    return rc != KVB_OK ? rc : 8 * (int64_t)list->blocks * list_split(list->blocks);
+    return rc != KVB_OK ? rc : 8 * list_most_sums(list->blocks);
 }
 
 int kvb_grad_norm(const kvb_list *list, float *norm, void *work, void *stream)

@@ -341,8 +341,14 @@ inline int64_t conv_most_parts(int64_t n_tokens, int64_t B, int units, bool wide
 }
 
 // Workgroups of a block of a list: several where the blocks alone do not fill the card
-constexpr int LIST_SPLIT = 4;
-inline int list_split(int blocks) { return blocks < 512 ? LIST_SPLIT : 1; }
+constexpr int LIST_SPLIT = 4, LIST_FULL = 512;
+inline int list_split(int blocks) { return blocks < LIST_FULL ? LIST_SPLIT : 1; }
+// The most sums that a list of up to so many blocks leaves, one a workgroup: what the longest split list does, where that is more
+inline int64_t list_most_sums(int64_t blocks)
+{
+    const int64_t split = LIST_SPLIT * (blocks < LIST_FULL ? blocks : LIST_FULL - 1);
+    return blocks > split ? blocks : split;
+}
 static_assert(KVB_LIST_BLOCK % (LIST_SPLIT * 8) == 0);
 
 // kvb_norm_backward, rows above 512 elements: vectors of 8 that a lane has of a row, threads of a row, rows of a workgroup at once

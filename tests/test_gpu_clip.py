@@ -141,3 +141,18 @@ def test_another_stream_and_a_replayed_graph():
         want = want_norm(tensors)
         assert abs(float(norm) - want) <= 2.0 ** -24 * want * 1.01
         assert abs(want_norm(to) - 1.0) < 0.004   # (bf16: each element is off by half a step of 2^-8 at most)
+
+
+def test_one_workspace_for_lists_of_any_length():
+    """The longest list's: one of 511 blocks, each of which leaves four sums, takes more of it than one of 600.  What lies behind stays"""
+    tensors = some([i * 5 % 90 + 1 for i in range(600)], [TYPES[i % 3] for i in range(600)])
+    room = kvb.grad_norm_work(kvb.TensorList(tensors).c())
+    buffer = torch.full((room + 65536,), 119, dtype=torch.uint8, device="cuda")
+    for n in (1, 127, 128, 511, 512, 600):
+        li, norm = kvb.TensorList(tensors[:n]), torch.full((1,), -1.0, device="cuda")
+        assert li.blocks == n
+        kvb.kvb_grad_norm(li.c(), norm, buffer)
+        torch.cuda.synchronize()
+        want = want_norm(tensors[:n])
+        assert abs(float(norm) - want) <= 2.0 ** -24 * want * 1.01
+        assert (buffer[room:] == 119).all()

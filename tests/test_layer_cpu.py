@@ -312,3 +312,13 @@ def test_structs_as_a_c_caller_sees_them(tmp_path):
     t, r, li = kvb.KvbTaps, kvb.KvbRows, kvb.KvbList
     assert got == [[ctypes.sizeof(t), t.x_stride.offset, t.width.offset, t.eps.offset], [ctypes.sizeof(r), r.n_tokens.offset, r.x_dtype.offset, r.scale.offset],
                    [ctypes.sizeof(li), li.first.offset, li.blocks.offset], [kvb.CONV_UNIT, kvb.MAX_WIDTH, kvb.LIST_BLOCK]]
+
+
+def test_workspace_of_a_norm_grows_with_the_list():
+    """That of the largest list serves shorter ones, which a call cuts up finer"""
+    def work(blocks):
+        return kvb.grad_norm_work(kvb.KvbList(A, A, A, A, 1, blocks) if blocks else kvb.KvbList(None, None, None, None, 0, 0))
+    at = [work(blocks) for blocks in list(range(3001)) + [10 ** 5, 10 ** 6]]
+    assert at == sorted(at) and at[0] == 0 and at[-1] <= 8 * 10 ** 6
+    # (each workgroup leaves 8 bytes: four a block below 512 blocks, one from there on)
+    assert all(w >= 8 * blocks * (4 if blocks < 512 else 1) for blocks, w in enumerate(at[:3001]))
