@@ -594,24 +594,36 @@ def kvb_clip(li, to, norm, largest, stream=None, check=True):
     return _call("kvb_clip", li, to, norm, largest, stream=stream, check=check)
 
 
+# structs that a call takes without: (call, argument)
+_MAY_BE_NONE = {("kvb_clip", 1)}
+
+
 def bind(fn_name, *args):
     """Pre-marshal one call: returns a zero-argument callable that re-issues it with the
     same pointers (for serving loops, where per-call marshalling would rival a 20 us
     kernel).  `args` are exactly the C arguments; tensors, structs and ints are converted
-    once.  The caller keeps the tensors and structs alive."""
-    _check_layouts(fn_name, args)
+    once, and here alone their types are looked at: TypeError for another struct than the call
+    takes, a struct where an address belongs, None where neither an address nor kvb_clip's `to`
+    does.  The caller keeps the tensors and structs alive."""
     types = getattr(lib(), fn_name).argtypes
     assert len(args) == len(types), fn_name
     conv = []
-    for a, t in zip(args, types):
-        if isinstance(a, ctypes.Structure):
-            conv.append(ctypes.byref(a))
-        elif a is None:
-            conv.append(None)
+    for i, (a, t) in enumerate(zip(args, types)):
+        wanted = getattr(t, "_type_", None) if t is not ctypes.c_void_p else None
+        if isinstance(wanted, type) and issubclass(wanted, ctypes.Structure):
+            if a is None and (fn_name, i) in _MAY_BE_NONE:
+                conv.append(None)
+            elif isinstance(a, wanted):
+                conv.append(ctypes.byref(a))
+            else:
+                raise TypeError("%s, argument %d: a %s is wanted, not %s" % (fn_name, i, wanted.__name__, type(a).__name__))
         elif t is ctypes.c_void_p:
+            if not (a is None or isinstance(a, int) or hasattr(a, "data_ptr")):
+                raise TypeError("%s, argument %d: a tensor, an address or None is wanted, not %s" % (fn_name, i, type(a).__name__))
             conv.append(ctypes.c_void_p(_ptr(a)))
         else:
             conv.append(t(a))
+    _check_layouts(fn_name, args)
     # a function object of its own without types: the arguments have theirs, and checking 16 of them once more takes a microsecond of 2.7
     fn = lib()[fn_name]
 
