@@ -488,7 +488,7 @@ def taps(weight, width=4, bias=None, A_log=None, dt_bias=None, x=None, a=None, b
 def _call(fn_name, *args, stream=None, check=True):
     """args: the C arguments, structs first, without the stream"""
     _check_layouts(fn_name, args)
-    conv = [ctypes.byref(x) if isinstance(x, ctypes.Structure) else x if t in (ctypes.c_int32, ctypes.c_float) else _ptr(x)
+    conv = [_ptr(x) if t is ctypes.c_void_p else ctypes.byref(x) if isinstance(x, ctypes.Structure) else x
             for x, t in zip(args, getattr(lib(), fn_name).argtypes)]
     return _check(getattr(lib(), fn_name)(*conv, _stream(stream)), fn_name, check)
 

@@ -69,3 +69,20 @@ def test_a_bound_call_passes_numbers_where_the_library_has_them():
     for n_slots, T in ((-1, 2), (2, 0), (2, kvb.MAX_DRAFTS + 1)):
         with pytest.raises(kvb.KvbError, match="kvb_conv_verify"):
             kvb.bind("kvb_conv_verify", SH, TA, A, n_slots, T, None, *[A] * 10)()
+
+
+AROUND = [n for n in CALLS if n.startswith(("kvb_conv", "kvb_norm")) or n in ("kvb_grad_norm", "kvb_clip")]
+
+
+@pytest.mark.parametrize("name", AROUND)
+def test_a_struct_is_no_address_in_a_plain_call_either(name):
+    """(sizes that the library refuses: nothing is launched)"""
+    args = list(CALLS[name][:-1])
+    bad = {kvb.KvbShape: kvb.shape(-1, 2, 4, 64, 64, 8, kvb.BF16), kvb.KvbRows: kvb.rows(-1, 1, 64, kvb.BF16), kvb.KvbList: kvb.KvbList(A, A, A, A, -1, 1)}
+    args[0] = bad[type(args[0])]
+    fn = getattr(kvb, name)
+    assert fn(*args, stream=0, check=False) == kvb.EINVAL
+    for i, a in enumerate(args):
+        if a is A:
+            with pytest.raises((TypeError, AttributeError)):
+                fn(*args[:i], kvb.KvbShape(), *args[i + 1:], stream=0, check=False)
