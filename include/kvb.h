@@ -511,7 +511,7 @@ typedef struct kvb_list {       /* some tensors, none of which share memory; all
     const int32_t *type;        /* [n] KVB_F32, KVB_BF16 or KVB_F16                                                  */
     const int32_t *first;       /* [n+1] running sum of ceil(size / KVB_LIST_BLOCK), from 0                          */
     int32_t        n;
-    int32_t        blocks;      /* first[n]                                                                          */
+    int32_t        blocks;      /* first[n]; below 2^24 - 1: 256 threads a block                                     */
 } kvb_list;
 
 /*

@@ -363,7 +363,7 @@ int norm_types(const kvb_rows *ro, F &&f)
 
 int check_list(const kvb_list *li)
 {
-    if (!li || li->n < 0 || li->blocks < 0 || (li->n == 0 && li->blocks > 0))
+    if (!li || li->n < 0 || li->blocks < 0 || li->blocks > MOST_WAVES / 4 || (li->n == 0 && li->blocks > 0))
         return KVB_EINVAL;
     if (li->n > 0 && (!li->data || !li->size || !li->type || !li->first))
         return KVB_EINVAL;

@@ -322,3 +322,12 @@ def test_workspace_of_a_norm_grows_with_the_list():
     assert at == sorted(at) and at[0] == 0 and at[-1] <= 8 * 10 ** 6
     # (each workgroup leaves 8 bytes: four a block below 512 blocks, one from there on)
     assert all(w >= 8 * blocks * (4 if blocks < 512 else 1) for blocks, w in enumerate(at[:3001]))
+
+
+def test_lists_that_a_launch_does_not_hold():
+    """256 threads a block"""
+    for blocks in (2 ** 24, 2 ** 31 - 1):
+        li = some_list(blocks=blocks)
+        assert kvb.lib().kvb_grad_norm_work(ctypes.byref(li)) == kvb.EINVAL
+        assert kvb.kvb_grad_norm(li, A, A, stream=0, check=False) == kvb.EINVAL and kvb.kvb_clip(li, None, A, 1.0, stream=0, check=False) == kvb.EINVAL
+    assert kvb.grad_norm_work(some_list(blocks=2 ** 24 - 2)) == 8 * (2 ** 24 - 2)
