@@ -156,3 +156,49 @@ def test_one_workspace_for_lists_of_any_length():
         want = want_norm(tensors[:n])
         assert abs(float(norm) - want) <= 2.0 ** -24 * want * 1.01
         assert (buffer[room:] == 119).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("at, other", [(0, 0), (1, 1), (5, 5), (1, 2), (0, 7)])
+def test_whole_blocks(dtype, at, other):
+    """Lists of 512 blocks and more have a workgroup for 16384 elements: parts of a flat buffer, at any element of it, with something between them that stays"""
+    sizes = [5_000_077, 3 * B, 3_400_001, B - 1, B, B + 1, 9, 14336, 14337 + 7 * B]
+    flat, flat_to = some([sum(sizes) + 16 * len(sizes) + 16] * 2, [dtype] * 2)
+    kept, kept_to = flat.clone(), flat_to.clone()
+
+    def parts(buffer, first):
+        out, p = [], first
+        for n in sizes:
+            out.append(buffer[p:p + n])
+            p += n + 16   # (source and result of each lie alike among 16 bytes if those of the first do)
+        return out
+    tensors, to = parts(flat, at), parts(flat_to, other)
+    li, norm = norm_of(tensors)
+    assert li.blocks >= 512
+    want = want_norm(tensors)
+    assert abs(float(norm) - want) <= 2.0 ** -24 * want * 1.01
+    kvb.kvb_clip(li.c(), kvb.TensorList(to).c(), norm, 1000.0)
+    torch.cuda.synchronize()
+    assert torch.equal(flat, kept)
+    cut, f = 1000.0 / (want + 1e-6), torch.finfo(dtype)
+    assert cut < 0.5
+    for x, y in zip(tensors, to):
+        # (as in check: norm, the sum with 1e-6, the quotient, the product; the last rounding)
+        off, size = (y.double() - cut * x.double()).abs(), cut * x.double().abs()
+        assert (off <= 8 * 2.0 ** -24 * size + (0 if dtype == torch.float32 else f.eps / 2) * size + f.smallest_normal * f.eps).all()
+    between = torch.ones(len(flat), dtype=torch.bool, device="cuda")
+    for x in parts(between, other):
+        x.zero_()
+    assert torch.equal(flat_to[between], kept_to[between])
+    kvb.kvb_clip(li.c(), None, norm, 1000.0)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(tensors, to))
+    between.fill_(True)
+    for x in parts(between, at):
+        x.zero_()
+    assert torch.equal(flat[between], kept[between])
+    # nothing to cut: in place as it is, elsewhere a copy
+    kvb.kvb_clip(li.c(), None, norm, 1e9)
+    kvb.kvb_clip(li.c(), kvb.TensorList(to).c(), norm, 1e9)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(tensors, to)) and torch.equal(flat[between], kept[between])
