@@ -218,3 +218,46 @@ def test_the_same_bits_another_stream_and_a_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, out) and all(torch.equal(want[n], r[n]) for n in want)
+
+
+def turns(rows, width):
+    """Turns that the rows take if each is a workgroup's, and rows of a turn"""
+    if width <= 512:
+        lanes = 4
+        while lanes < 64 and 8 * lanes < width:
+            lanes *= 2
+        at_once = 256 // lanes
+    else:
+        vectors = 1 if width <= 4096 else 2 if width <= 8192 else 4
+        at_once = 512 // (-(-(-(-width // 8 // vectors)) // 64) * 64)
+    return -(-rows // at_once), at_once
+
+
+MANY = [(8, 300), (32, 1100), (8, 12300), (128, 300), (120, 1100), (64, 2500), (512, 600), (520, 521), (2056, 530), (4096, 700)]
+
+
+@pytest.mark.parametrize("dtype, x_dtype, gate", [("bf16", "f32", True), ("f16", "f16", False), ("f32", "f32", True)])
+@pytest.mark.parametrize("width, want", MANY)
+def test_gradients_of_many_turns(width, want, dtype, x_dtype, gate):
+    """More turns than workgroups, the last one not full"""
+    n = want * turns(1, width)[1] - (turns(1, width)[1] > 1)
+    assert turns(n, width)[0] == want
+    check_many(Rows(n, 1, width, dtype, x_dtype, gate=gate, seed=want))
+
+
+@pytest.mark.parametrize("dtype, x_dtype, gate", [("bf16", "bf16", True), ("f16", "f32", False), ("f32", "f32", True)])
+@pytest.mark.parametrize("n", [3, 5, 521])
+@pytest.mark.parametrize("width", [4104, 8192, 8200, 16384])
+def test_gradients_of_wide_rows(width, n, dtype, x_dtype, gate):
+    """A workgroup a row, each with a part of the sums; the last of them with two rows"""
+    assert turns(n, width) == (n, 1)
+    check_many(Rows(n, 1, width, dtype, x_dtype, gate=gate, seed=n))
+
+
+def check_many(c):
+    """Additions on the way of a term of dweight: a lane's rows (turns / parts, at most 25 + rows / 1024), 4 waves of up to 16 rows, parts by 64 and then 64"""
+    r = backward(c)
+    want = norm_backward(f64(c.x), c.weight, c.gate, EPS, c.dout, c.dsum, c.scale, 25 + c.n * c.heads // 1024 + 64 + 16 + 64)
+    for n, y in r.items():
+        if y is not None:
+            check(y, want[n], n)
