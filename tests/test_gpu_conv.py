@@ -376,3 +376,29 @@ def test_another_stream_and_a_replayed_graph():
         check_sequences(c, o, None, before)
         assert torch.equal(state[int(c.slot[0])], c.x[67:70])
         assert torch.equal(state[int(c.slot[1])], c.x[70:73])
+
+
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("T, W, heads, d", [(1, 4, (2, 4), 128), (2, 4, (2, 4), 64), (4, 3, (16, 32), 128), (8, 4, (3, 9), 32), (8, 2, (1, 2), 128)])
+def test_drafts_in_fp16(T, W, heads, d, tree):
+    test_drafts(T, W, heads, d, tree, "f16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_drafts_are_written_as_single_tokens_are(dtype):
+    """A chain of three, token by token into results that hold nothing yet: every element is written, with the bits of the drafts"""
+    B, T = 5, 3
+    c = Case([T] * B, 2, 4, 128, 4, dtype, seed=13, bias=True)
+    o, state = c.outs(), c.state0.clone()
+    kvb.kvb_conv_verify(c.sh, c.ta, c.slot, c.n_slots, T, None, c.x, c.a, c.b, state, *o)
+    kvb.kvb_conv_commit(c.sh, c.ta, c.slot, c.n_slots, T, None, torch.full((B,), T, dtype=torch.int32, device="cuda"), c.x, state, state)
+    one = c.state0.clone()
+    ta = kvb.taps(c.weight, width=4, bias=c.bias, A_log=c.A_log, dt_bias=c.dt_bias, eps=EPS)
+    for t in range(T):
+        rows = [y.view(B, T, -1)[:, t].contiguous() for y in (c.x, c.a, c.b)]
+        mine = [torch.full((B,) + tuple(y.shape[1:]), FILL, dtype=y.dtype, device="cuda") for y in o]
+        kvb.kvb_conv_decode(c.sh, ta, c.slot, c.n_slots, *rows, one, one, *mine)
+        torch.cuda.synchronize()
+        for m, y in zip(mine, o):
+            assert not (m == FILL).any() and torch.equal(m, y.view((B, T) + tuple(y.shape[1:]))[:, t])
+    assert torch.equal(one, state)
