@@ -406,7 +406,9 @@ typedef struct kvb_taps {
  *   q, k, v device, written: [n_tokens, Hk or Hv, dk] in_dtype, strides of seqs
  *   g, beta device, written: [n_tokens, Hv] fp32
  * All arithmetic is fp32, results are rounded once.  What is written must not overlap x, a and b.
- * Rows of skipped sequences (slot outside 0..n_slots-1) are not written.  A call that would take 2^32 threads is refused, here and below: 64 for each 512
+ * Rows of skipped sequences (slot outside 0..n_slots-1) are not written.  Where start does not ascend, what its sequences give, and which of their tokens
+ * are done, is not said, here and in kvb_conv_backward; nothing outside them is read or written.
+ * A call that would take 2^32 threads is refused, here and below: 64 for each 512
  * channels, and for the gates, of each token or draft, here of up to 64 tokens (each sequence is as much as 8 more).
  */
 int kvb_conv(const kvb_shape *shape, const kvb_taps *taps, const kvb_seqs *seqs, const void *x, const void *a, const void *b,
