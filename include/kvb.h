@@ -452,7 +452,7 @@ int kvb_conv_commit(const kvb_shape *shape, const kvb_taps *taps, const int32_t 
  *   dA_log, ddt_bias  device [Hv] fp32, written
  *   dstate0         device [n_slots, width - 1, C] in_dtype, written, or NULL: not wanted.  Not dstate1
  *   work            device, kvb_conv_backward_work(shape, taps, seqs) bytes, 16-byte aligned; what it holds means nothing before and after the call.
- *                   It grows with B and n_tokens
+ *                   It grows with B and n_tokens; another shape or other taps have sizes of their own, which may be more for fewer channels
  * What is written must not overlap what is read.  Rows of skipped sequences are neither written nor counted in the sums.  The same inputs give the
  * same bits.
  */
@@ -499,6 +499,7 @@ int kvb_norm(const kvb_rows *rows, const void *x, const void *res, const void *g
  *   dgate    device, written: dtype, lies as gate does; NULL if and only if there is no gate
  *   dweight  device [width] fp32, written
  *   work     device, kvb_norm_backward_work(rows) bytes, 16-byte aligned; means nothing before and after the call.  It grows with n_tokens
+ *            and heads; other widths have sizes of their own, which may be more for a narrower row
  * What is written must not overlap what is read otherwise.  The same inputs give the same bits.
  */
 int64_t kvb_norm_backward_work(const kvb_rows *rows);
@@ -529,6 +530,7 @@ int kvb_grad_norm(const kvb_list *list, float *norm, void *work, void *stream);
  *   to       tensors of the same sizes and types (only data is looked at), or NULL: in place.  None may overlap another's source
  *   norm     device fp32 [1]: kvb_grad_norm's, or what ranks that hold a part each have made of theirs
  *   largest  at least 0
+ * A result that lies otherwise among 16 bytes than its source is written element by element, in about twice the time.
  * Where nothing is to be cut, nothing is written in place.  A norm that is infinite makes every finite element 0, one that is not a number all NaN.
  */
 int kvb_clip(const kvb_list *list, const kvb_list *to, const float *norm, float largest, void *stream);

@@ -6,6 +6,8 @@
 // Bounded by memory: 43 M bf16 elements are read in 15.6 us (5.5 TB/s, eight loads of a thread on their way; four: 24.6), then read once more and written in 26.8; both with the
 // norm between them 45 us.  Results go past the caches: what of the tensors the first pass left there is then still there (plain stores: 54 us; 134 M
 // elements in place, read by an addition next: the same either way).  Eleven small tensors 9.1 us, three launches.
+// A result that lies otherwise among 16 bytes than its source goes element by element: clipping into the next tensors 63 us instead of 27.  Each workgroup looks through the list of tensors, 64 a
+// step, before its first load: those 43 M elements in 50 / 300 / 1000 / 3000 tensors 44 / 48 / 54 / 90 us.
 #include "kvb_layer_device.h"
 
 namespace kvb_impl {

@@ -86,8 +86,8 @@ __device__ __forceinline__ void gates_of(const ConvBase &a, int64_t t0, int n, i
 }  // namespace
 
 // Whole sequences: a wave takes the tokens of `length` places one after the other, with the taps' inputs in registers, and asks for four tokens ahead: one as one is taken (16
-// bits, x from the caches); four as the four ahead of them are done; or (LARGE) before those are begun.  LARGE leaves a SIMD three waves for its registers, the others
-// four (fp32: three).  us, one / four / LARGE: 300 tokens 5.7 / 6.1 / 5.8, 1000 10.9 / 11.1 / 11.3, 2000 16.1 / 16.1 / 16.5; 24 sequences of up to 1500, 4 + 8 heads, past the caches
+// bits, x from the caches); four as the four ahead of them are done; or (LARGE) before those are begun.  LARGE leaves a SIMD three waves for its registers (W = 2: four), the others
+// four (fp32 with W = 4: three).  us, one / four / LARGE: 300 tokens 5.7 / 6.1 / 5.8, 1000 10.9 / 11.1 / 11.3, 2000 16.1 / 16.1 / 16.5; 24 sequences of up to 1500, 4 + 8 heads, past the caches
 // 36.2 / 34.8 / 36.3, one of 8191 62.2 / 62.0 / 58.6; fp32, 5284 tokens, W = 3, 81 / 75 / 81.
 template <typename T, int W, bool STREAM, bool LARGE>
 __global__ __launch_bounds__(256, LARGE || sizeof(T) == 4 ? 3 : 4) void kvb_conv_kernel(const ConvArgs a, int units, int64_t length)

@@ -7,7 +7,7 @@
 // in registers, then the four waves of a workgroup add theirs in LDS and leave one part; kvb_sums_kernel adds the parts in order, so
 // the same inputs give the same bits.
 // Bounded by memory: 4 x 2048 tokens, 16 + 32 heads of 128, bf16, 408 MB (a copy: 80 us) take 97 us, 5 of them the sums and some 6 the launch and what stands ahead of a wave's first
-// token.  The vector units are busy 64 of them (counters: 32.6 M instructions; without norms the call takes 96), with two waves a SIMD (216 registers), so what counts is that all
+// token.  The vector units are busy 64 of them (counters: 32.6 M instructions; without norms the call takes 96), with two waves a SIMD (200 registers, with a bias 216), so what counts is that all
 // of those have as much to do: stretches as long as fill the card once (three rounds of shorter ones took 136), and the groups of q and k on one compute
 // unit with those of v (group by group in the launch: 97, stretch by stretch: 106).  Calls of some hundred tokens: the chain of launch, start, slot, inputs, then half a
 // microsecond a token.

@@ -323,7 +323,8 @@ struct ConvParts {
     int64_t length;
     int parts;   // a workgroup's four waves leave one
 };
-// Those of kvb_conv_backward that fit a compute unit at once: its registers (fp32: of half as many channels) leave each SIMD two waves (three)
+// kvb_conv_backward, by the figures above.  In 16 bits two is what the registers leave a SIMD (W = 2 without a bias: three); in fp32, with half as many channels a wave, they
+// leave four (W = 4 with a bias: three), and three rounds are faster than four all the same.
 constexpr int grad_rounds(bool wide) { return wide ? 3 : 2; }
 inline int64_t conv_part_limit(int units, bool wide) { return 256 * grad_rounds(wide) / units < 1 ? 1 : 256 * grad_rounds(wide) / units; }
 inline ConvParts conv_parts(int64_t n_tokens, int64_t B, int units, bool wide)

@@ -142,7 +142,8 @@ void launch_norm_typed(const NormArgs &a, hipStream_t stream)
 {
     // x and the gate past the caches where they fill much of the last level: what reads the results next finds more of them there.  us, alone and with a matrix
     // product that reads out, plain / past them: gated, 4096 x 32 heads of 128 (64 MiB) 19.4 / 19.2 and 85.1 / 85.0, 8191 41.0 / 36.5 and 144.8 / 142.9; residual, 4096 rows
-    // of 2048 12.7 / 15.2 and 68.5 / 70.8, 8191 (64 MiB) 25.6 / 25.0 and 138.4 / 138.1, 18000 57.9 / 57.2 and 345 / 340.
+    // of 2048 12.7 / 15.2 and 68.5 / 70.8, 8191 (64 MiB) 25.6 / 25.0 and 138.4 / 138.1, 18000 57.9 / 57.2 and 345 / 340.  x in fp32, gated, alone: 8191 x 32 heads of 128 beside a
+    // gate in bf16 53.8 / 47.6; 20000 x 32 all in fp32 183 / 199, so that calls all in fp32 with a gate lose 8 % by this rule, which looks at bytes alone.
     const int64_t read = a.rows * a.width * (int64_t)(sizeof(TX) + (a.gate ? sizeof(T) : 0) + (a.res ? sizeof(TX) : 0));
     const bool stream_x = read > 96 << 20;
     const int vectors = a.width / 8;
